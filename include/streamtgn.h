@@ -278,7 +278,79 @@ int stgn_kernel_times(stgn_ctx *ctx, int enable, int reset, uint32_t cap,
 int stgn_probe_gather(const float *table, uint64_t n_rows, uint32_t row_bytes, const uint32_t *idx,
                       uint32_t n_groups, uint32_t per_group, float *out, void *hip_stream);
 
-const char *stgn_last_error(const stgn_ctx *ctx);   /* NULL ctx: message of the last failed create */
+/* ---- Operators on the caller's tensors: the dense product and the attention of the model's layers and heads, with
+ * their gradients.  They need no context: a program that learns the parameters of a head or a layer runs them on its own
+ * device memory, and what they give forwards is what the layers and heads of a context compute (a head's layers:
+ * stgn_set_predictor_mlp).
+ *  - Every pointer is a device pointer of the current device, aligned to its element; the stream is one of that device.
+ *    Calls are asynchronous, allocate nothing, copy nothing to or from the host and may be captured into a HIP graph.
+ *  - device_workspace: the caller's, 256-byte aligned, of the size the _workspace function tells for the same arguments
+ *    (0: may be NULL), in use until the stream has executed the call.  Calls that can run at the same time (two streams,
+ *    two graphs) need two workspaces.  Nothing in it outlives the call.
+ *  - Results do not depend on timing: the same arguments give the same bits.
+ *  - Elements are fp32, bf16 or fp16, one type per call; sums, softmax maxima and sums, and lse are fp32.  With 16-bit types
+ *    the factors of a second product (softmax weights, their gradients, dy act'(z)) are rounded to the type.
+ *  - Errors: STGN_E_INVALID_ARG, STGN_E_WORKSPACE or STGN_E_DEVICE, nothing enqueued; stgn_last_error(NULL) of the same
+ *    thread says why. */
+enum { STGN_F32 = 0, STGN_BF16 = 1, STGN_F16 = 2 };
+enum { STGN_ACT_NONE = 0, STGN_ACT_RELU = 1, STGN_ACT_GELU = 2 /* z Phi(z), by erf */, STGN_ACT_SILU = 3 /* z / (1 + e^-z) */ };
+
+/* Dense product.  Forward: z = x w + bias, y = act(z) + residual, and pre = z where pre is not NULL (the gradient of an
+ * activation needs it).  Gradient, from dy: dz = dy act'(pre), dx = dz w^T, dw = x^T dz, db = column sums of dz; a gradient
+ * whose pointer is NULL is not computed (the residual's is dy).  relu's slope at 0 is 0.
+ * x: [rows x d_in]; w: [d_in x d_out]; bias, db: [d_out]; residual, y, pre, dy: [rows x d_out]; rows lie ld_* elements apart, the
+ * numbers of a row side by side; dx and dw are dense.  bias and residual may be NULL.  rows may be 0 (dw and db are then
+ * zeros), d_in and d_out lie in 1 .. 2^24.  Outputs overlap nothing, except that y may be the residual itself. */
+typedef struct {
+  uint32_t dtype, activation;
+  uint32_t rows, d_in, d_out;
+  uint32_t reserved;                                          /* 0 */
+  uint64_t ld_x, ld_w, ld_residual, ld_y, ld_pre, ld_dy;
+  const void *x, *w, *bias, *residual;
+  void *y, *pre;                                              /* forward: written (pre: nullable); gradient: pre is read, y is not */
+  const void *dy;                                             /* gradient only, as all that follow */
+  void *dx, *dw, *db;
+} stgn_linear_args;
+
+/* Workspace bytes of the forward call and of the gradient (each nullable).  The gradient's depends on which of dx, dw, db are
+ * not NULL, on the activation and on the sizes; no pointer is followed. */
+int stgn_linear_workspace(const stgn_linear_args *args, size_t *forward_bytes, size_t *grad_bytes);
+int stgn_linear(const stgn_linear_args *args, void *device_workspace, size_t device_bytes, void *hip_stream);
+int stgn_linear_grad(const stgn_linear_args *args, void *device_workspace, size_t device_bytes, void *hip_stream);
+
+/* Softmax attention of `lists` lists of queries over their lists of keys (Eq. attn_detail for one query per list: a node over
+ * its recent neighbours).  Query i of a list sees key j when j < k_lens[list] and, with causal = 1, the lists being aligned at
+ * their ends (query i stands at k_lens - q_lens + i), j is not behind it; with a window of w > 0 (causal only) it sees the last
+ * w of those.  s_ij = scale q_i . k_j, lse_i = log sum_j exp s_ij, out_i = sum_j exp(s_ij - lse_i) v_j.  A query that sees no key
+ * has out = 0, lse = -infinity and gives no gradient.
+ * q, dout: [lists x q_len x heads x d_head], k, v: [lists x k_len x kv_heads x d_head], element strides for list, row and head (0:
+ * the same for all), the numbers of a head side by side; query head h reads key head h / (heads / kv_heads).  out, dq (as q) and
+ * dk, dv (as k) are dense; lse: dense fp32 [lists x heads x q_len].  q_lens, k_lens: int32 [lists], NULL: q_len, k_len for every
+ * list; values outside 0 .. q_len or k_len count as the nearer end.  Keys and values behind a list's end are not read.  Queries and dout rows
+ * behind its end are not read either; their out and dq rows, and the dk and dv rows behind the keys' end, are zeros, their lse
+ * -infinity.  A masked key inside its list's length may hold anything finite.
+ * d_head <= 256, kv_heads divides heads; lists, q_len, k_len may be 0.
+ * The gradient reads q, k, v, out, lse (as the forward call wrote them) and dout, and recomputes the softmax weights. */
+typedef struct {
+  uint32_t dtype, causal, window;
+  uint32_t lists, q_len, k_len, heads, kv_heads, d_head;
+  float scale;
+  uint64_t q_list, q_row, q_head, k_list, k_row, k_head, v_list, v_row, v_head, dout_list, dout_row, dout_head;
+  const int32_t *q_lens, *k_lens;
+  const void *q, *k, *v;
+  void *out;                                                  /* forward: written; gradient: read */
+  float *lse;
+  const void *dout;                                           /* gradient only, as all that follow */
+  void *dq, *dk, *dv;
+} stgn_attention_args;
+
+/* Workspace bytes of the forward call and of the gradient (each nullable), from dtype and sizes alone. */
+int stgn_attention_workspace(const stgn_attention_args *args, size_t *forward_bytes, size_t *grad_bytes);
+int stgn_attention(const stgn_attention_args *args, void *device_workspace, size_t device_bytes, void *hip_stream);
+int stgn_attention_grad(const stgn_attention_args *args, void *device_workspace, size_t device_bytes, void *hip_stream);
+
+/* NULL ctx: message of the thread's last failed call without a context (create, workspace queries, operators) */
+const char *stgn_last_error(const stgn_ctx *ctx);
 const char *stgn_version(void);
 
 #ifdef __cplusplus

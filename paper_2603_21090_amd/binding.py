@@ -48,6 +48,19 @@ class BatchStats(C.Structure):
                     us_stage=dict(zip(("sort", "memory", "apply", "propagate", "embed", "total"), self.us_stage)))
 
 
+class LinearArgs(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("dtype", "activation", "rows", "d_in", "d_out", "reserved")] + \
+               [(n, C.c_uint64) for n in ("ld_x", "ld_w", "ld_residual", "ld_y", "ld_pre", "ld_dy")] + \
+               [(n, C.c_void_p) for n in ("x", "w", "bias", "residual", "y", "pre", "dy", "dx", "dw", "db")]
+
+
+class AttentionArgs(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("dtype", "causal", "window", "lists", "q_len", "k_len", "heads", "kv_heads", "d_head")] + \
+               [("scale", C.c_float)] + \
+               [(f"{t}_{n}", C.c_uint64) for t in ("q", "k", "v", "dout") for n in ("list", "row", "head")] + \
+               [(n, C.c_void_p) for n in ("q_lens", "k_lens", "q", "k", "v", "out", "lse", "dout", "dq", "dk", "dv")]
+
+
 class StgnError(RuntimeError):
     def __init__(self, code, msg=""):
         super().__init__(f"libstreamtgn: {ERRORS.get(code, code)} ({code}) {msg}")
@@ -60,7 +73,8 @@ EXPORTS = ("stgn_query_workspace", "stgn_create", "stgn_destroy", "stgn_ingest_b
            "stgn_full_rebuild", "stgn_sync", "stgn_get_affected", "stgn_get_neighbors", "stgn_get_history",
            "stgn_get_memory", "stgn_get_totals", "stgn_kernel_times", "stgn_last_error", "stgn_version",
            "stgn_set_predictor", "stgn_predict_batch", "stgn_predict_batch_static", "stgn_drift_status",
-           "stgn_maintain", "stgn_probe_gather")
+           "stgn_maintain", "stgn_probe_gather", "stgn_linear_workspace", "stgn_linear", "stgn_linear_grad",
+           "stgn_attention_workspace", "stgn_attention", "stgn_attention_grad")
 
 
 def load_library():
@@ -94,6 +108,10 @@ def load_library():
     L.stgn_drift_status.argtypes = [vp, C.POINTER(C.c_double), _u32p, vp]
     L.stgn_maintain.argtypes = [vp, C.c_double, C.c_double, C.POINTER(C.c_int), _u32p]
     L.stgn_probe_gather.argtypes = [vp, C.c_uint64, C.c_uint32, vp, C.c_uint32, C.c_uint32, vp, vp]
+    for op, args in (("linear", LinearArgs), ("attention", AttentionArgs)):
+        getattr(L, f"stgn_{op}_workspace").argtypes = [C.POINTER(args), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]
+        for name in (f"stgn_{op}", f"stgn_{op}_grad"):
+            getattr(L, name).argtypes = [C.POINTER(args), vp, C.c_size_t, vp]
     L.stgn_last_error.argtypes = [vp]
     L.stgn_last_error.restype = C.c_char_p
     L.stgn_version.restype = C.c_char_p
@@ -132,6 +150,162 @@ def probe_gather(table, idx, per_group, out, stream=0):
                                           out.data_ptr(), stream)
     if rc:
         raise StgnError(rc)
+
+
+# ---- operators on the caller's tensors: torch device tensors in, new tensors out, on the current stream of their device
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+
+
+def _dtype_code(t):
+    import torch
+    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(t.dtype)
+    if code is None:
+        raise ValueError(f"elements must be float32, bfloat16 or float16, not {t.dtype}")
+    return code
+
+
+def _expect(name, t, like, shape):
+    """A tensor of this shape, of `like`'s type and device, whose last dimension lies side by side."""
+    if t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{name}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.numel() and shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: the numbers of a row must lie side by side (last stride {t.stride(-1)})")
+    return t
+
+
+def _ld(t):
+    """Elements between the rows of a matrix; any value that covers a row where there is one row at most."""
+    ld = t.stride(0)
+    if t.shape[0] <= 1:
+        return max(ld, t.shape[1])
+    if ld < t.shape[1]:
+        raise ValueError(f"rows of {t.shape[1]} numbers lie {ld} apart")
+    return ld
+
+
+def _run_operator(op, suffix, args, device):
+    """Workspace of the call (the caching allocator's, on the current stream), then the call."""
+    import torch
+    L = load_library()
+    if device.type != "cuda":
+        raise ValueError(f"tensors must be on the GPU, not on {device}")
+    n = C.c_size_t(0)
+    ask = (None, C.byref(n)) if suffix else (C.byref(n), None)
+    rc = getattr(L, f"stgn_{op}_workspace")(C.byref(args), *ask)
+    if rc == 0:
+        with torch.cuda.device(device):
+            ws = torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None
+            rc = getattr(L, f"stgn_{op}{suffix}")(C.byref(args), ws.data_ptr() if n.value else None, n.value,
+                                                  torch.cuda.current_stream(device).cuda_stream)
+    if rc:
+        raise StgnError(rc, L.stgn_last_error(None).decode())
+
+
+def linear(x, w, bias=None, activation="none", residual=None, keep_pre=False):
+    """y = act(x w + bias) + residual (stgn_linear): x [rows, d_in], w [d_in, d_out], bias [d_out], residual [rows, d_out], all
+    of one type (float32, bfloat16, float16); activation: "none", "relu", "gelu", "silu".  Returns y, or (y, pre) with
+    keep_pre: the values in front of the activation, which linear_grad needs."""
+    import torch
+    if x.dim() != 2 or w.dim() != 2:
+        raise ValueError("x and w must be matrices")
+    a = LinearArgs(dtype=_dtype_code(x), activation=ACTIVATIONS[activation], rows=x.shape[0], d_in=x.shape[1], d_out=w.shape[1])
+    _expect("x", x, x, x.shape)
+    _expect("w", w, x, (x.shape[1], w.shape[1]))
+    shape = (x.shape[0], w.shape[1])
+    y = torch.empty(shape, dtype=x.dtype, device=x.device)
+    a.x, a.w, a.y = x.data_ptr(), w.data_ptr(), y.data_ptr()
+    a.ld_x, a.ld_w, a.ld_y = _ld(x), _ld(w), w.shape[1]
+    if bias is not None:
+        a.bias = _expect("bias", bias, x, (w.shape[1],)).data_ptr()
+    if residual is not None:
+        a.residual, a.ld_residual = _expect("residual", residual, x, shape).data_ptr(), _ld(residual)
+    pre = torch.empty_like(y) if keep_pre else None
+    if keep_pre:
+        a.pre, a.ld_pre = pre.data_ptr(), w.shape[1]
+    _run_operator("linear", "", a, x.device)
+    return (y, pre) if keep_pre else y
+
+
+def linear_grad(dy, x, w, activation="none", pre=None, bias=True, need_x=True, need_w=True):
+    """Gradients of linear (stgn_linear_grad): (dx, dw, db), None for those not asked for.  pre: what linear kept, needed with an
+    activation.  The residual's gradient is dy itself."""
+    import torch
+    if x.dim() != 2 or w.dim() != 2:
+        raise ValueError("x and w must be matrices")
+    a = LinearArgs(dtype=_dtype_code(x), activation=ACTIVATIONS[activation], rows=x.shape[0], d_in=x.shape[1], d_out=w.shape[1])
+    _expect("x", x, x, x.shape)
+    _expect("w", w, x, (x.shape[1], w.shape[1]))
+    _expect("dy", dy, x, (x.shape[0], w.shape[1]))
+    a.x, a.w, a.dy = x.data_ptr(), w.data_ptr(), dy.data_ptr()
+    a.ld_x, a.ld_w, a.ld_dy = _ld(x), _ld(w), _ld(dy)
+    if activation != "none":
+        if pre is None:
+            raise ValueError("the gradient of an activation needs pre")
+        a.pre, a.ld_pre = _expect("pre", pre, x, dy.shape).data_ptr(), _ld(pre)
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_x else None
+    dw = torch.empty(w.shape, dtype=x.dtype, device=x.device) if need_w else None
+    db = torch.empty(w.shape[1], dtype=x.dtype, device=x.device) if bias else None
+    a.dx, a.dw, a.db = (t.data_ptr() if t is not None else None for t in (dx, dw, db))
+    _run_operator("linear", "_grad", a, x.device)
+    return dx, dw, db
+
+
+def _attention_args(q, k, v, q_lens, k_lens, causal, window, scale):
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q, k and v must be [lists, rows, heads, numbers]")
+    _expect("q", q, q, q.shape)
+    _expect("k", k, q, (q.shape[0], k.shape[1], k.shape[2], q.shape[3]))
+    _expect("v", v, q, k.shape)
+    for name, t in (("q_lens", q_lens), ("k_lens", k_lens)):
+        if t is not None:
+            import torch
+            if t.dtype != torch.int32 or t.device != q.device or tuple(t.shape) != (q.shape[0],) or not t.is_contiguous():
+                raise ValueError(f"{name}: a dense int32 tensor [lists] on {q.device} is expected")
+    a = AttentionArgs(dtype=_dtype_code(q), causal=int(bool(causal)), window=int(window), lists=q.shape[0], q_len=q.shape[1],
+                      k_len=k.shape[1], heads=q.shape[2], kv_heads=k.shape[2], d_head=q.shape[3],
+                      scale=q.shape[3] ** -0.5 if scale is None else scale)
+    a.q_list, a.q_row, a.q_head = q.stride()[:3]
+    a.k_list, a.k_row, a.k_head = k.stride()[:3]
+    a.v_list, a.v_row, a.v_head = v.stride()[:3]
+    a.q, a.k, a.v = q.data_ptr(), k.data_ptr(), v.data_ptr()
+    a.q_lens = q_lens.data_ptr() if q_lens is not None else None
+    a.k_lens = k_lens.data_ptr() if k_lens is not None else None
+    return a
+
+
+def attention(q, k, v, q_lens=None, k_lens=None, causal=False, window=0, scale=None):
+    """Softmax attention (stgn_attention): q [lists, q_len, heads, d], k and v [lists, k_len, kv_heads, d], any strides but for the
+    last; q_lens, k_lens: int32 [lists] on the device, None: all rows.  causal aligns the lists at their ends; window: only the last
+    `window` keys up to the query (0: all).  scale: d ** -0.5 by default.  Returns out (as q) and lse [lists, heads, q_len] fp32."""
+    import torch
+    a = _attention_args(q, k, v, q_lens, k_lens, causal, window, scale)
+    out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
+    a.out, a.lse = out.data_ptr(), lse.data_ptr()
+    _run_operator("attention", "", a, q.device)
+    return out, lse
+
+
+def attention_grad(dout, q, k, v, out, lse, q_lens=None, k_lens=None, causal=False, window=0, scale=None):
+    """Gradients of attention (stgn_attention_grad) from its inputs and outputs and dout (any strides but for the last):
+    (dq, dk, dv), dense.  Heads that share a key head add up in dk and dv."""
+    import torch
+    a = _attention_args(q, k, v, q_lens, k_lens, causal, window, scale)
+    _expect("dout", dout, q, q.shape)
+    _expect("out", out, q, q.shape)
+    if not out.is_contiguous() or not lse.is_contiguous() or lse.dtype != torch.float32 or lse.device != q.device \
+            or tuple(lse.shape) != (q.shape[0], q.shape[2], q.shape[1]):
+        raise ValueError("out and lse must be what attention returned")
+    a.dout_list, a.dout_row, a.dout_head = dout.stride()[:3]
+    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    dk = torch.empty(k.shape, dtype=q.dtype, device=q.device)
+    dv = torch.empty(k.shape, dtype=q.dtype, device=q.device)
+    a.dout, a.out, a.lse = dout.data_ptr(), out.data_ptr(), lse.data_ptr()
+    a.dq, a.dk, a.dv = dq.data_ptr(), dk.data_ptr(), dv.data_ptr()
+    _run_operator("attention", "_grad", a, q.device)
+    return dq, dk, dv
 
 
 def _marshal_weights(weights: dict, layers: int, has_memory: bool):

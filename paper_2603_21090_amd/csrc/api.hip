@@ -8,6 +8,7 @@
 
 #include "stgn_internal.h"
 #include "mfma16.h"
+#include "operators.h"
 
 using namespace stgn;
 
@@ -16,7 +17,7 @@ namespace {
 const char* const kClassNames[KC_COUNT] = {"stage_sort", "memory_update", "apply", "plan", "expand", "compact",
                                            "layer", "gather_rows", "noop", "project", "predict", "bucket_rows"};
 
-std::string g_create_error;
+thread_local std::string g_create_error;   // of the thread's last failed call without a context
 
 constexpr size_t kRowIoBytes = 1u << 20;   // pinned block of stgn_ctx::row_io
 
@@ -485,6 +486,11 @@ int sync_and_poll(stgn_ctx* ctx) {
 }
 
 }  // namespace
+
+int stgn::fail_operator(int code, const char* why) {
+  g_create_error = why;
+  return code;
+}
 
 extern "C" {
 

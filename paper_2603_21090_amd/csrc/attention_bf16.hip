@@ -1,0 +1,7 @@
+// attention kernels of one element type (a file per type: they compile beside each other)
+#include "attention.h"
+
+namespace stgn {
+hipError_t attention_bf16(const AttnArgs& a, hipStream_t s) { return attn::forward_of<__bf16>(a, s); }
+hipError_t attention_grad_bf16(const AttnArgs& a, hipStream_t s) { return attn::backward_of<__bf16>(a, s); }
+}  // namespace stgn

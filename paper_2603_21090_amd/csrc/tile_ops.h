@@ -1,0 +1,179 @@
+// Tiles of 16 x 16 products for operators on the caller's tensors, in three element types: fp32 (products in fp32), bf16 and
+// fp16 (products in 16 bits); every sum is fp32.
+//
+// One FRAGMENT is 16 bytes per lane, four floats or eight 16-bit numbers: a 16-row operand with KF elements of the summed
+// index (16 or 32).  Lane l serves row l % 16; lane group l / 16 owns E = 4 or 8 of the KF elements, and which ones does not
+// matter as long as both operands agree.  Two orders are used:
+//   straight  group g holds elements E g + j.  A row-major row in LDS gives it by one 16-byte read.
+//   split     16-bit only: group g holds 4 g + j (j < 4) and 16 + 4 g + (j - 4).  That is how two accumulator blocks lie in
+//             registers (row 4 g + r, column l % 16), so probabilities go from one product into the next without LDS.
+//             With floats one accumulator block is a fragment in the straight order.
+// An operand whose summed index runs down the rows of its LDS tile (V in P V) is read by the transposing LDS load of four
+// 16-bit numbers, or by four 4-byte reads of floats.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace stgn {
+
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+// rows of odd widths start anywhere: global memory takes wide accesses at any element's address
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+
+template <class T> struct Elem;
+
+template <> struct Elem<float> {
+  using Frag = floatx4;
+  using Four = floatx4;
+  static constexpr int E = 4, KF = 16, PB = 1;               // elements a lane, elements of the summed index, accumulator blocks a fragment
+  static __device__ inline floatx4 mma(const Frag& a, const Frag& b, floatx4 c) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[u], b[u], c, 0, 0, 0);
+    return c;
+  }
+};
+
+template <> struct Elem<__bf16> {
+  using Frag = bf16x8;
+  using Four = bf16x4;
+  static constexpr int E = 8, KF = 32, PB = 2;
+  static __device__ inline floatx4 mma(const Frag& a, const Frag& b, floatx4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+};
+
+template <> struct Elem<_Float16> {
+  using Frag = f16x8;
+  using Four = f16x4;
+  static constexpr int E = 8, KF = 32, PB = 2;
+  static __device__ inline floatx4 mma(const Frag& a, const Frag& b, floatx4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+  }
+};
+
+// PB accumulator blocks as one fragment, rounded to T: the factors of the next product (half a step each, as any 16-bit operand)
+template <class T>
+__device__ inline typename Elem<T>::Frag pack(const floatx4 (&blocks)[Elem<T>::PB]) {
+  if constexpr (Elem<T>::PB == 1) {
+    return blocks[0];
+  } else {
+    typename Elem<T>::Frag f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = (T)blocks[j / 4][j % 4];
+    return f;
+  }
+}
+
+// LDS rows of `width` elements are 16 bytes longer: 16 rows of a fragment then start in 16 different groups of four banks
+template <class T>
+__host__ __device__ constexpr int lds_stride(int width) { return width + Elem<T>::E; }
+
+// fragment of rows row .. row + 15, elements k .. k + KF - 1 of a row-major tile (straight order)
+template <class T>
+__device__ inline typename Elem<T>::Frag frag_rows(const T* tile, int stride, int row, int k) {
+  const int lane = threadIdx.x & 63;
+  return *reinterpret_cast<const typename Elem<T>::Frag*>(tile + (row + (lane & 15)) * stride + k + Elem<T>::E * (lane >> 4));
+}
+
+// four 16-bit numbers of column col + lane % 16, one from each of the rows that lane group g = lane / 16 names: row .. row + 3.
+// Sixteen lanes read four rows of 16 numbers, 8 bytes each, and get them transposed.
+template <class T>
+__device__ inline i16x4 transposed4(const T* tile, int stride, int row, int col) {
+  const int i = threadIdx.x & 15;
+  const T* p = tile + (row + (i >> 2)) * stride + col + 4 * (i & 3);
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(p));
+}
+
+// fragment of columns col .. col + 15 whose summed index runs down rows row .. row + KF - 1 of the tile
+template <class T, bool SPLIT>
+__device__ inline typename Elem<T>::Frag frag_cols(const T* tile, int stride, int row, int col) {
+  const int lane = threadIdx.x & 63, g = lane >> 4;
+  if constexpr (sizeof(T) == 4) {
+    floatx4 f;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) f[u] = tile[(row + 4 * g + u) * stride + col + (lane & 15)];
+    return f;
+  } else {
+    const i16x4 lo = transposed4(tile, stride, row + (SPLIT ? 4 * g : 8 * g), col);
+    const i16x4 hi = transposed4(tile, stride, row + (SPLIT ? 16 + 4 * g : 8 * g + 4), col);
+    typedef short i16x8 __attribute__((ext_vector_type(8)));
+    const i16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    return __builtin_bit_cast(typename Elem<T>::Frag, both);
+  }
+}
+
+// 16 bytes at p of which `count` elements exist (the rest zero)
+template <class T>
+__device__ inline u32x4 load16(const T* p, int count) {
+  constexpr int E = Elem<T>::E;
+  if (count >= E) return *reinterpret_cast<const u32x4_any*>(p);
+  union { T e[E]; u32x4 v; } u;
+  u.v = u32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int j = 0; j < E - 1; ++j)
+    if (j < count) u.e[j] = p[j];
+  return u.v;
+}
+
+// four sums as elements col .. col + 3 of a row of `cols` elements
+template <class T>
+__device__ inline void store4(T* row, int col, int cols, const floatx4& v) {
+  typename Elem<T>::Four f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) f[j] = (T)v[j];
+  if (col + 4 <= cols) {
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<u32x4_any*>(row + col) = __builtin_bit_cast(u32x4_any, f);
+    else *reinterpret_cast<u32x2_any*>(row + col) = __builtin_bit_cast(u32x2_any, f);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 3; ++j)
+      if (col + j < cols) row[col + j] = f[j];
+  }
+}
+
+template <class T>
+__device__ inline floatx4 load4(const T* row, int col, int cols) {
+  floatx4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (col + j < cols) v[j] = (float)row[col + j];
+  return v;
+}
+
+// A tile of ROWS x COLS elements on its way from global memory through registers into LDS; every thread of THREADS carries
+// NP pieces of 16 bytes.  Rows and columns that the matrix does not have are zeros: what a caller keeps there is never read.
+template <class T, int ROWS, int COLS, int THREADS>
+struct TileMove {
+  static constexpr int E = Elem<T>::E, PIECES = ROWS * COLS / E, NP = (PIECES + THREADS - 1) / THREADS;
+  u32x4 r[NP];
+
+  // row(i): the address of the tile's row i, or null if there is none.  cols: elements a row has from column 0 of the tile.
+  template <class Row>
+  __device__ inline void fetch(Row row, int cols) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int p = (int)threadIdx.x + i * THREADS, c = p % (COLS / E) * E;
+      r[i] = u32x4{0, 0, 0, 0};
+      if (PIECES % THREADS != 0 && p >= PIECES) continue;
+      const T* at = row(p / (COLS / E));
+      if (at != nullptr && c < cols) r[i] = load16(at + c, cols - c);
+    }
+  }
+  __device__ inline void store(T* tile, int stride) const {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int p = (int)threadIdx.x + i * THREADS;
+      if (PIECES % THREADS != 0 && p >= PIECES) continue;
+      *reinterpret_cast<u32x4*>(tile + p / (COLS / E) * stride + p % (COLS / E) * E) = r[i];
+    }
+  }
+};
+
+}  // namespace stgn

@@ -1,0 +1,116 @@
+"""The dense product with its epilogue and its gradients against 64 bits (bounds: operator_refs)."""
+import pytest
+import torch
+
+import operator_refs as refs
+from paper_2603_21090_amd import binding
+
+pytestmark = pytest.mark.gpu
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+# rows, d_in, d_out: single numbers, single rows and columns, odd sizes on both sides of a tile, tails shorter than 16 bytes,
+# sums long enough to be split, more than one tile each way
+SIZES = [(1, 1, 1), (1, 100, 1), (3, 7, 5), (1, 4096, 96), (5, 333, 129), (64, 64, 64), (65, 63, 127), (200, 200, 100), (17, 31, 1),
+         (129, 1, 65), (300, 257, 140), (2, 2000, 257), (16, 1027, 64), (1000, 40, 3), (700, 130, 257), (9, 640, 1030)]
+
+
+def make(rows, d_in, d_out, dt, seed=0):
+    g = torch.Generator().manual_seed(1000 * rows + 10 * d_in + d_out + seed)
+    n = lambda *s: torch.randn(*s, generator=g).to(dt)  # noqa: E731
+    return n(rows, d_in), (n(d_in, d_out).float() * d_in ** -0.5).to(dt), n(d_out), n(rows, d_out), n(rows, d_out)
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=str)
+@pytest.mark.parametrize("size", SIZES, ids=str)
+@pytest.mark.parametrize("name,bias,residual,keep", [("none", False, False, False), ("relu", True, False, True), ("gelu", True, True, True),
+                                                     ("silu", False, True, False)])
+def test_forward(size, dt, name, bias, residual, keep):
+    x, w, b, r, _ = make(*size, dt)
+    got = binding.linear(x.cuda(), w.cuda(), bias=b.cuda() if bias else None, activation=name, residual=r.cuda() if residual else None, keep_pre=keep)
+    y, z = refs.linear(x, w, b if bias else None, name, r if residual else None)
+    refs.within(got[0] if keep else got, y, "y")
+    if keep:
+        refs.within(got[1], z, "pre")
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=str)
+@pytest.mark.parametrize("size", SIZES + [(5000, 24, 40), (3001, 33, 17)], ids=str)
+@pytest.mark.parametrize("name", ["none", "relu", "gelu", "silu"])
+def test_gradients(size, dt, name):
+    x, w, b, z, dy = make(*size, dt)
+    got = binding.linear_grad(dy.cuda(), x.cuda(), w.cuda(), activation=name, pre=z.cuda() if name != "none" else None)
+    for g, want, what in zip(got, refs.linear_grad(dy, x, w, name, z), ("dx", "dw", "db")):
+        refs.within(g, want, what)
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=str)
+def test_only_the_gradients_asked_for(dt):
+    x, w, b, z, dy = (t.cuda() for t in make(130, 70, 50, dt))
+    full = binding.linear_grad(dy, x, w, activation="gelu", pre=z)
+    for need in [(True, False, False), (False, True, False), (False, False, True), (True, False, True)]:
+        got = binding.linear_grad(dy, x, w, activation="gelu", pre=z, need_x=need[0], need_w=need[1], bias=need[2])
+        for g, f, n in zip(got, full, need):
+            assert torch.equal(g, f) if n else g is None
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=str)
+def test_rows_that_lie_apart_and_start_anywhere(dt):
+    """Columns of wider matrices that start one element in: no row is aligned, and the numbers beside them are NaN."""
+    x, w, b, r, dy = make(90, 77, 45, dt)
+
+    def inside(t):
+        wide = torch.full((t.shape[0], t.shape[1] + 9), float("nan"), dtype=dt, device="cuda")
+        wide[:, 1:1 + t.shape[1]] = t.cuda()
+        return wide[:, 1:1 + t.shape[1]]
+    y, z = refs.linear(x, w, b, "silu", r)
+    got = binding.linear(inside(x), inside(w), bias=b.cuda(), activation="silu", residual=inside(r), keep_pre=True)
+    refs.within(got[0], y, "y")
+    refs.within(got[1], z, "pre")
+    for g, want, what in zip(binding.linear_grad(inside(dy), inside(x), inside(w), activation="silu", pre=inside(r)),
+                             refs.linear_grad(dy, x, w, "silu", r), ("dx", "dw", "db")):
+        refs.within(g, want, what)
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=str)
+def test_no_rows(dt):
+    x, w = torch.empty(0, 20, dtype=dt, device="cuda"), torch.ones(20, 30, dtype=dt, device="cuda")
+    y, z = binding.linear(x, w, keep_pre=True)
+    assert y.shape == z.shape == (0, 30)
+    dx, dw, db = binding.linear_grad(y, x, w)
+    assert dx.shape == (0, 20) and not dw.any() and not db.any()
+
+
+def test_infinities_and_nan_stay_in_their_rows():
+    x, w, *_ = make(70, 40, 33, torch.float32)
+    x[3, 5], x[40, 0] = float("inf"), float("nan")
+    y = binding.linear(x.cuda(), w.cuda(), activation="relu").cpu()
+    rows = torch.ones(70, dtype=torch.bool)
+    rows[3] = rows[40] = False
+    refs.within(y[rows], tuple(t for t in refs.linear(x[rows], w, None, "relu", None)[0]), "y")
+    assert not torch.isfinite(y[3]).all()
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=str)
+def test_the_same_bits_again_on_another_stream_and_in_a_graph(dt):
+    x, w, b, z, dy = (t.cuda() for t in make(300, 500, 200, dt))
+
+    def step():
+        y, pre = binding.linear(x, w, bias=b, activation="gelu", residual=z, keep_pre=True)
+        return (y, pre) + binding.linear_grad(dy, x, w, activation="gelu", pre=pre)
+    first = step()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = step()
+    torch.cuda.current_stream().wait_stream(side)
+    for a, c in zip(first, other):
+        assert torch.equal(a, c)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kept = step()
+    for turn in range(3):
+        x.mul_(-1 if turn else 1)                             # new contents for every replay
+        graph.replay()
+        eager = step()
+        torch.cuda.synchronize()
+        for a, c in zip(kept, eager):
+            assert torch.equal(a, c)
