@@ -57,7 +57,7 @@ class LinearArgs(C.Structure):
 class AttentionArgs(C.Structure):
     _fields_ = [(n, C.c_uint32) for n in ("dtype", "causal", "window", "lists", "q_len", "k_len", "heads", "kv_heads", "d_head")] + \
                [("scale", C.c_float)] + \
-               [(f"{t}_{n}", C.c_uint64) for t in ("q", "k", "v", "dout") for n in ("list", "row", "head")] + \
+               [(f"{t}_{n}", C.c_uint64) for t in ("q", "k", "v", "out", "dout") for n in ("list", "row", "head")] + \
                [(n, C.c_void_p) for n in ("q_lens", "k_lens", "q", "k", "v", "out", "lse", "dout", "dq", "dk", "dv")]
 
 
@@ -284,21 +284,23 @@ def attention(q, k, v, q_lens=None, k_lens=None, causal=False, window=0, scale=N
     out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
     a.out, a.lse = out.data_ptr(), lse.data_ptr()
+    a.out_list, a.out_row, a.out_head = out.stride()[:3]
     _run_operator("attention", "", a, q.device)
     return out, lse
 
 
 def attention_grad(dout, q, k, v, out, lse, q_lens=None, k_lens=None, causal=False, window=0, scale=None):
-    """Gradients of attention (stgn_attention_grad) from its inputs and outputs and dout (any strides but for the last):
+    """Gradients of attention (stgn_attention_grad) from its inputs and outputs and dout (out, dout: any strides but for the last):
     (dq, dk, dv), dense.  Heads that share a key head add up in dk and dv."""
     import torch
     a = _attention_args(q, k, v, q_lens, k_lens, causal, window, scale)
     _expect("dout", dout, q, q.shape)
     _expect("out", out, q, q.shape)
-    if not out.is_contiguous() or not lse.is_contiguous() or lse.dtype != torch.float32 or lse.device != q.device \
+    if not lse.is_contiguous() or lse.dtype != torch.float32 or lse.device != q.device \
             or tuple(lse.shape) != (q.shape[0], q.shape[2], q.shape[1]):
-        raise ValueError("out and lse must be what attention returned")
+        raise ValueError("lse must be what attention returned")
     a.dout_list, a.dout_row, a.dout_head = dout.stride()[:3]
+    a.out_list, a.out_row, a.out_head = out.stride()[:3]
     dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     dk = torch.empty(k.shape, dtype=q.dtype, device=q.device)
     dv = torch.empty(k.shape, dtype=q.dtype, device=q.device)

@@ -227,7 +227,7 @@ __global__ __launch_bounds__(WAVES * 64) void forward_kernel(AttnArgs a) {
     const int i = query_of(a, r[c]), head = hk * a.group + r[c] - i * a.group;
     const bool any = hi[c] > lo[c];
     const float inv = any ? 1.f / total : 0.f;
-    T* row = dense_row<T>(a, a.o, a.q_len, a.heads, b, i, head);
+    T* row = const_cast<T*>(row_of<T>(a.o, a.so, b, i, head));
 #pragma unroll
     for (int x = 0; x < DB; ++x) {
       floatx4 v = any ? o[x][c] * inv : floatx4{0.f, 0.f, 0.f, 0.f};
@@ -251,7 +251,7 @@ __global__ __launch_bounds__(256) void delta_kernel(AttnArgs a) {
     float acc = 0.f;
     if (i < qn) {
       const T* p = row_of<T>(a.dout, a.sdo, b, i, head);
-      const T* o = static_cast<const T*>(a.out) + x * a.d;
+      const T* o = row_of<T>(a.out, a.so, b, i, head);
       for (int c = sub; c < a.d; c += 16) acc = fmaf((float)p[c], (float)o[c], acc);
     }
     for (int w = 8; w > 0; w >>= 1) acc += __shfl_xor(acc, w);

@@ -1,4 +1,4 @@
-// attention kernels of one element type (a file per type: they compile beside each other)
+// attention of one element type: lists of many queries (a file per type and kind: they compile beside each other)
 #include "attention.h"
 
 namespace stgn {

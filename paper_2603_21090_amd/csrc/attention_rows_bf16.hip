@@ -1,0 +1,7 @@
+// attention of one element type: lists of few queries
+#include "attention_rows.h"
+
+namespace stgn {
+hipError_t attention_rows_bf16(const AttnArgs& a, float* part, hipStream_t s) { return attn::rows_of<__bf16, false>(a, part, s); }
+hipError_t attention_rows_grad_bf16(const AttnArgs& a, float* part, hipStream_t s) { return attn::rows_of<__bf16, true>(a, part, s); }
+}  // namespace stgn

@@ -11,12 +11,12 @@ namespace stgn {
 struct Strides { int64_t list, row, head; };                  // in elements; the numbers of one head lie side by side
 
 struct AttnArgs {
-  const void *q, *k, *v, *dout, *out;                         // out, o, dq, dk, dv: dense [lists, rows, heads, d]
+  const void *q, *k, *v, *dout, *out;                         // dq, dk, dv: dense [lists, rows, heads, d]
   void *o, *dq, *dk, *dv;
   float* lse;                                                 // [lists, heads, q_len]
   float* delta;                                               // workspace of the gradient: dout . out, laid out as lse
   const int *q_lens, *k_lens;                                 // [lists] or null: every list is q_len, k_len long
-  Strides sq, sk, sv, sdo;
+  Strides sq, sk, sv, so, sdo;
   int lists, q_len, k_len, heads, kv_heads, group, d;
   int causal, window;
   float scale;

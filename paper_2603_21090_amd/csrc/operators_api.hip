@@ -1,7 +1,8 @@
 // extern "C" boundary of the operators on the caller's tensors: argument checks and dispatch by element type.
 #include <math.h>
-#include <stdio.h>
+#include <utility>
 
+#include "attention_rows.h"
 #include "operators.h"
 #include "streamtgn.h"
 
@@ -10,6 +11,8 @@ namespace stgn {
 #define STGN_PER_TYPE(T)                                                                  \
   hipError_t attention_##T(const AttnArgs& a, hipStream_t s);                             \
   hipError_t attention_grad_##T(const AttnArgs& a, hipStream_t s);                        \
+  hipError_t attention_rows_##T(const AttnArgs& a, float* part, hipStream_t s);           \
+  hipError_t attention_rows_grad_##T(const AttnArgs& a, float* part, hipStream_t s);      \
   size_t linear_bytes_##T(const LinearArgs& a);                                           \
   size_t linear_grad_bytes_##T(const LinearGradArgs& a);                                  \
   hipError_t linear_##T(const LinearArgs& a, void* ws, hipStream_t s);                    \
@@ -26,8 +29,13 @@ size_t linear_bytes(const LinearArgs& a, int dtype) { return STGN_BY_TYPE(dtype,
 size_t linear_grad_bytes(const LinearGradArgs& a, int dtype) { return STGN_BY_TYPE(dtype, linear_grad_bytes, a); }
 hipError_t launch_linear(const LinearArgs& a, int dtype, void* ws, hipStream_t s) { return STGN_BY_TYPE(dtype, linear, a, ws, s); }
 
-size_t attention_grad_bytes(const AttnArgs& a) {              // delta
-  return (size_t)a.lists * a.q_len * a.heads * sizeof(float);
+bool few_rows(const AttnArgs& a, int dtype, bool grad) {
+  return (int64_t)a.q_len * a.group <= attn::most_rows(grad, dtype != STGN_F32);
+}
+
+size_t attention_bytes(const AttnArgs& a, int dtype) { return few_rows(a, dtype, false) ? attn::row_part_bytes(a, false) : 0; }
+size_t attention_grad_bytes(const AttnArgs& a, int dtype) {
+  return few_rows(a, dtype, true) ? attn::row_part_bytes(a, true) : (size_t)a.lists * a.q_len * a.heads * sizeof(float);   // delta
 }
 
 }  // namespace stgn
@@ -125,6 +133,20 @@ LinearGradArgs linear_grad_args(const stgn_linear_args* a) {
   return l;
 }
 
+// whether the rows of d numbers at these strides lie clear of each other: each stride reaches over all that smaller ones span
+bool apart(uint64_t n0, uint64_t s0, uint64_t n1, uint64_t s1, uint64_t n2, uint64_t s2, uint64_t d) {
+  uint64_t n[3] = {n0, n1, n2}, s[3] = {s0, s1, s2}, span = d;
+  for (int i = 0; i < 3; ++i)
+    for (int j = 0; j < 2; ++j)
+      if (s[j] > s[j + 1]) { std::swap(s[j], s[j + 1]); std::swap(n[j], n[j + 1]); }
+  for (int i = 0; i < 3; ++i) {
+    if (n[i] <= 1) continue;
+    if (s[i] < span) return false;
+    span += (n[i] - 1) * s[i];
+  }
+  return true;
+}
+
 int check_attention(const stgn_attention_args* a, bool grad, bool sizes_only) {
   if (!a) return no("NULL arguments");
   if (a->dtype > STGN_F16) return no("dtype must be STGN_F32, STGN_BF16 or STGN_F16");
@@ -146,7 +168,7 @@ int check_attention(const stgn_attention_args* a, bool grad, bool sizes_only) {
   for (const void* p : all)
     if (!aligned(p, es)) return no("a pointer is not aligned to its element");
   if (!aligned(a->lse, 4) || !aligned(a->q_lens, 4) || !aligned(a->k_lens, 4)) return no("a pointer is not aligned to its element");
-  const uint64_t strides[] = {a->q_list, a->q_row, a->q_head, a->k_list, a->k_row, a->k_head, a->v_list, a->v_row, a->v_head};
+  const uint64_t strides[] = {a->q_list, a->q_row, a->q_head, a->k_list, a->k_row, a->k_head, a->v_list, a->v_row, a->v_head, a->out_list, a->out_row, a->out_head};
   for (uint64_t s : strides)
     if (s > kMaxLd) return no("a stride is out of range");
   const bool have_q = a->lists && a->q_len, have_k = a->lists && a->k_len;
@@ -160,11 +182,12 @@ int check_attention(const stgn_attention_args* a, bool grad, bool sizes_only) {
   const uint64_t nq = (uint64_t)a->lists * a->q_len * a->heads, nk = (uint64_t)a->lists * a->k_len * a->kv_heads;
   const Span q = reach(a->q, a->q_len, a->heads, a->q_list, a->q_row, a->q_head), k = reach(a->k, a->k_len, a->kv_heads, a->k_list, a->k_row, a->k_head),
              v = reach(a->v, a->k_len, a->kv_heads, a->v_list, a->v_row, a->v_head);
-  const Span o = span_of(a->out, 1, nq * a->d_head, 0, es), lse = span_of(a->lse, 1, nq, 0, 4);
+  const Span o = reach(a->out, a->q_len, a->heads, a->out_list, a->out_row, a->out_head), lse = span_of(a->lse, 1, nq, 0, 4);
   if (!grad) {
     for (const Span& s : {q, k, v})
       if (meet(o, s) || meet(lse, s)) return no("an output overlaps an input");
     if (meet(o, lse)) return no("out and lse overlap");
+    if (!apart(a->lists, a->out_list, a->q_len, a->out_row, a->heads, a->out_head, a->d_head)) return no("two numbers of out share a place");
     return STGN_OK;
   }
   if (a->dout_list > kMaxLd || a->dout_row > kMaxLd || a->dout_head > kMaxLd) return no("a stride is out of range");
@@ -189,6 +212,7 @@ AttnArgs attention_args(const stgn_attention_args* a) {
   t.sq = {(int64_t)a->q_list, (int64_t)a->q_row, (int64_t)a->q_head};
   t.sk = {(int64_t)a->k_list, (int64_t)a->k_row, (int64_t)a->k_head};
   t.sv = {(int64_t)a->v_list, (int64_t)a->v_row, (int64_t)a->v_head};
+  t.so = {(int64_t)a->out_list, (int64_t)a->out_row, (int64_t)a->out_head};
   t.sdo = {(int64_t)a->dout_list, (int64_t)a->dout_row, (int64_t)a->dout_head};
   t.lists = (int)a->lists; t.q_len = (int)a->q_len; t.k_len = (int)a->k_len;
   t.heads = (int)a->heads; t.kv_heads = (int)a->kv_heads; t.group = (int)(a->heads / a->kv_heads); t.d = (int)a->d_head;
@@ -225,23 +249,28 @@ int stgn_linear_grad(const stgn_linear_args* args, void* device_workspace, size_
 int stgn_attention_workspace(const stgn_attention_args* args, size_t* forward_bytes, size_t* grad_bytes) {
   if (const int rc = check_attention(args, false, true)) return rc;
   const AttnArgs a = attention_args(args);
-  if (forward_bytes) *forward_bytes = 0;
-  if (grad_bytes) *grad_bytes = attention_grad_bytes(a);
+  if (forward_bytes) *forward_bytes = attention_bytes(a, (int)args->dtype);
+  if (grad_bytes) *grad_bytes = attention_grad_bytes(a, (int)args->dtype);
   return STGN_OK;
 }
 
 int stgn_attention(const stgn_attention_args* args, void* device_workspace, size_t device_bytes, void* hip_stream) {
   if (const int rc = check_attention(args, false, false)) return rc;
   const AttnArgs a = attention_args(args);
+  if (const int rc = check_workspace(attention_bytes(a, (int)args->dtype), device_workspace, device_bytes)) return rc;
   if (a.lists == 0 || a.q_len == 0) return STGN_OK;
+  if (few_rows(a, (int)args->dtype, false))
+    return finish(STGN_BY_TYPE(args->dtype, attention_rows, a, static_cast<float*>(device_workspace), static_cast<hipStream_t>(hip_stream)));
   return finish(STGN_BY_TYPE(args->dtype, attention, a, static_cast<hipStream_t>(hip_stream)));
 }
 
 int stgn_attention_grad(const stgn_attention_args* args, void* device_workspace, size_t device_bytes, void* hip_stream) {
   if (const int rc = check_attention(args, true, false)) return rc;
   AttnArgs a = attention_args(args);
-  if (const int rc = check_workspace(attention_grad_bytes(a), device_workspace, device_bytes)) return rc;
+  if (const int rc = check_workspace(attention_grad_bytes(a, (int)args->dtype), device_workspace, device_bytes)) return rc;
   if (a.lists == 0) return STGN_OK;
+  if (few_rows(a, (int)args->dtype, true))
+    return finish(STGN_BY_TYPE(args->dtype, attention_rows_grad, a, static_cast<float*>(device_workspace), static_cast<hipStream_t>(hip_stream)));
   a.delta = static_cast<float*>(device_workspace);
   return finish(STGN_BY_TYPE(args->dtype, attention_grad, a, static_cast<hipStream_t>(hip_stream)));
 }

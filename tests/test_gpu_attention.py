@@ -72,6 +72,17 @@ def test_strides_of_heads_first_of_packed_rows_and_of_shared_lists(dt):
 
 
 @pytest.mark.parametrize("dt", TYPES, ids=str)
+def test_outputs_kept_heads_first(dt):
+    q, k, v, do, qn, kn = make(3, 30, 50, 4, 2, 36, True, dt)
+    Q, K, V, DO, QN, KN = on_gpu(q, k, v, do, qn, kn)
+    out, lse = binding.attention(Q, K, V, q_lens=QN, k_lens=KN)
+    kept = out.transpose(1, 2).contiguous().transpose(1, 2)
+    for a, b in zip(binding.attention_grad(DO, Q, K, V, out, lse, q_lens=QN, k_lens=KN),
+                    binding.attention_grad(DO, Q, K, V, kept, lse, q_lens=QN, k_lens=KN)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=str)
 @pytest.mark.parametrize("ql", [1, 4, 40])
 def test_large_scores_and_other_scales(dt, ql):
     """Scores up to some hundreds: softmax weights of zero and one, nothing overflows; a scale of its own, zero and negative ones."""

@@ -30,7 +30,7 @@ def linear_args(**kw):
 def attention_args(**kw):
     base = dict(dtype=1, causal=0, window=0, lists=2, q_len=5, k_len=9, heads=4, kv_heads=2, d_head=16, scale=0.25,
                 q_list=320, q_row=64, q_head=16, k_list=288, k_row=32, k_head=16, v_list=288, v_row=32, v_head=16,
-                dout_list=320, dout_row=64, dout_head=16, q_lens=1 << 20, k_lens=2 << 20, q=3 << 20, k=4 << 20, v=5 << 20,
+                out_list=320, out_row=64, out_head=16, dout_list=320, dout_row=64, dout_head=16, q_lens=1 << 20, k_lens=2 << 20, q=3 << 20, k=4 << 20, v=5 << 20,
                 out=6 << 20, lse=7 << 20, dout=8 << 20, dq=9 << 20, dk=10 << 20, dv=11 << 20)
     base.update(kw)
     return binding.AttentionArgs(**base)
@@ -62,7 +62,7 @@ MASKS = [dict(dtype=3), dict(d_head=0), dict(d_head=257), dict(heads=0), dict(kv
          dict(q_lens=(1 << 20) + 2), dict(k_row=1 << 41), dict(lists=1 << 26, q_len=64)]
 
 
-@pytest.mark.parametrize("bad", MASKS + [dict(out=3 << 20), dict(out=4 << 20), dict(lse=5 << 20), dict(lse=6 << 20)], ids=str)
+@pytest.mark.parametrize("bad", MASKS + [dict(out=3 << 20), dict(out_head=15), dict(out_row=0), dict(out_list=319), dict(out=4 << 20), dict(lse=5 << 20), dict(lse=6 << 20)], ids=str)
 def test_attention_refuses(lib, bad):
     assert lib.stgn_attention(C.byref(attention_args(**bad)), None, 0, None) == INVALID
     assert lib.stgn_last_error(None)
