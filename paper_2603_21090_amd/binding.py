@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -61,6 +62,11 @@ class AttentionArgs(C.Structure):
                [(n, C.c_void_p) for n in ("q_lens", "k_lens", "q", "k", "v", "out", "lse", "dout", "dq", "dk", "dv")]
 
 
+# the same two, packed at once: a call's arguments cost the host a microsecond, not one per field
+_PACK_LINEAR, _PACK_ATTENTION = struct.Struct("@6I6Q10P"), struct.Struct("@9If15Q11P")
+assert _PACK_LINEAR.size == C.sizeof(LinearArgs) and _PACK_ATTENTION.size == C.sizeof(AttentionArgs)
+
+
 class StgnError(RuntimeError):
     def __init__(self, code, msg=""):
         super().__init__(f"libstreamtgn: {ERRORS.get(code, code)} ({code}) {msg}")
@@ -108,10 +114,10 @@ def load_library():
     L.stgn_drift_status.argtypes = [vp, C.POINTER(C.c_double), _u32p, vp]
     L.stgn_maintain.argtypes = [vp, C.c_double, C.c_double, C.POINTER(C.c_int), _u32p]
     L.stgn_probe_gather.argtypes = [vp, C.c_uint64, C.c_uint32, vp, C.c_uint32, C.c_uint32, vp, vp]
-    for op, args in (("linear", LinearArgs), ("attention", AttentionArgs)):
-        getattr(L, f"stgn_{op}_workspace").argtypes = [C.POINTER(args), C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]
+    for op in ("linear", "attention"):
+        getattr(L, f"stgn_{op}_workspace").argtypes = [vp, vp, vp]
         for name in (f"stgn_{op}", f"stgn_{op}_grad"):
-            getattr(L, name).argtypes = [C.POINTER(args), vp, C.c_size_t, vp]
+            getattr(L, name).argtypes = [vp, vp, C.c_size_t, vp]
     L.stgn_last_error.argtypes = [vp]
     L.stgn_last_error.restype = C.c_char_p
     L.stgn_version.restype = C.c_char_p
@@ -154,53 +160,67 @@ def probe_gather(table, idx, per_group, out, stream=0):
 
 # ---- operators on the caller's tensors: torch device tensors in, new tensors out, on the current stream of their device
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+_dtypes = None
 
 
 def _dtype_code(t):
-    import torch
-    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(t.dtype)
+    global _dtypes
+    if _dtypes is None:
+        import torch
+        _dtypes = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    code = _dtypes.get(t.dtype)
     if code is None:
         raise ValueError(f"elements must be float32, bfloat16 or float16, not {t.dtype}")
     return code
 
 
 def _expect(name, t, like, shape):
-    """A tensor of this shape, of `like`'s type and device, whose last dimension lies side by side."""
+    """The address of a tensor of this shape, of `like`'s type and device, whose last dimension lies side by side."""
     if t.dtype != like.dtype or t.device != like.device:
         raise ValueError(f"{name}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.numel() and shape[-1] > 1 and t.stride(-1) != 1:
+    if shape[-1] > 1 and t.stride(-1) != 1 and t.numel():
         raise ValueError(f"{name}: the numbers of a row must lie side by side (last stride {t.stride(-1)})")
-    return t
+    return t.data_ptr()
 
 
 def _ld(t):
     """Elements between the rows of a matrix; any value that covers a row where there is one row at most."""
-    ld = t.stride(0)
-    if t.shape[0] <= 1:
-        return max(ld, t.shape[1])
-    if ld < t.shape[1]:
-        raise ValueError(f"rows of {t.shape[1]} numbers lie {ld} apart")
+    ld, width = t.stride(0), t.shape[1]
+    if ld < width:
+        if t.shape[0] > 1:
+            raise ValueError(f"rows of {width} numbers lie {ld} apart")
+        return width
     return ld
 
 
-def _run_operator(op, suffix, args, device):
+def _run_operator(ask, call, args, grad, device):
     """Workspace of the call (the caching allocator's, on the current stream), then the call."""
     import torch
-    L = load_library()
     if device.type != "cuda":
         raise ValueError(f"tensors must be on the GPU, not on {device}")
-    n = C.c_size_t(0)
-    ask = (None, C.byref(n)) if suffix else (C.byref(n), None)
-    rc = getattr(L, f"stgn_{op}_workspace")(C.byref(args), *ask)
-    if rc == 0:
+    if torch.cuda.current_device() != device.index:
         with torch.cuda.device(device):
-            ws = torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None
-            rc = getattr(L, f"stgn_{op}{suffix}")(C.byref(args), ws.data_ptr() if n.value else None, n.value,
-                                                  torch.cuda.current_stream(device).cuda_stream)
+            return _run_operator(ask, call, args, grad, device)
+    n = C.c_size_t(0)
+    rc = ask(args, None, C.byref(n)) if grad else ask(args, C.byref(n), None)
+    if rc == 0:
+        size, ws = n.value, None
+        if size:
+            ws = torch.empty(size, dtype=torch.uint8, device=device)
+        rc = call(args, ws.data_ptr() if size else None, size, torch.cuda.current_stream().cuda_stream)
     if rc:
-        raise StgnError(rc, L.stgn_last_error(None).decode())
+        raise StgnError(rc, load_library().stgn_last_error(None).decode())
+
+
+def _linear_sizes(x, w, activation):
+    if x.dim() != 2 or w.dim() != 2:
+        raise ValueError("x and w must be matrices")
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}")
+    (rows, d_in), d_out = x.shape, w.shape[1]
+    return (_dtype_code(x), ACTIVATIONS[activation], rows, d_in, d_out, 0), (rows, d_out)
 
 
 def linear(x, w, bias=None, activation="none", residual=None, keep_pre=False):
@@ -208,23 +228,17 @@ def linear(x, w, bias=None, activation="none", residual=None, keep_pre=False):
     of one type (float32, bfloat16, float16); activation: "none", "relu", "gelu", "silu".  Returns y, or (y, pre) with
     keep_pre: the values in front of the activation, which linear_grad needs."""
     import torch
-    if x.dim() != 2 or w.dim() != 2:
-        raise ValueError("x and w must be matrices")
-    a = LinearArgs(dtype=_dtype_code(x), activation=ACTIVATIONS[activation], rows=x.shape[0], d_in=x.shape[1], d_out=w.shape[1])
-    _expect("x", x, x, x.shape)
-    _expect("w", w, x, (x.shape[1], w.shape[1]))
-    shape = (x.shape[0], w.shape[1])
+    L = load_library()
+    sizes, shape = _linear_sizes(x, w, activation)
+    d_out = shape[1]
+    xp, wp = _expect("x", x, x, x.shape), _expect("w", w, x, (x.shape[1], d_out))
+    bp = _expect("bias", bias, x, (d_out,)) if bias is not None else 0
+    rp = _expect("residual", residual, x, shape) if residual is not None else 0
     y = torch.empty(shape, dtype=x.dtype, device=x.device)
-    a.x, a.w, a.y = x.data_ptr(), w.data_ptr(), y.data_ptr()
-    a.ld_x, a.ld_w, a.ld_y = _ld(x), _ld(w), w.shape[1]
-    if bias is not None:
-        a.bias = _expect("bias", bias, x, (w.shape[1],)).data_ptr()
-    if residual is not None:
-        a.residual, a.ld_residual = _expect("residual", residual, x, shape).data_ptr(), _ld(residual)
     pre = torch.empty_like(y) if keep_pre else None
-    if keep_pre:
-        a.pre, a.ld_pre = pre.data_ptr(), w.shape[1]
-    _run_operator("linear", "", a, x.device)
+    args = _PACK_LINEAR.pack(*sizes, _ld(x), _ld(w), _ld(residual) if rp else 0, d_out, d_out, 0,
+                             xp, wp, bp, rp, y.data_ptr(), pre.data_ptr() if keep_pre else 0, 0, 0, 0, 0)
+    _run_operator(L.stgn_linear_workspace, L.stgn_linear, args, False, x.device)
     return (y, pre) if keep_pre else y
 
 
@@ -232,47 +246,38 @@ def linear_grad(dy, x, w, activation="none", pre=None, bias=True, need_x=True, n
     """Gradients of linear (stgn_linear_grad): (dx, dw, db), None for those not asked for.  pre: what linear kept, needed with an
     activation.  The residual's gradient is dy itself."""
     import torch
-    if x.dim() != 2 or w.dim() != 2:
-        raise ValueError("x and w must be matrices")
-    a = LinearArgs(dtype=_dtype_code(x), activation=ACTIVATIONS[activation], rows=x.shape[0], d_in=x.shape[1], d_out=w.shape[1])
-    _expect("x", x, x, x.shape)
-    _expect("w", w, x, (x.shape[1], w.shape[1]))
-    _expect("dy", dy, x, (x.shape[0], w.shape[1]))
-    a.x, a.w, a.dy = x.data_ptr(), w.data_ptr(), dy.data_ptr()
-    a.ld_x, a.ld_w, a.ld_dy = _ld(x), _ld(w), _ld(dy)
+    L = load_library()
+    sizes, shape = _linear_sizes(x, w, activation)
+    xp, wp, gp = _expect("x", x, x, x.shape), _expect("w", w, x, (x.shape[1], shape[1])), _expect("dy", dy, x, shape)
+    pp = 0
     if activation != "none":
         if pre is None:
             raise ValueError("the gradient of an activation needs pre")
-        a.pre, a.ld_pre = _expect("pre", pre, x, dy.shape).data_ptr(), _ld(pre)
+        pp = _expect("pre", pre, x, shape)
     dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_x else None
     dw = torch.empty(w.shape, dtype=x.dtype, device=x.device) if need_w else None
-    db = torch.empty(w.shape[1], dtype=x.dtype, device=x.device) if bias else None
-    a.dx, a.dw, a.db = (t.data_ptr() if t is not None else None for t in (dx, dw, db))
-    _run_operator("linear", "_grad", a, x.device)
+    db = torch.empty(shape[1:], dtype=x.dtype, device=x.device) if bias else None
+    args = _PACK_LINEAR.pack(*sizes, _ld(x), _ld(w), 0, 0, _ld(pre) if activation != "none" else 0, _ld(dy), xp, wp, 0, 0, 0, pp, gp,
+                             dx.data_ptr() if need_x else 0, dw.data_ptr() if need_w else 0, db.data_ptr() if bias else 0)
+    _run_operator(L.stgn_linear_workspace, L.stgn_linear_grad, args, True, x.device)
     return dx, dw, db
 
 
-def _attention_args(q, k, v, q_lens, k_lens, causal, window, scale):
+def _attention_call(q, k, v, q_lens, k_lens, causal, window, scale):
+    """Sizes and strides of the packed arguments, and the addresses of the lengths, q, k and v."""
     if q.dim() != 4 or k.dim() != 4:
         raise ValueError("q, k and v must be [lists, rows, heads, numbers]")
-    _expect("q", q, q, q.shape)
-    _expect("k", k, q, (q.shape[0], k.shape[1], k.shape[2], q.shape[3]))
-    _expect("v", v, q, k.shape)
-    for name, t in (("q_lens", q_lens), ("k_lens", k_lens)):
+    (lists, q_len, heads, d), (_, k_len, kv_heads, _) = q.shape, k.shape
+    shape = (lists, k_len, kv_heads, d)
+    where = [0, 0, _expect("q", q, q, q.shape), _expect("k", k, q, shape), _expect("v", v, q, shape)]
+    for at, t in enumerate((q_lens, k_lens)):
         if t is not None:
             import torch
-            if t.dtype != torch.int32 or t.device != q.device or tuple(t.shape) != (q.shape[0],) or not t.is_contiguous():
-                raise ValueError(f"{name}: a dense int32 tensor [lists] on {q.device} is expected")
-    a = AttentionArgs(dtype=_dtype_code(q), causal=int(bool(causal)), window=int(window), lists=q.shape[0], q_len=q.shape[1],
-                      k_len=k.shape[1], heads=q.shape[2], kv_heads=k.shape[2], d_head=q.shape[3],
-                      scale=q.shape[3] ** -0.5 if scale is None else scale)
-    a.q_list, a.q_row, a.q_head = q.stride()[:3]
-    a.k_list, a.k_row, a.k_head = k.stride()[:3]
-    a.v_list, a.v_row, a.v_head = v.stride()[:3]
-    a.q, a.k, a.v = q.data_ptr(), k.data_ptr(), v.data_ptr()
-    a.q_lens = q_lens.data_ptr() if q_lens is not None else None
-    a.k_lens = k_lens.data_ptr() if k_lens is not None else None
-    return a
+            if t.dtype != torch.int32 or t.device != q.device or t.shape != (lists,) or not t.is_contiguous():
+                raise ValueError(f"q_lens and k_lens: a dense int32 tensor [lists] on {q.device} is expected")
+            where[at] = t.data_ptr()
+    sizes = (_dtype_code(q), 1 if causal else 0, window, lists, q_len, k_len, heads, kv_heads, d, d ** -0.5 if scale is None else scale)
+    return sizes + q.stride()[:3] + k.stride()[:3] + v.stride()[:3], where
 
 
 def attention(q, k, v, q_lens=None, k_lens=None, causal=False, window=0, scale=None):
@@ -280,12 +285,13 @@ def attention(q, k, v, q_lens=None, k_lens=None, causal=False, window=0, scale=N
     last; q_lens, k_lens: int32 [lists] on the device, None: all rows.  causal aligns the lists at their ends; window: only the last
     `window` keys up to the query (0: all).  scale: d ** -0.5 by default.  Returns out (as q) and lse [lists, heads, q_len] fp32."""
     import torch
-    a = _attention_args(q, k, v, q_lens, k_lens, causal, window, scale)
+    L = load_library()
+    sizes, where = _attention_call(q, k, v, q_lens, k_lens, causal, window, scale)
+    lists, q_len, heads, d = q.shape
     out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
-    a.out, a.lse = out.data_ptr(), lse.data_ptr()
-    a.out_list, a.out_row, a.out_head = out.stride()[:3]
-    _run_operator("attention", "", a, q.device)
+    lse = torch.empty((lists, heads, q_len), dtype=torch.float32, device=q.device)
+    args = _PACK_ATTENTION.pack(*sizes, q_len * heads * d, heads * d, d, 0, 0, 0, *where, out.data_ptr(), lse.data_ptr(), 0, 0, 0, 0)
+    _run_operator(L.stgn_attention_workspace, L.stgn_attention, args, False, q.device)
     return out, lse
 
 
@@ -293,20 +299,18 @@ def attention_grad(dout, q, k, v, out, lse, q_lens=None, k_lens=None, causal=Fal
     """Gradients of attention (stgn_attention_grad) from its inputs and outputs and dout (out, dout: any strides but for the last):
     (dq, dk, dv), dense.  Heads that share a key head add up in dk and dv."""
     import torch
-    a = _attention_args(q, k, v, q_lens, k_lens, causal, window, scale)
-    _expect("dout", dout, q, q.shape)
-    _expect("out", out, q, q.shape)
-    if not lse.is_contiguous() or lse.dtype != torch.float32 or lse.device != q.device \
-            or tuple(lse.shape) != (q.shape[0], q.shape[2], q.shape[1]):
+    L = load_library()
+    sizes, where = _attention_call(q, k, v, q_lens, k_lens, causal, window, scale)
+    gp, op = _expect("dout", dout, q, q.shape), _expect("out", out, q, q.shape)
+    lists, q_len, heads, _ = q.shape
+    if lse.dtype != torch.float32 or lse.device != q.device or lse.shape != (lists, heads, q_len) or not lse.is_contiguous():
         raise ValueError("lse must be what attention returned")
-    a.dout_list, a.dout_row, a.dout_head = dout.stride()[:3]
-    a.out_list, a.out_row, a.out_head = out.stride()[:3]
     dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     dk = torch.empty(k.shape, dtype=q.dtype, device=q.device)
     dv = torch.empty(k.shape, dtype=q.dtype, device=q.device)
-    a.dout, a.out, a.lse = dout.data_ptr(), out.data_ptr(), lse.data_ptr()
-    a.dq, a.dk, a.dv = dq.data_ptr(), dk.data_ptr(), dv.data_ptr()
-    _run_operator("attention", "_grad", a, q.device)
+    args = _PACK_ATTENTION.pack(*sizes, *out.stride()[:3], *dout.stride()[:3], *where, op, lse.data_ptr(), gp,
+                                dq.data_ptr(), dk.data_ptr(), dv.data_ptr())
+    _run_operator(L.stgn_attention_workspace, L.stgn_attention_grad, args, True, q.device)
     return dq, dk, dv
 
 

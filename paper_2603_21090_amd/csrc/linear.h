@@ -18,21 +18,50 @@ namespace dense {
 
 enum { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };
 
-__device__ inline float act_value(int act, float z) {
-  switch (act) {
-    case ACT_RELU: return z > 0.f ? z : 0.f;
-    case ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752440f));
-    case ACT_SILU: return z / (1.f + expf(-z));
-    default: return z;
+// Phi(z), the normal distribution's share below z, and e^(-z^2/2).  16-bit types: Phi(-|z|) = poly(t) e^(-z^2/2) / 2, t = 1 / (1 + 0.3275911
+// |z| / sqrt 2) (Abramowitz & Stegun 7.1.26, 1.5e-7 off at most; the tail keeps its size: 0.07 % off at -4).  erff takes several times
+// the instructions on every output: 8,192 x 4,096 x 4,096 in bf16 spent 90 of its 534 us on them.
+template <class T>
+__device__ inline void normal_share(float z, float& share, float& bell) {
+  if constexpr (sizeof(T) == 4) {
+    share = 0.5f * (1.f + erff(z * 0.70710678118654752440f));
+    bell = expf(-0.5f * z * z);
+  } else {
+    const float x = fabsf(z) * 0.70710678118654752440f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f));
+    bell = __builtin_amdgcn_exp2f(-1.44269504088896340736f * x * x);
+    const float poly = fmaf(fmaf(fmaf(fmaf(1.061405429f, t, -1.453152027f), t, 1.421413741f), t, -0.284496736f), t, 0.254829592f);
+    const float tail = 0.5f * poly * t * bell;
+    share = z < 0.f ? tail : 1.f - tail;
   }
 }
-__device__ inline float act_slope(int act, float z) {
-  switch (act) {
-    case ACT_RELU: return z > 0.f ? 1.f : 0.f;
-    case ACT_GELU: return 0.5f * (1.f + erff(z * 0.70710678118654752440f)) + z * expf(-0.5f * z * z) * 0.39894228040143267794f;
-    case ACT_SILU: { const float s = 1.f / (1.f + expf(-z)); return s * (1.f + z * (1.f - s)); }
-    default: return 1.f;
+// 1 / (1 + e^-z)
+template <class T>
+__device__ inline float logistic(float z) {
+  if constexpr (sizeof(T) == 4) return 1.f / (1.f + expf(-z));
+  else return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * z));
+}
+
+template <class T, int ACT>
+__device__ inline float act_value(float z) {
+  if constexpr (ACT == ACT_RELU) return z > 0.f ? z : 0.f;
+  if constexpr (ACT == ACT_GELU) {
+    float share, bell;
+    normal_share<T>(z, share, bell);
+    return z * share;
   }
+  if constexpr (ACT == ACT_SILU) return z * logistic<T>(z);
+  return z;
+}
+template <class T>
+__device__ inline float act_slope(int act, float z) {
+  if (act == ACT_RELU) return z > 0.f ? 1.f : 0.f;
+  if (act == ACT_GELU) {
+    float share, bell;
+    normal_share<T>(z, share, bell);
+    return fmaf(z * 0.39894228040143267794f, bell, share);
+  }
+  const float s = logistic<T>(z);
+  return s * fmaf(z, 1.f - s, 1.f);
 }
 
 struct Product {
@@ -47,17 +76,57 @@ struct Product {
   float* part;                                                // [splits, m, n] where splits > 1
 };
 
-// bias, activation, residual: four neighbouring outputs of row m
+template <class T, int ACT>
+__device__ inline void activate(floatx4& v) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = act_value<T, ACT>(v[j]);
+}
+
+// bias, activation, residual: four neighbouring outputs of row m (one place in the code for all of them: `act` is the same for all)
 template <class T>
 __device__ inline void finish4(const Product& a, int64_t m, int n, floatx4 v) {
   if (a.bias) v += load4(static_cast<const T*>(a.bias), n, a.n);
   if (a.pre) store4(static_cast<T*>(a.pre) + m * a.ld_pre, n, a.n, v);
-  if (a.act != ACT_NONE) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = act_value(a.act, v[j]);
+  switch (a.act) {
+    case ACT_RELU: activate<T, ACT_RELU>(v); break;
+    case ACT_GELU: activate<T, ACT_GELU>(v); break;
+    case ACT_SILU: activate<T, ACT_SILU>(v); break;
+    default: break;
   }
   if (a.residual) v += load4(static_cast<const T*>(a.residual) + m * a.ld_res, n, a.n);
   store4(static_cast<T*>(a.out) + m * a.ld_out, n, a.n, v);
+}
+
+// A wave's blocks of 16 x 16, from output (m0, n0): a split's sums, or the epilogue.  Sixteen rows at a time: the scheduler would have
+// all rows' residuals in registers at once and spill the sums.
+template <class T, int NB, int MB>
+__device__ __forceinline__ void finish_tile(const Product& a, int split, int m0, int n0, floatx4 (&acc)[NB][MB]) {
+  const int lane = threadIdx.x & 63, nb = n0 + 4 * (lane >> 4);
+#pragma unroll
+  for (int y = 0; y < MB; ++y) {
+    __builtin_amdgcn_sched_barrier(0);
+    const int64_t m = m0 + y * 16 + (lane & 15);
+    if (m >= a.m) continue;
+    auto each = [&](auto f) {
+#pragma unroll
+      for (int x = 0; x < NB; ++x)
+        if (nb + x * 16 < a.n) f(nb + x * 16, acc[x][y]);
+    };
+    if (a.splits > 1) {
+      each([&](int n, floatx4& v) { store4(a.part + (split * (int64_t)a.m + m) * a.n, n, a.n, v); });
+      continue;
+    }
+    if (a.bias) each([&](int n, floatx4& v) { v += load4(static_cast<const T*>(a.bias), n, a.n); });
+    if (a.pre) each([&](int n, floatx4& v) { store4(static_cast<T*>(a.pre) + m * a.ld_pre, n, a.n, v); });
+    switch (a.act) {
+      case ACT_RELU: each([&](int, floatx4& v) { activate<T, ACT_RELU>(v); }); break;
+      case ACT_GELU: each([&](int, floatx4& v) { activate<T, ACT_GELU>(v); }); break;
+      case ACT_SILU: each([&](int, floatx4& v) { activate<T, ACT_SILU>(v); }); break;
+      default: break;
+    }
+    if (a.residual) each([&](int n, floatx4& v) { v += load4(static_cast<const T*>(a.residual) + m * a.ld_res, n, a.n); });
+    each([&](int n, floatx4& v) { store4(static_cast<T*>(a.out) + m * a.ld_out, n, a.n, v); });
+  }
 }
 
 // Workgroup number -> output tile.  Consecutive workgroups go to the eight dies in turn: each die gets one run of tiles,
@@ -78,7 +147,7 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product a) {
   constexpr int BK = kTileK<T>, THREADS = WM * WN * 64, MB = BM / WM / 16, NB = BN / WN / 16;
   constexpr int SL = lds_stride<T>(L_ROWS ? BK : BN), SR = lds_stride<T>(R_ROWS ? BK : BM);
   __shared__ __attribute__((aligned(16))) T ls[(L_ROWS ? BN : BK) * SL], rs[(R_ROWS ? BM : BK) * SR];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave % WM * MB * 16, wn = wave / WM * NB * 16;
+  const int wave = threadIdx.x >> 6, wm = wave % WM * MB * 16, wn = wave / WM * NB * 16;
   const unsigned tm = (unsigned)(a.m + BM - 1) / BM, tn = (unsigned)(a.n + BN - 1) / BN;
   const int split = (int)(blockIdx.x / (tm * tn));
   int row, col;
@@ -129,18 +198,107 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product a) {
     }
   }
 
+  finish_tile<T, NB, MB>(a, split, m0 + wm, n0 + wn, acc);
+}
+
+// The same for large outputs of 16-bit types: 256 x 256 outputs a workgroup of eight waves, each 64 rows x 128 columns, two tiles of
+// k in LDS: one is multiplied while the next one is on its way through registers into the other, one barrier a tile.  Rows are not
+// padded (two buffers of both operands are 128 KB); piece p (16 bytes) of row r lies at p ^ turn(r), which spreads what one read touches
+// over the banks: eight rows of a fragment along k, four rows of a transposed one.  Rows and columns past the edge repeat the last
+// ones and are not stored; k has whole tiles.
+template <class T, bool ROWS>
+struct LargeMove {                                            // ROWS: [256 lines][64 of k], else [64 of k][256 lines]
+  const T* at[4];
+  u32x4 r[4];
+  int64_t step;
+  static __device__ inline int turn(int row) { return ROWS ? row & 7 : ((row & 3) << 1) | (row & 8); }
+  __device__ inline void start(const T* base, int64_t ld, int first, int lines, int k) {
 #pragma unroll
-  for (int y = 0; y < MB; ++y) {
-    const int m = m0 + wm + y * 16 + (lane & 15);
-    if (m >= a.m) continue;
+    for (int i = 0; i < 4; ++i) {
+      const int p = i * 512 + (int)threadIdx.x;
+      if constexpr (ROWS) at[i] = base + (int64_t)min(first + p / 8, lines - 1) * ld + k + p % 8 * 8;
+      else at[i] = base + (int64_t)(k + p / 32) * ld + min(first + p % 32 * 8, lines - 8);
+    }
+    step = ROWS ? 64 : 64 * ld;
+  }
+  __device__ inline void fetch() {
 #pragma unroll
-    for (int x = 0; x < NB; ++x) {
-      const int n = n0 + wn + x * 16 + 4 * (lane >> 4);
-      if (n >= a.n) continue;
-      if (a.splits > 1) store4(a.part + ((int64_t)split * a.m + m) * a.n, n, a.n, acc[x][y]);
-      else finish4<T>(a, m, n, acc[x][y]);
+    for (int i = 0; i < 4; ++i) {
+      r[i] = *reinterpret_cast<const u32x4_any*>(at[i]);
+      at[i] += step;
     }
   }
+  __device__ inline void store(T* tile) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int p = i * 512 + (int)threadIdx.x, row = ROWS ? p / 8 : p / 32, piece = ROWS ? p % 8 : p % 32;
+      *reinterpret_cast<u32x4*>(tile + (p - piece + (piece ^ turn(row))) * 8) = r[i];
+    }
+  }
+  // fragment of 16 lines from `line`, elements k .. k + 31 of the tile
+  static __device__ inline typename Elem<T>::Frag frag(const T* tile, int line, int k) {
+    const int lane = threadIdx.x & 63, g = lane >> 4, i = lane & 15;
+    if constexpr (ROWS) {
+      return *reinterpret_cast<const typename Elem<T>::Frag*>(tile + (line + i) * 64 + ((k / 8 + g) ^ (i & 7)) * 8);
+    } else {
+      const int row = k + 8 * g + (i >> 2);                   // and four further on: the same turn
+      const T* p = tile + row * 256 + ((line / 8 + ((i & 3) >> 1)) ^ turn(row)) * 8 + (i & 1) * 4;
+      return join_transposed<T>(read_transposed(p), read_transposed(p + 4 * 256));
+    }
+  }
+};
+
+template <class T, bool L_ROWS, bool R_ROWS>
+__global__ __launch_bounds__(512) void large_product_kernel(Product a) {
+  constexpr int BK = 64, NB = 8, MB = 4, TILE = 256 * BK;
+  __shared__ __attribute__((aligned(16))) T ls[2][TILE], rs[2][TILE];
+  const int wave = threadIdx.x >> 6, wm = wave % 4 * 64, wn = wave / 4 * 128;
+  const unsigned tm = (unsigned)(a.m + 255) / 256, tn = (unsigned)(a.n + 255) / 256;
+  const int split = (int)(blockIdx.x / (tm * tn));
+  int row, col;
+  tile_of(blockIdx.x % (tm * tn), tm, tn, row, col);
+  const int m0 = row * 256, n0 = col * 256, kb = split * a.k_per, tiles = (min(a.k, kb + a.k_per) - kb) / BK;
+
+  LargeMove<T, L_ROWS> ml;
+  LargeMove<T, R_ROWS> mr;
+  ml.start(static_cast<const T*>(a.l), a.ld_l, n0, a.n, kb);
+  mr.start(static_cast<const T*>(a.r), a.ld_r, m0, a.m, kb);
+  floatx4 acc[NB][MB];
+#pragma unroll
+  for (int x = 0; x < NB; ++x)
+#pragma unroll
+    for (int y = 0; y < MB; ++y) acc[x][y] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+  ml.fetch();
+  mr.fetch();
+  ml.store(ls[0]);
+  mr.store(rs[0]);
+  for (int t = 0; t < tiles; ++t) {
+    __syncthreads();                                          // tile t is there, and nobody reads the other buffer any more
+    const bool more = t + 1 < tiles;
+    if (more) {
+      ml.fetch();
+      mr.fetch();
+    }
+    const T *l = ls[t & 1], *r = rs[t & 1];
+#pragma unroll
+    for (int s = 0; s < BK; s += 32) {
+      typename Elem<T>::Frag lf[NB], rf[MB];
+#pragma unroll
+      for (int y = 0; y < MB; ++y) rf[y] = mr.frag(r, wm + y * 16, s);
+#pragma unroll
+      for (int x = 0; x < NB; ++x) lf[x] = ml.frag(l, wn + x * 16, s);
+#pragma unroll
+      for (int x = 0; x < NB; ++x)
+#pragma unroll
+        for (int y = 0; y < MB; ++y) acc[x][y] = Elem<T>::mma(lf[x], rf[y], acc[x][y]);
+    }
+    if (more) {
+      ml.store(ls[(t + 1) & 1]);
+      mr.store(rs[(t + 1) & 1]);
+    }
+  }
+  finish_tile<T, NB, MB>(a, split, m0 + wm, n0 + wn, acc);
 }
 
 // sums of the splits, in their order, and the epilogue
@@ -171,7 +329,7 @@ __global__ __launch_bounds__(256) void dz_kernel(LinearGradArgs a, T* dz, int64_
       if (dz) {
         const floatx4 z = load4(static_cast<const T*>(a.pre) + m * a.ld_pre, n, a.d_out);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] *= act_slope(a.act, z[j]);
+        for (int j = 0; j < 4; ++j) v[j] *= act_slope<T>(a.act, z[j]);
         store4(dz + m * ld_dz, n, a.d_out, v);
       }
       acc += v;
@@ -200,16 +358,19 @@ __global__ __launch_bounds__(256) void db_kernel(const float* sums, int chunks, 
 
 inline int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-struct Plan { bool wide; int splits, k_per; };
+struct Plan { int tile, splits, k_per; };
 
-// Large outputs take tiles of 128 x 128 (a wave 64 x 64), small ones 64 x 64.  Where the tiles leave the chip's 256 CUs idle and k
+// Outputs of 256 tiles of 256 x 256 and more take those, where k has whole tiles and rows per k hold whole pieces of 16 bytes (16-bit
+// types).  Others take tiles of 128 x 128 (a wave 64 x 64), small ones 64 x 64.  Where the tiles leave the chip's 256 CUs idle and k
 // is long, k is split: at least eight tiles of k a split, two workgroups a CU.
 template <class T>
-Plan plan_of(int64_t m, int64_t n, int64_t k) {
+Plan plan_of(int64_t m, int64_t n, int64_t k, bool l_rows, bool r_rows) {
   constexpr int BK = kTileK<T>;
+  const auto tiles_of = [&](int64_t t) { return ((m + t - 1) / t) * ((n + t - 1) / t); };
   Plan p;
-  p.wide = ((m + 127) / 128) * ((n + 127) / 128) >= 256;
-  const int64_t tile = p.wide ? 128 : 64, tiles = ((m + tile - 1) / tile) * ((n + tile - 1) / tile);
+  const bool whole = sizeof(T) == 2 && k % 64 == 0 && (l_rows || n % 8 == 0) && (r_rows || m % 8 == 0);
+  p.tile = whole && tiles_of(256) >= 256 ? 256 : tiles_of(128) >= 256 ? 128 : 64;
+  const int64_t tiles = tiles_of(p.tile);
   int64_t splits = tiles ? 512 / tiles : 1;
   const int64_t most = k / (8 * BK);
   if (splits > most) splits = most;
@@ -222,22 +383,25 @@ Plan plan_of(int64_t m, int64_t n, int64_t k) {
 }
 
 template <class T>
-size_t part_bytes(int64_t m, int64_t n, int64_t k) {
-  const Plan p = plan_of<T>(m, n, k);
+size_t part_bytes(int64_t m, int64_t n, int64_t k, bool l_rows, bool r_rows) {
+  const Plan p = plan_of<T>(m, n, k, l_rows, r_rows);
   return p.splits > 1 ? (size_t)p.splits * m * n * sizeof(float) : 0;
 }
 
 template <class T, bool L_ROWS, bool R_ROWS>
 hipError_t product(Product a, void* part, hipStream_t s) {
   if (a.m == 0 || a.n == 0) return hipSuccess;
-  const Plan p = plan_of<T>(a.m, a.n, a.k);
+  const Plan p = plan_of<T>(a.m, a.n, a.k, L_ROWS, R_ROWS);
   a.splits = p.splits;
   a.k_per = p.k_per;
   a.part = static_cast<float*>(part);
-  const int tile = p.wide ? 128 : 64;
-  const int64_t grid = (int64_t)((a.m + tile - 1) / tile) * ((a.n + tile - 1) / tile) * p.splits;
-  hipError_t e = p.wide ? launch(product_kernel<T, 128, 128, 2, 2, L_ROWS, R_ROWS>, grid, 256, s, a)
-                        : launch(product_kernel<T, 64, 64, 2, 2, L_ROWS, R_ROWS>, grid, 256, s, a);
+  const int64_t grid = (int64_t)((a.m + p.tile - 1) / p.tile) * ((a.n + p.tile - 1) / p.tile) * p.splits;
+  hipError_t e = hipErrorInvalidValue;
+  if constexpr (sizeof(T) == 2) {
+    if (p.tile == 256) e = launch(large_product_kernel<T, L_ROWS, R_ROWS>, grid, 512, s, a);
+  }
+  if (p.tile == 128) e = launch(product_kernel<T, 128, 128, 2, 2, L_ROWS, R_ROWS>, grid, 256, s, a);
+  if (p.tile == 64) e = launch(product_kernel<T, 64, 64, 2, 2, L_ROWS, R_ROWS>, grid, 256, s, a);
   if (e != hipSuccess || p.splits == 1) return e;
   const int64_t blocks = ((int64_t)a.m * ((a.n + 3) / 4) + 255) / 256;
   return launch(join_kernel<T>, blocks < 4096 ? blocks : 4096, 256, s, a);
@@ -269,7 +433,7 @@ GradLayout layout_of(const LinearGradArgs& a) {
   g.chunks = (int)chunks;
   g.sums = a.act != ACT_NONE ? (size_t)up((int64_t)a.rows * g.ld_dz * sizeof(T), 256) : 0;
   g.part = g.sums + (a.db ? (size_t)up((int64_t)g.chunks * a.d_out * sizeof(float), 256) : 0);
-  const size_t px = a.dx ? part_bytes<T>(a.rows, a.d_in, a.d_out) : 0, pw = a.dw ? part_bytes<T>(a.d_in, a.d_out, a.rows) : 0;
+  const size_t px = a.dx ? part_bytes<T>(a.rows, a.d_in, a.d_out, true, true) : 0, pw = a.dw ? part_bytes<T>(a.d_in, a.d_out, a.rows, false, false) : 0;
   g.total = g.part + (px > pw ? px : pw);
   return g;
 }

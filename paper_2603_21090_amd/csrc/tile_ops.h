@@ -82,13 +82,17 @@ __device__ inline typename Elem<T>::Frag frag_rows(const T* tile, int stride, in
   return *reinterpret_cast<const typename Elem<T>::Frag*>(tile + (row + (lane & 15)) * stride + k + Elem<T>::E * (lane >> 4));
 }
 
-// four 16-bit numbers of column col + lane % 16, one from each of the rows that lane group g = lane / 16 names: row .. row + 3.
-// Sixteen lanes read four rows of 16 numbers, 8 bytes each, and get them transposed.
+// The transposing LDS load: the sixteen lanes of a group read four rows of 16 numbers, 8 bytes each (lane i: row i / 4, numbers
+// 4 (i % 4) and on), and lane i gets the four numbers of column i.
 template <class T>
-__device__ inline i16x4 transposed4(const T* tile, int stride, int row, int col) {
-  const int i = threadIdx.x & 15;
-  const T* p = tile + (row + (i >> 2)) * stride + col + 4 * (i & 3);
+__device__ inline i16x4 read_transposed(const T* p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(p));
+}
+template <class T>
+__device__ inline typename Elem<T>::Frag join_transposed(const i16x4& lo, const i16x4& hi) {
+  typedef short i16x8 __attribute__((ext_vector_type(8)));
+  const i16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  return __builtin_bit_cast(typename Elem<T>::Frag, both);
 }
 
 // fragment of columns col .. col + 15 whose summed index runs down rows row .. row + KF - 1 of the tile
@@ -101,11 +105,9 @@ __device__ inline typename Elem<T>::Frag frag_cols(const T* tile, int stride, in
     for (int u = 0; u < 4; ++u) f[u] = tile[(row + 4 * g + u) * stride + col + (lane & 15)];
     return f;
   } else {
-    const i16x4 lo = transposed4(tile, stride, row + (SPLIT ? 4 * g : 8 * g), col);
-    const i16x4 hi = transposed4(tile, stride, row + (SPLIT ? 16 + 4 * g : 8 * g + 4), col);
-    typedef short i16x8 __attribute__((ext_vector_type(8)));
-    const i16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    return __builtin_bit_cast(typename Elem<T>::Frag, both);
+    const int i = lane & 15;
+    const T* p = tile + (row + (SPLIT ? 4 * g : 8 * g) + (i >> 2)) * stride + col + 4 * (i & 3);
+    return join_transposed<T>(read_transposed(p), read_transposed(p + (SPLIT ? 16 : 4) * stride));
   }
 }
 
@@ -141,9 +143,17 @@ __device__ inline void store4(T* row, int col, int cols, const floatx4& v) {
 template <class T>
 __device__ inline floatx4 load4(const T* row, int col, int cols) {
   floatx4 v = {0.f, 0.f, 0.f, 0.f};
+  if (col + 4 <= cols) {
+    typename Elem<T>::Four f;
+    if constexpr (sizeof(T) == 4) f = __builtin_bit_cast(typename Elem<T>::Four, *reinterpret_cast<const u32x4_any*>(row + col));
+    else f = __builtin_bit_cast(typename Elem<T>::Four, *reinterpret_cast<const u32x2_any*>(row + col));
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (col + j < cols) v[j] = (float)row[col + j];
+    for (int j = 0; j < 4; ++j) v[j] = (float)f[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 3; ++j)
+      if (col + j < cols) v[j] = (float)row[col + j];
+  }
   return v;
 }
 
