@@ -187,7 +187,7 @@ int check_attention(const stgn_attention_args* a, bool grad, bool sizes_only) {
     for (const Span& s : {q, k, v})
       if (meet(o, s) || meet(lse, s)) return no("an output overlaps an input");
     if (meet(o, lse)) return no("out and lse overlap");
-    if (!apart(a->lists, a->out_list, a->q_len, a->out_row, a->heads, a->out_head, a->d_head)) return no("two numbers of out share a place");
+    if (have_q && !apart(a->lists, a->out_list, a->q_len, a->out_row, a->heads, a->out_head, a->d_head)) return no("two numbers of out share a place");
     return STGN_OK;
   }
   if (a->dout_list > kMaxLd || a->dout_row > kMaxLd || a->dout_head > kMaxLd) return no("a stride is out of range");
