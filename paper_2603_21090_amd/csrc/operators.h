@@ -17,7 +17,7 @@ struct AttnArgs {
   float* delta;                                               // workspace of the gradient: dout . out, laid out as lse
   const int *q_lens, *k_lens;                                 // [lists] or null: every list is q_len, k_len long
   Strides sq, sk, sv, so, sdo;
-  int lists, q_len, k_len, heads, kv_heads, group, d;
+  int lists, q_len, k_len, heads, kv_heads, group, group_shift, d;                // group: query heads a key head; its logarithm or -1
   int causal, window;
   float scale;
 };

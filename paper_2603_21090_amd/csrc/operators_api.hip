@@ -216,6 +216,7 @@ AttnArgs attention_args(const stgn_attention_args* a) {
   t.sdo = {(int64_t)a->dout_list, (int64_t)a->dout_row, (int64_t)a->dout_head};
   t.lists = (int)a->lists; t.q_len = (int)a->q_len; t.k_len = (int)a->k_len;
   t.heads = (int)a->heads; t.kv_heads = (int)a->kv_heads; t.group = (int)(a->heads / a->kv_heads); t.d = (int)a->d_head;
+  t.group_shift = (t.group & (t.group - 1)) == 0 ? __builtin_ctz((unsigned)t.group) : -1;
   t.causal = (int)a->causal; t.window = (int)a->window; t.scale = a->scale;
   return t;
 }

@@ -186,4 +186,37 @@ struct TileMove {
   }
 };
 
+// The same for consecutive tiles of a matrix whose rows lie `stride` apart: addresses are computed once and advance by a tile.
+template <class T, int ROWS, int COLS, int THREADS>
+struct StreamMove {
+  static constexpr int E = Elem<T>::E, PER_ROW = COLS / E, NP = ROWS * PER_ROW / THREADS, APART = THREADS / PER_ROW;
+  static_assert(ROWS * PER_ROW % THREADS == 0 && THREADS % PER_ROW == 0, "every thread carries whole pieces of one column");
+  const T* at;                                                // this thread's first piece of the next tile
+  int64_t stride;
+  int row, count;                                             // its row in the tile; elements the matrix has from its column on
+  u32x4 r[NP];
+
+  __device__ inline void start(const T* base, int64_t stride_, int cols) {
+    const int t = (int)threadIdx.x, c = t % PER_ROW * E;
+    row = t / PER_ROW;
+    count = cols - c;
+    stride = stride_;
+    at = base + row * stride_ + c;
+  }
+  // rows: how many the matrix has from the tile's first row on (the same for all threads)
+  __device__ inline void fetch(int rows) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      r[i] = u32x4{0, 0, 0, 0};
+      if (count > 0 && (rows >= ROWS || row + i * APART < rows)) r[i] = load16(at + i * APART * stride, count);
+    }
+    at += ROWS * stride;
+  }
+  __device__ inline void store(T* tile, int lds_row) const {
+    T* to = tile + row * lds_row + (int)threadIdx.x % PER_ROW * E;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) *reinterpret_cast<u32x4*>(to + i * APART * lds_row) = r[i];
+  }
+};
+
 }  // namespace stgn
