@@ -36,7 +36,7 @@ template <class T> constexpr float kUnshift = kShift<T> != 0.f ? 1.f / 16384.f :
 template <class T> constexpr float kShiftLazy = kShift<T> / 2.f;
 constexpr float kLazy = 8.f;
 
-// rows of a streamed tile: two tiles of 64 x 128 16-bit numbers and their padding are 34 KB, four workgroups a CU
+// rows of a streamed tile: two buffers of two tiles of 64 x 128 16-bit numbers are 68 KB, two workgroups a CU
 template <class T, int DP>
 constexpr int stream_rows() {
   constexpr int n = 64 * 256 / (DP * (int)sizeof(T));
@@ -105,28 +105,55 @@ __device__ inline float over_groups_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-// Workgroup -> (tile of a list and key head, list, key head).  The last tiles come first: with `causal` they are the longest.  One tile
-// number of all lists and heads after the other, so that workgroups that read the same keys are a multiple of the number of lists
-// and heads apart, on one die where that is a multiple of eight.
-__device__ inline int place_of(const AttnArgs& a, int tiles, int& b, int& hk) {
-  const unsigned pairs = (unsigned)a.lists * (unsigned)a.kv_heads, bh = blockIdx.x % pairs;
-  b = (int)(bh / (unsigned)a.kv_heads);
-  hk = (int)(bh % (unsigned)a.kv_heads);
-  return tiles - 1 - (int)(blockIdx.x / pairs);
+// what fits a CU at once: two workgroups, or one of eight waves whose rows are 128 numbers
+template <int WAVES, int DP> constexpr bool kTwo = WAVES * DP <= 512;
+
+// Workgroup -> (tile of a list and key head, run of the tile's stream, list, key head).  The longest tiles come first (with `causal` the
+// last queries, or the first keys); where all workgroups are on the chip at once, two a CU, the second half comes in the
+// other order instead, so that a long and a short one share a CU.  The same tile of all lists and heads lies side by side: workgroups that
+// read the same keys are a multiple of their number apart, on one die where that is a multiple of eight.
+struct Place { int tile, run, b, hk; };
+__device__ inline Place place_of(const AttnArgs& a, int tiles, int runs, bool two, bool last_first) {
+  const unsigned pairs = (unsigned)a.lists * (unsigned)a.kv_heads, bh = blockIdx.x % pairs, x = blockIdx.x / pairs;
+  Place p;
+  p.b = (int)(bh / (unsigned)a.kv_heads);
+  p.hk = (int)(bh % (unsigned)a.kv_heads);
+  p.run = (int)(x % (unsigned)runs);
+  const int q = (int)(x / (unsigned)runs), half = (tiles + 1) / 2;
+  const int nth = two && gridDim.x <= 512u && q >= half ? tiles - 1 - (q - half) : q;      // nth longest
+  p.tile = last_first ? tiles - 1 - nth : nth;
+  return p;
+}
+
+// A workgroup's run of the `n` streamed rows from `first` on, whole tiles of `tile` rows
+__device__ inline void run_of(int run, int runs, int tile, int& first, int& end) {
+  if (runs == 1) return;
+  const int n = max(end - first, 0), per = (n + runs * tile - 1) / (runs * tile) * tile;
+  const int from = min(first + run * per, end);
+  end = min(from + per, end);
+  first = from;
+}
+
+// Where the tiles are fewer than two workgroups a CU, each tile's stream is cut into runs of 512 rows or more (eight tiles, about what
+// the launch costs that adds the runs' sums, in their order).
+inline int runs_for(int64_t workgroups, int64_t streamed) {
+  int64_t runs = workgroups ? 512 / workgroups : 1;
+  if (runs > streamed / 512) runs = streamed / 512;
+  return runs < 1 ? 1 : (int)runs;
 }
 
 // ---- forward
 // The softmax needs some reference score per row, not the largest one: it moves only when a score exceeds it by more than 2^kLazy, which is
 // rare after the first tiles, and the accumulators are rescaled only then.
 template <class T, int DP, int NB, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void forward_kernel(AttnArgs a) {
+__global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void forward_kernel(AttnArgs a, int runs, float* part) {
   using El = Elem<T>;
   constexpr int BK = stream_rows<T, DP>(), S = lds_stride<T>(DP), ROWS = WAVES * NB * 16, KB = BK / 16, DB = DP / 16;
   __shared__ __attribute__((aligned(16))) T ks[2][BK * S], vs[2][BK * S];
   const int lane = threadIdx.x & 63, g = lane >> 4, wave = threadIdx.x >> 6;
   const int rows = a.q_len * a.group, tiles = (rows + ROWS - 1) / ROWS;
-  int b, hk;
-  const int t = place_of(a, tiles, b, hk);
+  const Place at = place_of(a, tiles, runs, kTwo<WAVES, DP>, true);
+  const int t = at.tile, b = at.b, hk = at.hk;
   const List l = list_of(a, b);
 
   int r[NB], lo[NB], hi[NB];
@@ -166,13 +193,14 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void forward_kernel(A
 
   StreamMove<T, BK, DP, WAVES * 64> mk, mv;
   int kt = k0 / 16 * 16, buf = 0;
+  run_of(at.run, runs, BK, kt, k1);
   mk.start(row_of<T>(a.k, a.sk, b, kt, hk), a.sk.row, a.d);
   mv.start(row_of<T>(a.v, a.sv, b, kt, hk), a.sv.row, a.d);
   if (kt < k1) {
     mk.fetch(l.kn - kt);
     mv.fetch(l.kn - kt);
-    mk.store(ks[0], S);
-    mv.store(vs[0], S);
+    mk.store(ks[0]);
+    mv.store(vs[0]);
   }
   for (; kt < k1; kt += BK, buf ^= 1) {
     __syncthreads();                                          // this tile is there, and nobody reads the other buffer any more
@@ -189,7 +217,7 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void forward_kernel(A
         for (int c = 0; c < NB; ++c) s[y][c] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < DP / El::KF; ++k) {
-          const typename El::Frag f = frag_rows(ks[buf], S, y * 16, k * El::KF);
+          const typename El::Frag f = placed_rows<T, DP>(ks[buf], y * 16, k * El::KF);
 #pragma unroll
           for (int c = 0; c < NB; ++c) s[y][c] = El::mma(f, qf[c][k], s[y][c]);
         }
@@ -252,15 +280,15 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void forward_kernel(A
         }
 #pragma unroll
         for (int x = 0; x < DB; ++x) {
-          const typename El::Frag f = frag_cols<T, true>(vs[buf], S, y * 16, x * 16);
+          const typename El::Frag f = placed_cols<T, DP>(vs[buf], y * 16, x * 16);
 #pragma unroll
           for (int c = 0; c < NB; ++c) o[x][c] = El::mma(f, pf[c], o[x][c]);
         }
       }
     }
     if (more) {
-      mk.store(ks[buf ^ 1], S);
-      mv.store(vs[buf ^ 1], S);
+      mk.store(ks[buf ^ 1]);
+      mv.store(vs[buf ^ 1]);
     }
   }
 
@@ -269,6 +297,13 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void forward_kernel(A
     const float total = over_groups_sum(sum[c]);
     if (r[c] >= rows) continue;
     const int i = query_of(a, r[c]), head = hk * a.group + r[c] - i * a.group;
+    if (runs > 1) {                                           // (as the runs of few queries are kept)
+      float* p = part + (((int64_t)(b * a.kv_heads + hk) * runs + at.run) * rows + r[c]) * (a.d + 2);
+#pragma unroll
+      for (int x = 0; x < DB; ++x) store4(p + 2, x * 16 + 4 * g, a.d, o[x][c]);
+      if (g == 0) { p[0] = m[c] - kShiftLazy<T>; p[1] = total; }
+      continue;
+    }
     const bool any = hi[c] > lo[c];
     const float inv = any ? 1.f / total : 0.f;
     T* row = const_cast<T*>(row_of<T>(a.o, a.so, b, i, head));
@@ -288,14 +323,14 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void forward_kernel(A
 // instead, from the unrounded weights: a short list's delta is not small beside its dp (lists of 10 to 30 keys in bf16: dq 0.27 % off, 0.24 %
 // with it; half of that is the rounding of dq itself).
 template <class T, int DP, int NB, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void query_grad_kernel(AttnArgs a) {
+__global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void query_grad_kernel(AttnArgs a, int runs, float* part) {
   using El = Elem<T>;
   constexpr int BK = stream_rows<T, DP>(), S = lds_stride<T>(DP), ROWS = WAVES * NB * 16, DB = DP / 16, PB = El::PB;
   __shared__ __attribute__((aligned(16))) T ks[2][BK * S], vs[2][BK * S];
   const int lane = threadIdx.x & 63, g = lane >> 4, wave = threadIdx.x >> 6;
   const int rows = a.q_len * a.group, tiles = (rows + ROWS - 1) / ROWS;
-  int b, hk;
-  const int t = place_of(a, tiles, b, hk);
+  const Place pos = place_of(a, tiles, runs, kTwo<WAVES, DP>, true);
+  const int t = pos.tile, b = pos.b, hk = pos.hk;
   const List l = list_of(a, b);
 
   int r[NB], lo[NB], hi[NB], head[NB], qi[NB];
@@ -321,13 +356,15 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void query_grad_kerne
 
   StreamMove<T, BK, DP, WAVES * 64> mk, mv;
   int kt = k0 / 16 * 16, buf = 0;
+  const bool one_tile = sizeof(T) == 2 && kt < k1 && k1 - kt <= BK;
+  run_of(pos.run, runs, BK, kt, k1);
   mk.start(row_of<T>(a.k, a.sk, b, kt, hk), a.sk.row, a.d);
   mv.start(row_of<T>(a.v, a.sv, b, kt, hk), a.sv.row, a.d);
   if (kt < k1) {
     mk.fetch(l.kn - kt);
     mv.fetch(l.kn - kt);
-    mk.store(ks[0], S);
-    mv.store(vs[0], S);
+    mk.store(ks[0]);
+    mv.store(vs[0]);
   }
 
   const float scale2 = a.scale * kLog2e;
@@ -356,7 +393,7 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void query_grad_kerne
       for (int c = 0; c < NB; ++c) p[u][c] = dp[u][c] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < DP / El::KF; ++k) {
-        const typename El::Frag kf = frag_rows(ks[buf], S, (y + u) * 16, k * El::KF), vf = frag_rows(vs[buf], S, (y + u) * 16, k * El::KF);
+        const typename El::Frag kf = placed_rows<T, DP>(ks[buf], (y + u) * 16, k * El::KF), vf = placed_rows<T, DP>(vs[buf], (y + u) * 16, k * El::KF);
 #pragma unroll
         for (int c = 0; c < NB; ++c) {
           p[u][c] = El::mma(kf, qf[c][k], p[u][c]);
@@ -382,7 +419,7 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void query_grad_kerne
           }
     }
   };
-  if (sizeof(T) == 2 && kt < k1 && k1 - kt <= BK) {
+  if (one_tile && kt < k1) {
     __syncthreads();
     float sum[NB] = {};
     for (int y = 0; y < BK / 16; y += PB) {
@@ -400,7 +437,7 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void query_grad_kerne
   }
 #pragma unroll
   for (int c = 0; c < NB; ++c)
-    if (g == 0 && r[c] < rows) a.delta[((int64_t)b * a.heads + head[c]) * a.q_len + qi[c]] = delta[c];
+    if (g == 0 && r[c] < rows && pos.run == 0) a.delta[((int64_t)b * a.heads + head[c]) * a.q_len + qi[c]] = delta[c];
 
   floatx4 dq[DB][NB];
 #pragma unroll
@@ -430,22 +467,28 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void query_grad_kerne
         }
 #pragma unroll
         for (int x = 0; x < DB; ++x) {
-          const typename El::Frag kf = frag_cols<T, true>(ks[buf], S, y * 16, x * 16);
+          const typename El::Frag kf = placed_cols<T, DP>(ks[buf], y * 16, x * 16);
 #pragma unroll
           for (int c = 0; c < NB; ++c) dq[x][c] = El::mma(kf, f[c], dq[x][c]);
         }
       }
     }
     if (more) {
-      mk.store(ks[buf ^ 1], S);
-      mv.store(vs[buf ^ 1], S);
+      mk.store(ks[buf ^ 1]);
+      mv.store(vs[buf ^ 1]);
     }
   }
 #pragma unroll
   for (int c = 0; c < NB; ++c) {
     if (r[c] >= rows) continue;
-    T* row = dense_row<T>(a, a.dq, a.q_len, a.heads, b, qi[c], head[c]);
     const bool any = hi[c] > lo[c];
+    if (runs > 1) {
+      float* p = part + (((int64_t)(b * a.kv_heads + hk) * runs + pos.run) * rows + r[c]) * a.d;
+#pragma unroll
+      for (int x = 0; x < DB; ++x) store4(p, x * 16 + 4 * g, a.d, any ? dq[x][c] * a.scale : floatx4{0.f, 0.f, 0.f, 0.f});
+      continue;
+    }
+    T* row = dense_row<T>(a, a.dq, a.q_len, a.heads, b, qi[c], head[c]);
 #pragma unroll
     for (int x = 0; x < DB; ++x) store4(row, x * 16 + 4 * g, a.d, any ? dq[x][c] * a.scale : floatx4{0.f, 0.f, 0.f, 0.f});
   }
@@ -469,16 +512,12 @@ struct RowMove {
       }
     }
   }
-  __device__ inline void store(T* tile, int lds_row) const {
-    T* to = tile + (int)threadIdx.x / PER_ROW * lds_row + (int)threadIdx.x % PER_ROW * E;
-#pragma unroll
-    for (int i = 0; i < NP; ++i) *reinterpret_cast<u32x4*>(to + i * APART * lds_row) = r[i];
-  }
+  __device__ inline void store(T* tile) const { store_placed<T, BQ, DP, THREADS>(tile, r); }
 };
 
 // dk, dv: keys and values in registers, queries and dout stream
 template <class T, int DP, int NB, int WAVES, int BQ, int OCC>
-__global__ __launch_bounds__(WAVES * 64, OCC) void key_grad_kernel(AttnArgs a) {
+__global__ __launch_bounds__(WAVES * 64, OCC) void key_grad_kernel(AttnArgs a, int runs, float* part) {
   using El = Elem<T>;
   constexpr int S = lds_stride<T>(DP), KEYS = WAVES * NB * 16, DB = DP / 16, PB = El::PB;
   __shared__ __attribute__((aligned(16))) T qs[2][BQ * S], gs[2][BQ * S];
@@ -486,8 +525,8 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void key_grad_kernel(AttnArgs a) {
   __shared__ int los[2][BQ], his[2][BQ];
   const int lane = threadIdx.x & 63, g = lane >> 4, wave = threadIdx.x >> 6;
   const int tiles = (a.k_len + KEYS - 1) / KEYS;
-  int b, hk;
-  const int t = tiles - 1 - place_of(a, tiles, b, hk);        // with `causal` the first keys are seen by the most queries
+  const Place pos = place_of(a, tiles, runs, kTwo<WAVES, DP>, false);
+  const int t = pos.tile, b = pos.b, hk = pos.hk;
   const List l = list_of(a, b);
   const int j0 = t * KEYS, jw = j0 + wave * NB * 16 + (lane & 15);
 
@@ -519,7 +558,8 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void key_grad_kernel(AttnArgs a) {
   RowMove<T, BQ, DP, WAVES * 64> mq, md;
   float ml = 0.f, mt = 0.f;
   int mlo = 0, mhi = 0;
-  const int r1 = q1 * a.group;
+  int rt = q0 * a.group, r1 = q1 * a.group, buf = 0;
+  run_of(pos.run, runs, BQ, rt, r1);
   auto fetch = [&](int rt) {
     mq.fetch(a, a.q, a.sq, b, hk, rt, r1);
     md.fetch(a, a.dout, a.sdo, b, hk, rt, r1);
@@ -536,11 +576,10 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void key_grad_kernel(AttnArgs a) {
     }
   };
   auto store = [&](int buf) {
-    mq.store(qs[buf], S);
-    md.store(gs[buf], S);
+    mq.store(qs[buf]);
+    md.store(gs[buf]);
     if ((int)threadIdx.x < BQ) { lses[buf][threadIdx.x] = ml; deltas[buf][threadIdx.x] = mt; los[buf][threadIdx.x] = mlo; his[buf][threadIdx.x] = mhi; }
   };
-  int rt = q0 * a.group, buf = 0;
   if (rt < r1) {
     fetch(rt);
     store(0);
@@ -560,7 +599,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void key_grad_kernel(AttnArgs a) {
         for (int c = 0; c < NB; ++c) s[u][c] = dp[u][c] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < DP / El::KF; ++k) {
-          const typename El::Frag qf = frag_rows(qt, S, (y + u) * 16, k * El::KF), df = frag_rows(gt, S, (y + u) * 16, k * El::KF);
+          const typename El::Frag qf = placed_rows<T, DP>(qt, (y + u) * 16, k * El::KF), df = placed_rows<T, DP>(gt, (y + u) * 16, k * El::KF);
 #pragma unroll
           for (int c = 0; c < NB; ++c) {
             s[u][c] = El::mma(qf, kf[c][k], s[u][c]);
@@ -598,7 +637,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void key_grad_kernel(AttnArgs a) {
       }
 #pragma unroll
       for (int x = 0; x < DB; ++x) {
-        const typename El::Frag df = frag_cols<T, true>(gt, S, y * 16, x * 16), qf = frag_cols<T, true>(qt, S, y * 16, x * 16);
+        const typename El::Frag df = placed_cols<T, DP>(gt, y * 16, x * 16), qf = placed_cols<T, DP>(qt, y * 16, x * 16);
 #pragma unroll
         for (int c = 0; c < NB; ++c) {
           dv[x][c] = El::mma(df, pf[c], dv[x][c]);
@@ -612,6 +651,16 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void key_grad_kernel(AttnArgs a) {
   for (int c = 0; c < NB; ++c) {
     const int j = jw + c * 16;
     if (j >= a.k_len) continue;
+    if (runs > 1) {                                           // dk's runs, then dv's
+      const int64_t unit = (int64_t)b * a.kv_heads + hk, kept = (int64_t)a.lists * a.kv_heads * runs * a.k_len * a.d;
+      float* p = part + ((unit * runs + pos.run) * a.k_len + j) * a.d;
+#pragma unroll
+      for (int x = 0; x < DB; ++x) {
+        store4(p, x * 16 + 4 * g, a.d, dk[x][c] * a.scale);
+        store4(p + kept, x * 16 + 4 * g, a.d, kShift<T> != 0.f ? dv[x][c] * kUnshift<T> : dv[x][c]);
+      }
+      continue;
+    }
     T* krow = dense_row<T>(a, a.dk, a.k_len, a.kv_heads, b, j, hk);
     T* vrow = dense_row<T>(a, a.dv, a.k_len, a.kv_heads, b, j, hk);
 #pragma unroll
@@ -622,31 +671,136 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void key_grad_kernel(AttnArgs a) {
   }
 }
 
+// out, lse: the runs' softmaxes in their order.  One wave a row, four numbers a lane.
+template <class T>
+__global__ __launch_bounds__(256) void join_kernel(AttnArgs a, int runs, const float* part) {
+  const int rows = a.q_len * a.group, lane = threadIdx.x & 63;
+  const int64_t n = (int64_t)a.lists * a.kv_heads * rows, x = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (x >= n) return;
+  const int64_t unit = x / rows;
+  const int r = (int)(x % rows), b = (int)(unit / a.kv_heads), hk = (int)(unit % a.kv_heads);
+  const int i = query_of(a, r), head = hk * a.group + r - i * a.group;
+  const List l = list_of(a, b);
+  int lo, hi;
+  seen(a, l, i, lo, hi);
+  const bool any = hi > lo;
+  const int64_t ld = a.d + 2;
+  const float* p = part + (unit * runs * rows + r) * ld;
+  float top = -INFINITY;
+  for (int s = lane; s < runs; s += 64) top = fmaxf(top, p[(int64_t)s * rows * ld]);
+  for (int w = 32; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
+  const float ref = top == -INFINITY ? 0.f : top;
+  float sum = 0.f;
+  floatx4 o = {0.f, 0.f, 0.f, 0.f};
+  const int at = 4 * lane;
+  for (int s = 0; s < runs; ++s) {
+    const float* y = p + (int64_t)s * rows * ld;
+    const float w = __builtin_amdgcn_exp2f(y[0] - ref);
+    if (w == 0.f) continue;                                   // a run behind the list's end holds nothing
+    sum += y[1] * w;
+    if (at < a.d) o += load4(y + 2, at, a.d) * w;
+  }
+  const float inv = any ? 1.f / sum : 0.f;
+  if (at < a.d) store4(const_cast<T*>(row_of<T>(a.o, a.so, b, i, head)), at, a.d, any ? o * inv : floatx4{0.f, 0.f, 0.f, 0.f});
+  if (lane == 0) a.lse[((int64_t)b * a.heads + head) * a.q_len + i] = any ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+}
+
+// A gradient's rows [lists, len, kv_heads * group], or two gradients' one after the other: the runs' sums in their order.  One wave a row.
+template <class T>
+__global__ __launch_bounds__(256) void sum_runs_kernel(AttnArgs a, void* out, void* second, int len, int group, int runs, const float* part) {
+  const int rows = len * group, at = 4 * (threadIdx.x & 63);
+  const int64_t n = (int64_t)a.lists * a.kv_heads * rows;
+  int64_t x = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (x >= n && second) {
+    x -= n;
+    out = second;
+    part += n * runs * a.d;
+  }
+  if (x >= n || at >= a.d) return;
+  const int64_t unit = x / rows;
+  const int r = (int)(x % rows), b = (int)(unit / a.kv_heads), hk = (int)(unit % a.kv_heads), i = r / group;
+  const float* p = part + (unit * runs * rows + r) * a.d;
+  floatx4 v = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < runs; ++s) v += load4(p + (int64_t)s * rows * a.d, at, a.d);
+  store4(dense_row<T>(a, out, len, a.kv_heads * group, b, i, hk * group + r - i * group), at, a.d, v);
+}
+template <class T>
+hipError_t sum_runs(const AttnArgs& a, void* out, void* second, int len, int group, int runs, const float* part, hipStream_t s) {
+  const int64_t rows = (int64_t)a.lists * a.kv_heads * len * group * (second ? 2 : 1);
+  return launch(sum_runs_kernel<T>, (rows + 3) / 4, 256, s, a, out, second, len, group, runs, part);
+}
+
+// How many rows or keys a workgroup takes.  16-bit types: 128 queries, four waves of 32; the dk/dv kernel keeps twice the operands and
+// sums a wave, so eight waves of 16 keys (four of 32 in 479 registers, one wave a SIMD: 1,323 us where these take 874; four of 32 with the values
+// in LDS: as long as these).  fp32: 64, four waves
+// of 16.
 template <class T, int DP>
-hipError_t forward(const AttnArgs& a, hipStream_t s) {
-  constexpr int NB = sizeof(T) == 4 || DP > 128 ? 1 : 2;
-  const int64_t tiles = ((int64_t)a.q_len * a.group + 64 * NB - 1) / (64 * NB);
-  return launch(forward_kernel<T, DP, NB, 4>, tiles * a.lists * a.kv_heads, 256, s, a);
+struct Shape {
+  static constexpr int NB = sizeof(T) == 4 || DP > 128 ? 1 : 2, BQ = stream_rows<T, DP>();
+  static constexpr int KW = sizeof(T) == 2 && DP <= 128 ? 8 : 4, OCC = DP <= 128 ? 2 : 1;
+  static int64_t query_tiles(const AttnArgs& a) { return ((int64_t)a.q_len * a.group + 64 * NB - 1) / (64 * NB); }
+  static int64_t key_tiles(const AttnArgs& a) { return ((int64_t)a.k_len + 16 * KW - 1) / (16 * KW); }
+  static int64_t pairs(const AttnArgs& a) { return (int64_t)a.lists * a.kv_heads; }
+  static int64_t reach(const AttnArgs& a, int64_t len, int64_t tile) { return a.window && a.window + tile < len ? a.window + tile : len; }
+  static int query_runs(const AttnArgs& a) { return runs_for(query_tiles(a) * pairs(a), reach(a, a.k_len, 64 * NB / a.group + 1)); }
+  static int key_runs(const AttnArgs& a) { return runs_for(key_tiles(a) * pairs(a), reach(a, a.q_len, 16 * KW) * a.group); }
+  static size_t forward_bytes(const AttnArgs& a) {
+    const int r = query_runs(a);
+    return r > 1 ? (size_t)pairs(a) * r * a.q_len * a.group * (a.d + 2) * sizeof(float) : 0;
+  }
+  // delta | the runs' sums of dq, and after it of dk and dv
+  static size_t delta_bytes(const AttnArgs& a) { return ((size_t)a.lists * a.q_len * a.heads * sizeof(float) + 255) / 256 * 256; }
+  static size_t backward_bytes(const AttnArgs& a) {
+    const int rq = query_runs(a), rk = key_runs(a);
+    const size_t q = rq > 1 ? (size_t)pairs(a) * rq * a.q_len * a.group * a.d : 0, k = rk > 1 ? (size_t)pairs(a) * rk * a.k_len * a.d * 2 : 0;
+    return delta_bytes(a) + (q > k ? q : k) * sizeof(float);
+  }
+};
+
+template <class T, int DP>
+hipError_t forward(const AttnArgs& a, float* part, hipStream_t s) {
+  using Sh = Shape<T, DP>;
+  const int runs = Sh::query_runs(a);
+  const hipError_t e = launch(forward_kernel<T, DP, Sh::NB, 4>, Sh::query_tiles(a) * Sh::pairs(a) * runs, 256, s, a, runs, part);
+  if (e != hipSuccess || runs == 1) return e;
+  return launch(join_kernel<T>, (Sh::pairs(a) * a.q_len * a.group + 3) / 4, 256, s, a, runs, (const float*)part);
 }
 
 template <class T, int DP>
-hipError_t backward(const AttnArgs& a, hipStream_t s) {
-  constexpr int NB = sizeof(T) == 4 || DP > 128 ? 1 : 2, BQ = stream_rows<T, DP>();
-  const int64_t qt = ((int64_t)a.q_len * a.group + 64 * NB - 1) / (64 * NB), kt = ((int64_t)a.k_len + 64 * NB - 1) / (64 * NB);
+hipError_t backward(AttnArgs a, void* ws, hipStream_t s) {
+  using Sh = Shape<T, DP>;
+  a.delta = static_cast<float*>(ws);
+  float* part = reinterpret_cast<float*>(static_cast<char*>(ws) + Sh::delta_bytes(a));
+  const int rq = Sh::query_runs(a), rk = Sh::key_runs(a);
   hipError_t e = hipSuccess;
-  if (qt) e = launch(query_grad_kernel<T, DP, NB, 4>, qt * a.lists * a.kv_heads, 256, s, a);
-  if (e == hipSuccess && kt) e = launch(key_grad_kernel<T, DP, NB, 4, BQ, 1>, kt * a.lists * a.kv_heads, 256, s, a);
+  if (a.q_len) {
+    e = launch(query_grad_kernel<T, DP, Sh::NB, 4>, Sh::query_tiles(a) * Sh::pairs(a) * rq, 256, s, a, rq, part);
+    if (e == hipSuccess && rq > 1) e = sum_runs<T>(a, a.dq, nullptr, a.q_len, a.group, rq, part, s);
+  }
+  if (e == hipSuccess && a.k_len) {
+    e = launch(key_grad_kernel<T, DP, 1, Sh::KW, Sh::BQ, Sh::OCC>, Sh::key_tiles(a) * Sh::pairs(a) * rk, Sh::KW * 64, s, a, rk, part);
+    if (e == hipSuccess && rk > 1) e = sum_runs<T>(a, a.dk, a.dv, a.k_len, 1, rk, part, s);
+  }
   return e;
 }
 
-template <class T>
-hipError_t forward_of(const AttnArgs& a, hipStream_t s) {
-  return a.d <= 64 ? forward<T, 64>(a, s) : a.d <= 128 ? forward<T, 128>(a, s) : forward<T, 256>(a, s);
+template <class T, class F>
+auto by_width(const AttnArgs& a, F f) {
+  return a.d <= 64 ? f(Shape<T, 64>(), std::integral_constant<int, 64>()) : a.d <= 128 ? f(Shape<T, 128>(), std::integral_constant<int, 128>())
+                                                                                       : f(Shape<T, 256>(), std::integral_constant<int, 256>());
 }
 template <class T>
-hipError_t backward_of(const AttnArgs& a, hipStream_t s) {
-  return a.d <= 64 ? backward<T, 64>(a, s) : a.d <= 128 ? backward<T, 128>(a, s) : backward<T, 256>(a, s);
+hipError_t forward_of(const AttnArgs& a, void* ws, hipStream_t s) {
+  return by_width<T>(a, [&](auto, auto d) { return forward<T, d()>(a, static_cast<float*>(ws), s); });
 }
+template <class T>
+hipError_t backward_of(const AttnArgs& a, void* ws, hipStream_t s) {
+  return by_width<T>(a, [&](auto, auto d) { return backward<T, d()>(a, ws, s); });
+}
+template <class T>
+size_t forward_bytes_of(const AttnArgs& a) { return by_width<T>(a, [&](auto sh, auto) { return sh.forward_bytes(a); }); }
+template <class T>
+size_t backward_bytes_of(const AttnArgs& a) { return by_width<T>(a, [&](auto sh, auto) { return sh.backward_bytes(a); }); }
 
 }  // namespace attn
 }  // namespace stgn

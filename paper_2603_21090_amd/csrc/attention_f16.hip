@@ -2,6 +2,8 @@
 #include "attention.h"
 
 namespace stgn {
-hipError_t attention_f16(const AttnArgs& a, hipStream_t s) { return attn::forward_of<_Float16>(a, s); }
-hipError_t attention_grad_f16(const AttnArgs& a, hipStream_t s) { return attn::backward_of<_Float16>(a, s); }
+size_t attention_bytes_f16(const AttnArgs& a) { return attn::forward_bytes_of<_Float16>(a); }
+size_t attention_grad_bytes_f16(const AttnArgs& a) { return attn::backward_bytes_of<_Float16>(a); }
+hipError_t attention_f16(const AttnArgs& a, void* ws, hipStream_t s) { return attn::forward_of<_Float16>(a, ws, s); }
+hipError_t attention_grad_f16(const AttnArgs& a, void* ws, hipStream_t s) { return attn::backward_of<_Float16>(a, ws, s); }
 }  // namespace stgn

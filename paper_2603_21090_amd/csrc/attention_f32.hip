@@ -2,6 +2,8 @@
 #include "attention.h"
 
 namespace stgn {
-hipError_t attention_f32(const AttnArgs& a, hipStream_t s) { return attn::forward_of<float>(a, s); }
-hipError_t attention_grad_f32(const AttnArgs& a, hipStream_t s) { return attn::backward_of<float>(a, s); }
+size_t attention_bytes_f32(const AttnArgs& a) { return attn::forward_bytes_of<float>(a); }
+size_t attention_grad_bytes_f32(const AttnArgs& a) { return attn::backward_bytes_of<float>(a); }
+hipError_t attention_f32(const AttnArgs& a, void* ws, hipStream_t s) { return attn::forward_of<float>(a, ws, s); }
+hipError_t attention_grad_f32(const AttnArgs& a, void* ws, hipStream_t s) { return attn::backward_of<float>(a, ws, s); }
 }  // namespace stgn

@@ -242,40 +242,6 @@ __global__ __launch_bounds__(256) void rows_forward_kernel(AttnArgs a, RowPlan p
   }
 }
 
-// one wave a row: the runs' softmaxes in their order, four numbers a lane
-template <class T>
-__global__ __launch_bounds__(256) void rows_join_kernel(AttnArgs a, int splits, const float* part) {
-  const int rows = a.q_len * a.group, lane = threadIdx.x & 63;
-  const int64_t n = (int64_t)a.lists * a.kv_heads * rows, x = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (x >= n) return;
-  const int64_t unit = x / rows;
-  const int r = (int)(x % rows), b = (int)(unit / a.kv_heads), hk = (int)(unit % a.kv_heads);
-  const int i = query_of(a, r), head = hk * a.group + r - i * a.group;
-  const List l = list_of(a, b);
-  int lo, hi;
-  seen(a, l, i, lo, hi);
-  const bool any = hi > lo;
-  const int64_t ld = a.d + 2;
-  const float* p = part + (unit * splits * rows + r) * ld;
-  float top = -INFINITY;
-  for (int s = lane; s < splits; s += 64) top = fmaxf(top, p[(int64_t)s * rows * ld]);
-  for (int w = 32; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
-  const float ref = top == -INFINITY ? 0.f : top;
-  float sum = 0.f;
-  floatx4 o = {0.f, 0.f, 0.f, 0.f};
-  const int at = 4 * lane;
-  for (int s = 0; s < splits; ++s) {
-    const float* y = p + (int64_t)s * rows * ld;
-    const float w = __builtin_amdgcn_exp2f(y[0] - ref);
-    if (w == 0.f) continue;                                   // a run behind the list's end holds nothing
-    sum += y[1] * w;
-    if (at < a.d) o += load4(y + 2, at, a.d) * w;
-  }
-  const float inv = any ? 1.f / sum : 0.f;
-  if (at < a.d) store4(const_cast<T*>(row_of<T>(a.o, a.so, b, i, head)), at, a.d, any ? o * inv : floatx4{0.f, 0.f, 0.f, 0.f});
-  if (lane == 0) a.lse[((int64_t)b * a.heads + head) * a.q_len + i] = any ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
-}
-
 // Gradients: one pass over the keys; each is written back as dk and dv, and dq adds up in the lane groups.
 template <class T, int L, int R, int U, bool WIDE>
 __global__ __launch_bounds__(256) void rows_grad_kernel(AttnArgs a, RowPlan plan, float* part) {
@@ -403,22 +369,6 @@ __global__ __launch_bounds__(256) void rows_grad_kernel(AttnArgs a, RowPlan plan
   }
 }
 
-// dq: the runs' sums in their order
-template <class T>
-__global__ __launch_bounds__(256) void rows_grad_join_kernel(AttnArgs a, int splits, const float* part) {
-  const int rows = a.q_len * a.group;
-  const int64_t n = (int64_t)a.lists * a.kv_heads * rows, x = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int at = 4 * (threadIdx.x & 63);
-  if (x >= n || at >= a.d) return;
-  const int64_t unit = x / rows;
-  const int r = (int)(x % rows), b = (int)(unit / a.kv_heads), hk = (int)(unit % a.kv_heads);
-  const int i = query_of(a, r), head = hk * a.group + r - i * a.group;
-  const float* p = part + (unit * splits * rows + r) * a.d;
-  floatx4 v = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < splits; ++s) v += load4(p + (int64_t)s * rows * a.d, at, a.d);
-  store4(dense_row<T>(a, a.dq, a.q_len, a.heads, b, i, head), at, a.d, v);
-}
-
 // Rows a list and key head that go this way: eight; four in the gradient of 16-bit types, whose lanes hold twice the numbers
 // (q, dout and dq of eight rows would be 192 registers).
 inline int most_rows(bool grad, bool narrow) { return grad && narrow ? 4 : 8; }
@@ -456,7 +406,8 @@ hipError_t rows_launch(const AttnArgs& a, float* part, hipStream_t s) {
     e = wide_rows(a) ? launch(rows_forward_kernel<T, L, R, U, true>, units * p.splits, 256, s, a, p, part)
                      : launch(rows_forward_kernel<T, L, R, U, false>, (units + 3) / 4, 256, s, a, p, part);
   if (e != hipSuccess || p.splits == 1) return e;
-  return launch(GRAD ? rows_grad_join_kernel<T> : rows_join_kernel<T>, (units * rows + 3) / 4, 256, s, a, p.splits, (const float*)part);
+  if constexpr (GRAD) return sum_runs<T>(a, a.dq, nullptr, a.q_len, a.group, p.splits, part, s);
+  else return launch(join_kernel<T>, (units * rows + 3) / 4, 256, s, a, p.splits, (const float*)part);
 }
 
 template <class T, int L, bool GRAD>

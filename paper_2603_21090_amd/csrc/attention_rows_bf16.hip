@@ -2,6 +2,6 @@
 #include "attention_rows.h"
 
 namespace stgn {
-hipError_t attention_rows_bf16(const AttnArgs& a, float* part, hipStream_t s) { return attn::rows_of<__bf16, false>(a, part, s); }
-hipError_t attention_rows_grad_bf16(const AttnArgs& a, float* part, hipStream_t s) { return attn::rows_of<__bf16, true>(a, part, s); }
+hipError_t attention_rows_bf16(const AttnArgs& a, void* ws, hipStream_t s) { return attn::rows_of<__bf16, false>(a, static_cast<float*>(ws), s); }
+hipError_t attention_rows_grad_bf16(const AttnArgs& a, void* ws, hipStream_t s) { return attn::rows_of<__bf16, true>(a, static_cast<float*>(ws), s); }
 }  // namespace stgn

@@ -14,7 +14,7 @@ struct AttnArgs {
   const void *q, *k, *v, *dout, *out;                         // dq, dk, dv: dense [lists, rows, heads, d]
   void *o, *dq, *dk, *dv;
   float* lse;                                                 // [lists, heads, q_len]
-  float* delta;                                               // workspace of the gradient: dout . out, laid out as lse
+  float* delta;                                               // of the gradient: dout . out, laid out as lse
   const int *q_lens, *k_lens;                                 // [lists] or null: every list is q_len, k_len long
   Strides sq, sk, sv, so, sdo;
   int lists, q_len, k_len, heads, kv_heads, group, group_shift, d;                // group: query heads a key head; its logarithm or -1

@@ -9,10 +9,12 @@
 namespace stgn {
 
 #define STGN_PER_TYPE(T)                                                                  \
-  hipError_t attention_##T(const AttnArgs& a, hipStream_t s);                             \
-  hipError_t attention_grad_##T(const AttnArgs& a, hipStream_t s);                        \
-  hipError_t attention_rows_##T(const AttnArgs& a, float* part, hipStream_t s);           \
-  hipError_t attention_rows_grad_##T(const AttnArgs& a, float* part, hipStream_t s);      \
+  size_t attention_bytes_##T(const AttnArgs& a);                                          \
+  size_t attention_grad_bytes_##T(const AttnArgs& a);                                     \
+  hipError_t attention_##T(const AttnArgs& a, void* ws, hipStream_t s);                   \
+  hipError_t attention_grad_##T(const AttnArgs& a, void* ws, hipStream_t s);              \
+  hipError_t attention_rows_##T(const AttnArgs& a, void* ws, hipStream_t s);              \
+  hipError_t attention_rows_grad_##T(const AttnArgs& a, void* ws, hipStream_t s);         \
   size_t linear_bytes_##T(const LinearArgs& a);                                           \
   size_t linear_grad_bytes_##T(const LinearGradArgs& a);                                  \
   hipError_t linear_##T(const LinearArgs& a, void* ws, hipStream_t s);                    \
@@ -33,9 +35,11 @@ bool few_rows(const AttnArgs& a, int dtype, bool grad) {
   return (int64_t)a.q_len * a.group <= attn::most_rows(grad, dtype != STGN_F32);
 }
 
-size_t attention_bytes(const AttnArgs& a, int dtype) { return few_rows(a, dtype, false) ? attn::row_part_bytes(a, false) : 0; }
+size_t attention_bytes(const AttnArgs& a, int dtype) {
+  return few_rows(a, dtype, false) ? attn::row_part_bytes(a, false) : STGN_BY_TYPE(dtype, attention_bytes, a);
+}
 size_t attention_grad_bytes(const AttnArgs& a, int dtype) {
-  return few_rows(a, dtype, true) ? attn::row_part_bytes(a, true) : (size_t)a.lists * a.q_len * a.heads * sizeof(float);   // delta
+  return few_rows(a, dtype, true) ? attn::row_part_bytes(a, true) : STGN_BY_TYPE(dtype, attention_grad_bytes, a);
 }
 
 }  // namespace stgn
@@ -260,20 +264,19 @@ int stgn_attention(const stgn_attention_args* args, void* device_workspace, size
   const AttnArgs a = attention_args(args);
   if (const int rc = check_workspace(attention_bytes(a, (int)args->dtype), device_workspace, device_bytes)) return rc;
   if (a.lists == 0 || a.q_len == 0) return STGN_OK;
-  if (few_rows(a, (int)args->dtype, false))
-    return finish(STGN_BY_TYPE(args->dtype, attention_rows, a, static_cast<float*>(device_workspace), static_cast<hipStream_t>(hip_stream)));
-  return finish(STGN_BY_TYPE(args->dtype, attention, a, static_cast<hipStream_t>(hip_stream)));
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  if (few_rows(a, (int)args->dtype, false)) return finish(STGN_BY_TYPE(args->dtype, attention_rows, a, device_workspace, s));
+  return finish(STGN_BY_TYPE(args->dtype, attention, a, device_workspace, s));
 }
 
 int stgn_attention_grad(const stgn_attention_args* args, void* device_workspace, size_t device_bytes, void* hip_stream) {
   if (const int rc = check_attention(args, true, false)) return rc;
-  AttnArgs a = attention_args(args);
+  const AttnArgs a = attention_args(args);
   if (const int rc = check_workspace(attention_grad_bytes(a, (int)args->dtype), device_workspace, device_bytes)) return rc;
   if (a.lists == 0) return STGN_OK;
-  if (few_rows(a, (int)args->dtype, true))
-    return finish(STGN_BY_TYPE(args->dtype, attention_rows_grad, a, static_cast<float*>(device_workspace), static_cast<hipStream_t>(hip_stream)));
-  a.delta = static_cast<float*>(device_workspace);
-  return finish(STGN_BY_TYPE(args->dtype, attention_grad, a, static_cast<hipStream_t>(hip_stream)));
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  if (few_rows(a, (int)args->dtype, true)) return finish(STGN_BY_TYPE(args->dtype, attention_rows_grad, a, device_workspace, s));
+  return finish(STGN_BY_TYPE(args->dtype, attention_grad, a, device_workspace, s));
 }
 
 }  // extern "C"

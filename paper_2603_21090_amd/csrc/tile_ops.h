@@ -111,6 +111,34 @@ __device__ inline typename Elem<T>::Frag frag_cols(const T* tile, int stride, in
   }
 }
 
+// Where a row of a 16-bit tile lies that is read both ways (fragments along its rows, and down them in the split order).  LDS gives 256
+// bytes a cycle: sixteen rows of 16 bytes, or eight rows of 32 bytes of a transposed read.  With rows 16 bytes longer than a multiple of 128,
+// any order of sixteen rows serves the first; for the second, rows 0 .. 7 and 8 .. 15 lie two places apart.  (Rows in their own order: 40 % of
+// the attention kernels' LDS cycles were conflicts.  Pieces permuted within a row instead of padding: no conflicts, but an address
+// register per fragment.)  fp32 tiles are read down their rows four rows of 64 bytes a cycle: in their own order.
+template <class T>
+__device__ inline int placed(int row) {
+  if constexpr (sizeof(T) == 4) return row;
+  else return (row & ~15) | ((row & 7) << 1) | ((row >> 3) & 1);
+}
+template <class T, int COLS>
+__device__ inline typename Elem<T>::Frag placed_rows(const T* tile, int row, int k) {        // row: a multiple of 16
+  constexpr int S = lds_stride<T>(COLS);
+  const int lane = threadIdx.x & 63;
+  return *reinterpret_cast<const typename Elem<T>::Frag*>(tile + (row + placed<T>(lane & 15)) * S + k + Elem<T>::E * (lane >> 4));
+}
+template <class T, int COLS>
+__device__ inline typename Elem<T>::Frag placed_cols(const T* tile, int row, int col) {      // the split order
+  constexpr int S = lds_stride<T>(COLS);
+  const int lane = threadIdx.x & 63, g = lane >> 4, i = lane & 15;
+  if constexpr (sizeof(T) == 4) {
+    return frag_cols<T, true>(tile, S, row, col);
+  } else {
+    const T* p = tile + (row + placed<T>(4 * g + (i >> 2))) * S + col + 4 * (i & 3);
+    return join_transposed<T>(read_transposed(p), read_transposed(p + 16 * S));
+  }
+}
+
 // 16 bytes at p of which `count` elements exist (the rest zero)
 template <class T>
 __device__ inline u32x4 load16(const T* p, int count) {
@@ -186,6 +214,17 @@ struct TileMove {
   }
 };
 
+// the pieces of StreamMove and its like into their tile
+template <class T, int ROWS, int COLS, int THREADS, int NP>
+__device__ inline void store_placed(T* tile, const u32x4 (&r)[NP]) {
+  constexpr int E = Elem<T>::E, PER_ROW = COLS / E;
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int row = (int)threadIdx.x / PER_ROW + i * (THREADS / PER_ROW);
+    *reinterpret_cast<u32x4*>(tile + placed<T>(row) * lds_stride<T>(COLS) + (int)threadIdx.x % PER_ROW * E) = r[i];
+  }
+}
+
 // The same for consecutive tiles of a matrix whose rows lie `stride` apart: addresses are computed once and advance by a tile.
 template <class T, int ROWS, int COLS, int THREADS>
 struct StreamMove {
@@ -212,11 +251,7 @@ struct StreamMove {
     }
     at += ROWS * stride;
   }
-  __device__ inline void store(T* tile, int lds_row) const {
-    T* to = tile + row * lds_row + (int)threadIdx.x % PER_ROW * E;
-#pragma unroll
-    for (int i = 0; i < NP; ++i) *reinterpret_cast<u32x4*>(to + i * APART * lds_row) = r[i];
-  }
+  __device__ inline void store(T* tile) const { store_placed<T, ROWS, COLS, THREADS>(tile, r); }
 };
 
 }  // namespace stgn
