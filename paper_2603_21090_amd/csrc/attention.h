@@ -671,11 +671,37 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void key_grad_kernel(AttnArgs a, i
   }
 }
 
-// out, lse: the runs' softmaxes in their order.  One wave a row, four numbers a lane.
+// The runs of a row are joined by a wave, or where they are many by the four waves of a workgroup (one row 256 runs one after the other
+// took longer than the runs), four numbers a lane; always in the same order.
+constexpr int kManyRuns = 16;
+inline int64_t join_grid(int64_t rows, int runs) { return runs >= kManyRuns ? rows : (rows + 3) / 4; }
+
+// sums of f(run) over the runs that this wave takes, then over the workgroup's waves where they share the row; true where the sum is
+template <class F>
+__device__ inline bool over_runs(int runs, F f, floatx4& v, float& extra) {
+  __shared__ floatx4 part[4][64];
+  __shared__ float parts[4][64];
+  const bool many = runs >= kManyRuns;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  v = floatx4{0.f, 0.f, 0.f, 0.f};
+  extra = 0.f;
+#pragma unroll 4
+  for (int s = many ? wave : 0; s < runs; s += many ? 4 : 1) f(s, v, extra);
+  if (!many) return true;
+  part[wave][lane] = v;
+  parts[wave][lane] = extra;
+  __syncthreads();
+  if (wave) return false;
+  v = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
+  extra = (parts[0][lane] + parts[1][lane]) + (parts[2][lane] + parts[3][lane]);
+  return true;
+}
+
+// out, lse: the runs' softmaxes
 template <class T>
 __global__ __launch_bounds__(256) void join_kernel(AttnArgs a, int runs, const float* part) {
   const int rows = a.q_len * a.group, lane = threadIdx.x & 63;
-  const int64_t n = (int64_t)a.lists * a.kv_heads * rows, x = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t n = (int64_t)a.lists * a.kv_heads * rows, x = runs >= kManyRuns ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (x >= n) return;
   const int64_t unit = x / rows;
   const int r = (int)(x % rows), b = (int)(unit / a.kv_heads), hk = (int)(unit % a.kv_heads);
@@ -690,44 +716,47 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a, int runs, const f
   for (int s = lane; s < runs; s += 64) top = fmaxf(top, p[(int64_t)s * rows * ld]);
   for (int w = 32; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
   const float ref = top == -INFINITY ? 0.f : top;
-  float sum = 0.f;
-  floatx4 o = {0.f, 0.f, 0.f, 0.f};
+  float sum;
+  floatx4 o;
   const int at = 4 * lane;
-  for (int s = 0; s < runs; ++s) {
-    const float* y = p + (int64_t)s * rows * ld;
+  const bool mine = over_runs(runs, [&](int s, floatx4& v, float& t) {
+    const float* y = p + (int64_t)s * rows * ld;              // (a run behind the list's end holds zeros)
     const float w = __builtin_amdgcn_exp2f(y[0] - ref);
-    if (w == 0.f) continue;                                   // a run behind the list's end holds nothing
-    sum += y[1] * w;
-    if (at < a.d) o += load4(y + 2, at, a.d) * w;
-  }
+    t += y[1] * w;
+    if (at < a.d) v += load4(y + 2, at, a.d) * w;
+  }, o, sum);
+  if (!mine) return;
   const float inv = any ? 1.f / sum : 0.f;
   if (at < a.d) store4(const_cast<T*>(row_of<T>(a.o, a.so, b, i, head)), at, a.d, any ? o * inv : floatx4{0.f, 0.f, 0.f, 0.f});
   if (lane == 0) a.lse[((int64_t)b * a.heads + head) * a.q_len + i] = any ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
 }
 
-// A gradient's rows [lists, len, kv_heads * group], or two gradients' one after the other: the runs' sums in their order.  One wave a row.
+// A gradient's rows [lists, len, kv_heads * group], or two gradients' one after the other: the runs' sums
 template <class T>
 __global__ __launch_bounds__(256) void sum_runs_kernel(AttnArgs a, void* out, void* second, int len, int group, int runs, const float* part) {
   const int rows = len * group, at = 4 * (threadIdx.x & 63);
   const int64_t n = (int64_t)a.lists * a.kv_heads * rows;
-  int64_t x = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  int64_t x = runs >= kManyRuns ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (x >= n && second) {
     x -= n;
     out = second;
     part += n * runs * a.d;
   }
-  if (x >= n || at >= a.d) return;
+  if (x >= n) return;
   const int64_t unit = x / rows;
   const int r = (int)(x % rows), b = (int)(unit / a.kv_heads), hk = (int)(unit % a.kv_heads), i = r / group;
   const float* p = part + (unit * runs * rows + r) * a.d;
-  floatx4 v = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < runs; ++s) v += load4(p + (int64_t)s * rows * a.d, at, a.d);
-  store4(dense_row<T>(a, out, len, a.kv_heads * group, b, i, hk * group + r - i * group), at, a.d, v);
+  floatx4 v;
+  float none;
+  const bool mine = over_runs(runs, [&](int s, floatx4& v, float&) {
+    if (at < a.d) v += load4(p + (int64_t)s * rows * a.d, at, a.d);
+  }, v, none);
+  if (mine && at < a.d) store4(dense_row<T>(a, out, len, a.kv_heads * group, b, i, hk * group + r - i * group), at, a.d, v);
 }
 template <class T>
 hipError_t sum_runs(const AttnArgs& a, void* out, void* second, int len, int group, int runs, const float* part, hipStream_t s) {
   const int64_t rows = (int64_t)a.lists * a.kv_heads * len * group * (second ? 2 : 1);
-  return launch(sum_runs_kernel<T>, (rows + 3) / 4, 256, s, a, out, second, len, group, runs, part);
+  return launch(sum_runs_kernel<T>, join_grid(rows, runs), 256, s, a, out, second, len, group, runs, part);
 }
 
 // How many rows or keys a workgroup takes.  16-bit types: 128 queries, four waves of 32; the dk/dv kernel keeps twice the operands and
@@ -763,7 +792,7 @@ hipError_t forward(const AttnArgs& a, float* part, hipStream_t s) {
   const int runs = Sh::query_runs(a);
   const hipError_t e = launch(forward_kernel<T, DP, Sh::NB, 4>, Sh::query_tiles(a) * Sh::pairs(a) * runs, 256, s, a, runs, part);
   if (e != hipSuccess || runs == 1) return e;
-  return launch(join_kernel<T>, (Sh::pairs(a) * a.q_len * a.group + 3) / 4, 256, s, a, runs, (const float*)part);
+  return launch(join_kernel<T>, join_grid(Sh::pairs(a) * a.q_len * a.group, runs), 256, s, a, runs, (const float*)part);
 }
 
 template <class T, int DP>

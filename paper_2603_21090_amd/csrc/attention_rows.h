@@ -117,25 +117,16 @@ __global__ __launch_bounds__(256) void rows_forward_kernel(AttnArgs a, RowPlan p
   const List l = list_of(a, b);
 
   int lo[R], hi[R], k0 = a.k_len, k1 = 0, all0 = 0, all1 = a.k_len;
-  float q[R][E];
-  Softmax<E> x[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const int i = query_of(a, r);
     lo[r] = hi[r] = 0;
-    u32x4 raw = {0, 0, 0, 0};
-    if (r < rows) {
-      seen(a, l, i, lo[r], hi[r]);
-      if (i < l.qn && at < a.d) raw = load16(row_of<T>(a.q, a.sq, b, i, hk * a.group + r - i * a.group) + at, a.d - at);
-    }
+    if (r < rows) seen(a, l, query_of(a, r), lo[r], hi[r]);
     if (hi[r] > lo[r]) {
       k0 = min(k0, lo[r]);
       k1 = max(k1, hi[r]);
     }
     all0 = max(all0, lo[r]);
     all1 = min(all1, hi[r]);
-    spread<T>(raw, q[r]);
-    x[r].clear();
   }
   if (WIDE) {
     k0 = max(k0, split * plan.per);
@@ -144,9 +135,8 @@ __global__ __launch_bounds__(256) void rows_forward_kernel(AttnArgs a, RowPlan p
   const float scale2 = a.scale * kLog2e;
   const T* kp = row_of<T>(a.k, a.sk, b, 0, hk) + at;
   const T* vp = row_of<T>(a.v, a.sv, b, 0, hk) + at;
-
-  for (int base = k0 + (WIDE ? wave * STEP : 0); base < k1; base += WIDE ? 4 * STEP : STEP) {
-    u32x4 kr[U], vr[U];
+  u32x4 kr[U], vr[U];
+  auto fetch = [&](int base) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int j = base + u * G + slot;
@@ -156,6 +146,22 @@ __global__ __launch_bounds__(256) void rows_forward_kernel(AttnArgs a, RowPlan p
         vr[u] = load16(vp + (int64_t)j * a.sv.row, a.d - at);
       }
     }
+  };
+  int base = k0 + (WIDE ? wave * STEP : 0);
+  if (base < k1) fetch(base);                                 // (with the rows on their way too: one wait for a short list)
+
+  float q[R][E];
+  Softmax<E> x[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int i = query_of(a, r);
+    u32x4 raw = {0, 0, 0, 0};
+    if (r < rows && i < l.qn && at < a.d) raw = load16(row_of<T>(a.q, a.sq, b, i, hk * a.group + r - i * a.group) + at, a.d - at);
+    spread<T>(raw, q[r]);
+    x[r].clear();
+  }
+
+  while (base < k1) {
     const bool partial = base < all0 || base + STEP > min(all1, k1);
     float s[R][U];
 #pragma unroll
@@ -194,6 +200,8 @@ __global__ __launch_bounds__(256) void rows_forward_kernel(AttnArgs a, RowPlan p
 #pragma unroll
         for (int j = 0; j < E; ++j) x[r].o[j] = fmaf(s[r][u], f[j], x[r].o[j]);
     }
+    base += WIDE ? 4 * STEP : STEP;
+    if (base < k1) fetch(base);
   }
 
 #pragma unroll
@@ -254,24 +262,46 @@ __global__ __launch_bounds__(256) void rows_grad_kernel(AttnArgs a, RowPlan plan
   const List l = list_of(a, b);
 
   int lo[R], hi[R], k0 = a.k_len, k1 = 0;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    lo[r] = hi[r] = 0;
+    if (r < rows) seen(a, l, query_of(a, r), lo[r], hi[r]);
+    if (hi[r] > lo[r]) {
+      k0 = min(k0, lo[r]);
+      k1 = max(k1, hi[r]);
+    }
+  }
+  const int first = WIDE ? split * plan.per : 0, last = WIDE ? min(a.k_len, (split + 1) * plan.per) : a.k_len;
+  k1 = min(k1, last);                                         // (the next run's keys: zeros here, which add nothing to dq)
+  const T* kp = row_of<T>(a.k, a.sk, b, 0, hk) + at;
+  const T* vp = row_of<T>(a.v, a.sv, b, 0, hk) + at;
+  u32x4 kr[U], vr[U];
+  auto fetch = [&](int base) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int j = base + u * G + slot;
+      kr[u] = vr[u] = u32x4{0, 0, 0, 0};
+      if (j >= k0 && j < k1 && at < a.d) {
+        kr[u] = load16(kp + (int64_t)j * a.sk.row, a.d - at);
+        vr[u] = load16(vp + (int64_t)j * a.sv.row, a.d - at);
+      }
+    }
+  };
+  int base = first + (WIDE ? wave * STEP : 0);
+  if (base < last) fetch(base);                               // (with the rows on their way too: one wait for a short list)
+
   float q[R][E], go[R][E], dq[R][E], lse2[R], delta[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int i = query_of(a, r), head = hk * a.group + r - i * a.group;
-    lo[r] = hi[r] = 0;
     u32x4 rq = {0, 0, 0, 0}, rd = rq, ro = rq;
     lse2[r] = INFINITY;                                       // a row that sees nothing has no probability
-    if (r < rows) {
-      seen(a, l, i, lo[r], hi[r]);
-      if (hi[r] > lo[r]) {
-        lse2[r] = a.lse[((int64_t)b * a.heads + head) * a.q_len + i] * kLog2e;
-        if (at < a.d) {
-          rq = load16(row_of<T>(a.q, a.sq, b, i, head) + at, a.d - at);
-          rd = load16(row_of<T>(a.dout, a.sdo, b, i, head) + at, a.d - at);
-          ro = load16(row_of<T>(a.out, a.so, b, i, head) + at, a.d - at);
-        }
-        k0 = min(k0, lo[r]);
-        k1 = max(k1, hi[r]);
+    if (hi[r] > lo[r]) {
+      lse2[r] = a.lse[((int64_t)b * a.heads + head) * a.q_len + i] * kLog2e;
+      if (at < a.d) {
+        rq = load16(row_of<T>(a.q, a.sq, b, i, head) + at, a.d - at);
+        rd = load16(row_of<T>(a.dout, a.sdo, b, i, head) + at, a.d - at);
+        ro = load16(row_of<T>(a.out, a.so, b, i, head) + at, a.d - at);
       }
     }
     float o[E];
@@ -283,27 +313,14 @@ __global__ __launch_bounds__(256) void rows_grad_kernel(AttnArgs a, RowPlan plan
     for (int j = 0; j < E; ++j) dq[r][j] = 0.f;
   }
   const float scale2 = a.scale * kLog2e;
-  const T* kp = row_of<T>(a.k, a.sk, b, 0, hk) + at;
-  const T* vp = row_of<T>(a.v, a.sv, b, 0, hk) + at;
   const int64_t out_row = (int64_t)a.kv_heads * a.d, out0 = ((int64_t)b * a.k_len * a.kv_heads + hk) * a.d + at;
   T *dk = static_cast<T*>(a.dk) + out0, *dv = static_cast<T*>(a.dv) + out0;
-  const int first = WIDE ? split * plan.per : 0, last = WIDE ? min(a.k_len, (split + 1) * plan.per) : a.k_len;
-  k1 = min(k1, last);                                         // (the next run's keys: zeros here, which add nothing to dq)
 
-  for (int base = first + (WIDE ? wave * STEP : 0); base < last; base += WIDE ? 4 * STEP : STEP) {
-    u32x4 kr[U], vr[U];
+  while (base < last) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int j = base + u * G + slot;
-      kr[u] = vr[u] = u32x4{0, 0, 0, 0};
-      if (j >= k0 && j < k1 && at < a.d) {
-        kr[u] = load16(kp + (int64_t)j * a.sk.row, a.d - at);
-        vr[u] = load16(vp + (int64_t)j * a.sv.row, a.d - at);
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int j = base + u * G + slot;
+      if (base + u * G >= last) continue;                     // (the same for all lanes)
       float k[E], v[E], gk[E], gv[E];
       spread<T>(kr[u], k);
       spread<T>(vr[u], v);
@@ -327,6 +344,8 @@ __global__ __launch_bounds__(256) void rows_grad_kernel(AttnArgs a, RowPlan plan
         store_piece(dv + (int64_t)j * out_row, gv, a.d - at);
       }
     }
+    base += WIDE ? 4 * STEP : STEP;
+    if (base < last) fetch(base);
   }
 
 #pragma unroll
@@ -373,14 +392,15 @@ __global__ __launch_bounds__(256) void rows_grad_kernel(AttnArgs a, RowPlan plan
 // (q, dout and dq of eight rows would be 192 registers).
 inline int most_rows(bool grad, bool narrow) { return grad && narrow ? 4 : 8; }
 
-// A wave a list up to 128 keys.  Longer lists get a workgroup each, and are cut into runs of at least 256 keys until there are 2,048
-// workgroups, eight a CU.
+// A wave a list up to 128 keys.  Longer lists get a workgroup each, and are cut into runs of at least 256 keys, 64 a list at most (joining
+// 256 took as long as the runs), until there are 2,048 workgroups, eight a CU.
 inline bool wide_rows(const AttnArgs& a) { return a.k_len > 128; }
 inline RowPlan row_plan(const AttnArgs& a) {
   const int64_t units = (int64_t)a.lists * a.kv_heads;
   int64_t splits = wide_rows(a) && units ? (2048 + units - 1) / units : 1;
   const int64_t most = (a.k_len + 255) / 256;
   if (splits > most) splits = most;
+  if (splits > 64) splits = 64;
   if (splits < 1) splits = 1;
   RowPlan p;
   p.per = (int)((a.k_len + splits - 1) / splits);
@@ -407,7 +427,7 @@ hipError_t rows_launch(const AttnArgs& a, float* part, hipStream_t s) {
                      : launch(rows_forward_kernel<T, L, R, U, false>, (units + 3) / 4, 256, s, a, p, part);
   if (e != hipSuccess || p.splits == 1) return e;
   if constexpr (GRAD) return sum_runs<T>(a, a.dq, nullptr, a.q_len, a.group, p.splits, part, s);
-  else return launch(join_kernel<T>, (units * rows + 3) / 4, 256, s, a, p.splits, (const float*)part);
+  else return launch(join_kernel<T>, join_grid(units * rows, p.splits), 256, s, a, p.splits, (const float*)part);
 }
 
 template <class T, int L, bool GRAD>
