@@ -141,7 +141,9 @@ __device__ inline void tile_of(unsigned id, unsigned tm, unsigned tn, int& row, 
 
 template <class T> constexpr int kTileK = 128 / (int)sizeof(T);    // 64 16-bit numbers, 32 floats: 128 bytes
 
-template <class T, int BM, int BN, int WM, int WN, bool L_ROWS, bool R_ROWS>
+// DEPTH tiles of k are on their way in registers while one is multiplied: where tiles are small and few, what a tile takes is the wait
+// for memory (13 x 4,096 x 11,008 in bf16: 26.6 us with one, 19.9 with three).
+template <class T, int BM, int BN, int WM, int WN, int DEPTH, bool L_ROWS, bool R_ROWS>
 __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product a) {
   using El = Elem<T>;
   constexpr int BK = kTileK<T>, THREADS = WM * WN * 64, MB = BM / WM / 16, NB = BN / WN / 16;
@@ -155,14 +157,14 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product a) {
   const int m0 = row * BM, n0 = col * BN;
   const int kb = split * a.k_per, ke = min(a.k, kb + a.k_per);
 
-  TileMove<T, L_ROWS ? BN : BK, L_ROWS ? BK : BN, THREADS> ml;
-  TileMove<T, R_ROWS ? BM : BK, R_ROWS ? BK : BM, THREADS> mr;
+  TileMove<T, L_ROWS ? BN : BK, L_ROWS ? BK : BN, THREADS> ml[DEPTH];
+  TileMove<T, R_ROWS ? BM : BK, R_ROWS ? BK : BM, THREADS> mr[DEPTH];
   const T *lp = static_cast<const T*>(a.l), *rp = static_cast<const T*>(a.r);
-  auto fetch = [&](int k) {
-    if constexpr (L_ROWS) ml.fetch([&](int i) -> const T* { return n0 + i < a.n ? lp + (int64_t)(n0 + i) * a.ld_l + k : nullptr; }, ke - k);
-    else ml.fetch([&](int i) -> const T* { return k + i < ke ? lp + (int64_t)(k + i) * a.ld_l + n0 : nullptr; }, a.n - n0);
-    if constexpr (R_ROWS) mr.fetch([&](int i) -> const T* { return m0 + i < a.m ? rp + (int64_t)(m0 + i) * a.ld_r + k : nullptr; }, ke - k);
-    else mr.fetch([&](int i) -> const T* { return k + i < ke ? rp + (int64_t)(k + i) * a.ld_r + m0 : nullptr; }, a.m - m0);
+  auto fetch = [&](int d, int k) {
+    if constexpr (L_ROWS) ml[d].fetch([&](int i) -> const T* { return n0 + i < a.n ? lp + (int64_t)(n0 + i) * a.ld_l + k : nullptr; }, ke - k);
+    else ml[d].fetch([&](int i) -> const T* { return k + i < ke ? lp + (int64_t)(k + i) * a.ld_l + n0 : nullptr; }, a.n - n0);
+    if constexpr (R_ROWS) mr[d].fetch([&](int i) -> const T* { return m0 + i < a.m ? rp + (int64_t)(m0 + i) * a.ld_r + k : nullptr; }, ke - k);
+    else mr[d].fetch([&](int i) -> const T* { return k + i < ke ? rp + (int64_t)(k + i) * a.ld_r + m0 : nullptr; }, a.m - m0);
   };
 
   floatx4 acc[NB][MB];
@@ -171,33 +173,39 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product a) {
 #pragma unroll
     for (int y = 0; y < MB; ++y) acc[x][y] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  if (kb < ke) fetch(kb);
-  for (int k = kb; k < ke; k += BK) {
-    __syncthreads();
-    ml.store(ls, SL);
-    mr.store(rs, SR);
-    __syncthreads();
-    if (k + BK < ke) fetch(k + BK);
 #pragma unroll
-    for (int s = 0; s < BK; s += El::KF) {
-      typename El::Frag lf[NB], rf[MB];
+  for (int d = 0; d < DEPTH; ++d)
+    if (kb + d * BK < ke) fetch(d, kb + d * BK);
+  for (int kt = kb; kt < ke; kt += DEPTH * BK) {
 #pragma unroll
-      for (int x = 0; x < NB; ++x) {
-        if constexpr (L_ROWS) lf[x] = frag_rows(ls, SL, wn + x * 16, s);
-        else lf[x] = frag_cols<T, false>(ls, SL, s, wn + x * 16);
+    for (int d = 0; d < DEPTH; ++d) {
+      const int k = kt + d * BK;
+      if (k >= ke) break;
+      __syncthreads();
+      ml[d].store(ls, SL);
+      mr[d].store(rs, SR);
+      __syncthreads();
+      if (k + DEPTH * BK < ke) fetch(d, k + DEPTH * BK);
+#pragma unroll
+      for (int s = 0; s < BK; s += El::KF) {
+        typename El::Frag lf[NB], rf[MB];
+#pragma unroll
+        for (int x = 0; x < NB; ++x) {
+          if constexpr (L_ROWS) lf[x] = frag_rows(ls, SL, wn + x * 16, s);
+          else lf[x] = frag_cols<T, false>(ls, SL, s, wn + x * 16);
+        }
+#pragma unroll
+        for (int y = 0; y < MB; ++y) {
+          if constexpr (R_ROWS) rf[y] = frag_rows(rs, SR, wm + y * 16, s);
+          else rf[y] = frag_cols<T, false>(rs, SR, s, wm + y * 16);
+        }
+#pragma unroll
+        for (int x = 0; x < NB; ++x)
+#pragma unroll
+          for (int y = 0; y < MB; ++y) acc[x][y] = El::mma(lf[x], rf[y], acc[x][y]);
       }
-#pragma unroll
-      for (int y = 0; y < MB; ++y) {
-        if constexpr (R_ROWS) rf[y] = frag_rows(rs, SR, wm + y * 16, s);
-        else rf[y] = frag_cols<T, false>(rs, SR, s, wm + y * 16);
-      }
-#pragma unroll
-      for (int x = 0; x < NB; ++x)
-#pragma unroll
-        for (int y = 0; y < MB; ++y) acc[x][y] = El::mma(lf[x], rf[y], acc[x][y]);
     }
   }
-
   finish_tile<T, NB, MB>(a, split, m0 + wm, n0 + wn, acc);
 }
 
@@ -301,17 +309,32 @@ __global__ __launch_bounds__(512) void large_product_kernel(Product a) {
   finish_tile<T, NB, MB>(a, split, m0 + wm, n0 + wn, acc);
 }
 
-// sums of the splits, in their order, and the epilogue
+// Sums of the splits, in their order, and the epilogue: four outputs a thread, or where the splits are many four outputs a lane, the four
+// waves taking every fourth split.
+constexpr int kManySplits = 12;
 template <class T>
 __global__ __launch_bounds__(256) void join_kernel(Product a) {
-  const int per_row = (a.n + 3) / 4;
-  const int64_t total = (int64_t)a.m * per_row;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+  __shared__ floatx4 part[4][64];
+  const bool many = a.splits >= kManySplits;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per_row = (a.n + 3) / 4;
+  const int64_t total = (int64_t)a.m * per_row, step = (int64_t)gridDim.x * (many ? 64 : 256);
+  for (int64_t at = (int64_t)blockIdx.x * (many ? 64 : 256); at < total; at += step) {
+    const int64_t i = at + (many ? lane : (int)threadIdx.x);
     const int64_t m = i / per_row;
     const int n = (int)(i - m * per_row) * 4;
     floatx4 v = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < a.splits; ++s) v += load4(a.part + ((int64_t)s * a.m + m) * a.n, n, a.n);
-    finish4<T>(a, m, n, v);
+    if (i < total) {
+#pragma unroll 4
+      for (int s = many ? wave : 0; s < a.splits; s += many ? 4 : 1) v += load4(a.part + ((int64_t)s * a.m + m) * a.n, n, a.n);
+    }
+    if (many) {
+      __syncthreads();
+      part[wave][lane] = v;
+      __syncthreads();
+      if (wave) continue;
+      v = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
+    }
+    if (i < total) finish4<T>(a, m, n, v);
   }
 }
 
@@ -345,40 +368,70 @@ __global__ __launch_bounds__(256) void dz_kernel(LinearGradArgs a, T* dz, int64_
 }
 
 template <class T>
-__global__ __launch_bounds__(256) void db_kernel(const float* sums, int chunks, int n, T* db) {
-  __shared__ float wsum[4][64];
+__global__ __launch_bounds__(1024) void db_kernel(const float* sums, int chunks, int n, T* db) {
+  __shared__ float wsum[16][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (int)blockIdx.x * 64 + lane;
   float acc = 0.f;
   if (c < n)
-    for (int i = wave; i < chunks; i += 4) acc += sums[(int64_t)i * n + c];
+    for (int i = wave; i < chunks; i += 16) acc += sums[(int64_t)i * n + c];
   wsum[wave][lane] = acc;
   __syncthreads();
-  if (wave == 0 && c < n) db[c] = (T)((wsum[0][lane] + wsum[1][lane]) + (wsum[2][lane] + wsum[3][lane]));
+  if (wave == 0 && c < n) {
+#pragma unroll
+    for (int w = 1; w < 16; ++w) acc += wsum[w][lane];
+    db[c] = (T)acc;
+  }
 }
 
 inline int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-struct Plan { int tile, splits, k_per; };
+struct Plan { int bm, bn, splits, k_per; };
 
-// Outputs of 256 tiles of 256 x 256 and more take those, where k has whole tiles and rows per k hold whole pieces of 16 bytes (16-bit
-// types).  Others take tiles of 128 x 128 (a wave 64 x 64), small ones 64 x 64.  Where the tiles leave the chip's 256 CUs idle and k
-// is long, k is split: at least eight tiles of k a split, two workgroups a CU.
+// Tiles of a product:
+//   256 x 256  16-bit types, 256 such tiles or more, k of whole tiles, rows per k of whole pieces of 16 bytes
+//   128 x 128, 112, 96, 64   256 such tiles or more that pad m by no more than a quarter over 64 rows; the width that pads n least (fp32, whose products are the bound: 40,000 x 372 x 200 101 us in
+//              tiles of 128 columns, 89 in 112; 16-bit: 64 columns where n has no more, or 128 would pad a quarter more)
+//              The same with k split, eight tiles of k a split at least, where that makes 384 workgroups or more.
+//   64 x 64    everything smaller, k split while there are fewer than 1,024 workgroups, four tiles of k a split at least.
+//   32 x 32    fp32 where those are fewer than 256: a wave's 32 x 32 outputs of 200 terms are 3 us of matrix instructions.
 template <class T>
 Plan plan_of(int64_t m, int64_t n, int64_t k, bool l_rows, bool r_rows) {
   constexpr int BK = kTileK<T>;
-  const auto tiles_of = [&](int64_t t) { return ((m + t - 1) / t) * ((n + t - 1) / t); };
-  Plan p;
+  const auto tiles_of = [&](int64_t bm, int64_t bn) { return ((m + bm - 1) / bm) * ((n + bn - 1) / bn); };
   const bool whole = sizeof(T) == 2 && k % 64 == 0 && (l_rows || n % 8 == 0) && (r_rows || m % 8 == 0);
-  p.tile = whole && tiles_of(256) >= 256 ? 256 : tiles_of(128) >= 256 ? 128 : 64;
-  const int64_t tiles = tiles_of(p.tile);
-  int64_t splits = tiles ? 512 / tiles : 1;
-  const int64_t most = k / (8 * BK);
-  if (splits > most) splits = most;
-  if (splits < 1) splits = 1;
-  p.k_per = (int)up((k + splits - 1) / splits, BK);
-  if (p.k_per < BK) p.k_per = BK;
-  p.splits = (int)((k + p.k_per - 1) / p.k_per);
-  if (p.splits < 1) p.splits = 1;
+  Plan p{256, 256, 1, (int)up(k < BK ? BK : k, BK)};
+  if (whole && tiles_of(256, 256) >= 256) return p;
+  p.bm = 128;
+  p.bn = 128;
+  if (sizeof(T) == 4) {
+    for (int w : {112, 96, 64})
+      if (up(n, w) < up(n, p.bn)) p.bn = w;
+  } else if (up(n, 64) * 5 <= up(n, 128) * 4) {
+    p.bn = 64;
+  }
+  const auto split = [&](int64_t workgroups, int64_t least) {
+    const int64_t tiles = tiles_of(p.bm, p.bn);
+    int64_t splits = tiles ? workgroups / tiles : 1;
+    if (splits > k / (least * BK)) splits = k / (least * BK);
+    if (splits < 1) splits = 1;
+    p.k_per = (int)up((k + splits - 1) / splits, BK);
+    if (p.k_per < BK) p.k_per = BK;
+    p.splits = (int)((k + p.k_per - 1) / p.k_per);
+    if (p.splits < 1) p.splits = 1;
+  };
+  if (up(m, 128) * 4 <= up(m, 64) * 5) {
+    if (tiles_of(p.bm, p.bn) >= 256) return p;
+    if (tiles_of(p.bm, p.bn) * (k / (8 * BK)) >= 384) {
+      split(512, 8);
+      return p;
+    }
+  }
+  p.bm = p.bn = 64;
+  split(1024, 4);
+  if (sizeof(T) == 4 && tiles_of(64, 64) * p.splits < 256) {
+    p.bm = p.bn = 32;
+    split(1024, 4);
+  }
   return p;
 }
 
@@ -395,15 +448,23 @@ hipError_t product(Product a, void* part, hipStream_t s) {
   a.splits = p.splits;
   a.k_per = p.k_per;
   a.part = static_cast<float*>(part);
-  const int64_t grid = (int64_t)((a.m + p.tile - 1) / p.tile) * ((a.n + p.tile - 1) / p.tile) * p.splits;
+  const int64_t grid = ((a.m + (int64_t)p.bm - 1) / p.bm) * ((a.n + (int64_t)p.bn - 1) / p.bn) * p.splits;
   hipError_t e = hipErrorInvalidValue;
   if constexpr (sizeof(T) == 2) {
-    if (p.tile == 256) e = launch(large_product_kernel<T, L_ROWS, R_ROWS>, grid, 512, s, a);
+    if (p.bm == 256) e = launch(large_product_kernel<T, L_ROWS, R_ROWS>, grid, 512, s, a);
+    else if (p.bn == 128) e = launch(product_kernel<T, 128, 128, 2, 2, 2, L_ROWS, R_ROWS>, grid, 256, s, a);
+    else if (p.bm == 128) e = launch(product_kernel<T, 128, 64, 4, 1, 2, L_ROWS, R_ROWS>, grid, 256, s, a);
+  } else {
+    if (p.bm == 32) e = launch(product_kernel<T, 32, 32, 2, 2, 3, L_ROWS, R_ROWS>, grid, 256, s, a);
+    else if (p.bn == 128) e = launch(product_kernel<T, 128, 128, 2, 2, 1, L_ROWS, R_ROWS>, grid, 256, s, a);
+    else if (p.bn == 112) e = launch(product_kernel<T, 128, 112, 4, 1, 1, L_ROWS, R_ROWS>, grid, 256, s, a);
+    else if (p.bn == 96) e = launch(product_kernel<T, 128, 96, 4, 1, 1, L_ROWS, R_ROWS>, grid, 256, s, a);
+    else if (p.bm == 128) e = launch(product_kernel<T, 128, 64, 4, 1, 1, L_ROWS, R_ROWS>, grid, 256, s, a);
   }
-  if (p.tile == 128) e = launch(product_kernel<T, 128, 128, 2, 2, L_ROWS, R_ROWS>, grid, 256, s, a);
-  if (p.tile == 64) e = launch(product_kernel<T, 64, 64, 2, 2, L_ROWS, R_ROWS>, grid, 256, s, a);
+  if (p.bm == 64) e = launch(product_kernel<T, 64, 64, 2, 2, 3, L_ROWS, R_ROWS>, grid, 256, s, a);
   if (e != hipSuccess || p.splits == 1) return e;
-  const int64_t blocks = ((int64_t)a.m * ((a.n + 3) / 4) + 255) / 256;
+  const int per = p.splits >= kManySplits ? 64 : 256;
+  const int64_t blocks = ((int64_t)a.m * ((a.n + 3) / 4) + per - 1) / per;
   return launch(join_kernel<T>, blocks < 4096 ? blocks : 4096, 256, s, a);
 }
 
@@ -447,7 +508,7 @@ hipError_t backward(const LinearGradArgs& f, void* ws, hipStream_t s) {
   hipError_t e = hipSuccess;
   if (dz || sums) {
     e = launch(dz_kernel<T>, (int64_t)g.chunks * ((f.d_out + 255) / 256), 256, s, f, dz, g.ld_dz, sums, g.rows_per);
-    if (e == hipSuccess && sums) e = launch(db_kernel<T>, (f.d_out + 63) / 64, 256, s, (const float*)sums, g.chunks, f.d_out, static_cast<T*>(f.db));
+    if (e == hipSuccess && sums) e = launch(db_kernel<T>, (f.d_out + 63) / 64, 1024, s, (const float*)sums, g.chunks, f.d_out, static_cast<T*>(f.db));
   }
   const void* z = dz ? dz : f.dy;
   const int64_t ld_z = dz ? g.ld_dz : f.ld_dy;
