@@ -205,6 +205,17 @@ int stgn_maintain(stgn_ctx *ctx, double delta_max, double alpha, int *action, ui
  * w: host [2 * d_emb], source half first; copied.  May be called again at any time. */
 int stgn_set_predictor(stgn_ctx *ctx, const float *w, float b);
 
+/* A head with one hidden layer instead (what temporal graph networks are commonly trained with):
+ *     y = act([h_u | h_v] . w1 + b1) . w2 + b2.
+ * hidden: 1 .. STGN_MAX_HIDDEN; activation: STGN_ACT_*; w1: host [2 * d_emb x hidden], b1, w2: host [hidden]; copied.  The head's
+ * parameters and the rows of a batch lie in a workspace of the caller's on the context's device, 256-byte aligned, of the size
+ * stgn_predictor_mlp_workspace tells; it must outlive every prediction until the next stgn_set_predictor or stgn_set_predictor_mlp call, or
+ * the context.  The last head set is the one that scores.  May be called again at any time; synchronises the stream. */
+#define STGN_MAX_HIDDEN 4096
+int stgn_predictor_mlp_workspace(stgn_ctx *ctx, uint32_t hidden, size_t *device_bytes);
+int stgn_set_predictor_mlp(stgn_ctx *ctx, uint32_t hidden, uint32_t activation, const float *w1, const float *b1,
+                           const float *w2, float b2, void *device_workspace, size_t device_bytes);
+
 /* Per-batch root-node inference (Algorithm 1: embed, predict, THEN update; Sec. 3.6.2,
  * Eq. parallel_embed): link scores of n edges (u_i, v_i, t_i) that have NOT been ingested yet,
  * from the current (pre-batch) state.  Call it before stgn_ingest_batch of the same edges.
@@ -214,7 +225,7 @@ int stgn_set_predictor(stgn_ctx *ctx, const float *w, float b);
  *       gaps t_i - t_j to the root's recent neighbours, query side phi(0)); the layers below are
  *       the cached rows.  With one layer this is Eq. parallel_embed evaluated at t_i.
  * src, dst, ts, scores: [n], all on the host (inputs_on_device = 0; synchronises) or all on the
- * device (1; asynchronous on hip_stream).  n <= max_batch.  Needs stgn_set_predictor.  Host
+ * device (1; asynchronous on hip_stream).  n <= max_batch.  Needs stgn_set_predictor or stgn_set_predictor_mlp.  Host
  * inputs with an id >= num_nodes return STGN_E_NODE_OUT_OF_RANGE; device inputs give that edge
  * the score NaN.  scores may lie over ts, or begin where src or dst begins.  Changes no state. */
 int stgn_predict_batch(stgn_ctx *ctx, uint32_t n, const uint32_t *src, const uint32_t *dst,

@@ -80,7 +80,8 @@ EXPORTS = ("stgn_query_workspace", "stgn_create", "stgn_destroy", "stgn_ingest_b
            "stgn_get_memory", "stgn_get_totals", "stgn_kernel_times", "stgn_last_error", "stgn_version",
            "stgn_set_predictor", "stgn_predict_batch", "stgn_predict_batch_static", "stgn_drift_status",
            "stgn_maintain", "stgn_probe_gather", "stgn_linear_workspace", "stgn_linear", "stgn_linear_grad",
-           "stgn_attention_workspace", "stgn_attention", "stgn_attention_grad")
+           "stgn_attention_workspace", "stgn_attention", "stgn_attention_grad", "stgn_predictor_mlp_workspace",
+           "stgn_set_predictor_mlp")
 
 
 def load_library():
@@ -109,6 +110,8 @@ def load_library():
     L.stgn_kernel_times.argtypes = [vp, C.c_int, C.c_int, C.c_uint32, C.POINTER(C.c_char_p), _f64p,
                                     C.POINTER(C.c_uint64)]
     L.stgn_set_predictor.argtypes = [vp, vp, C.c_float]
+    L.stgn_predictor_mlp_workspace.argtypes = [vp, C.c_uint32, C.POINTER(C.c_size_t)]
+    L.stgn_set_predictor_mlp.argtypes = [vp, C.c_uint32, C.c_uint32, vp, vp, vp, C.c_float, vp, C.c_size_t]
     L.stgn_predict_batch.argtypes = [vp, C.c_uint32, vp, vp, vp, C.c_int, C.c_int, vp]
     L.stgn_predict_batch_static.argtypes = [vp, C.c_uint32, vp, vp, vp, C.c_int, vp]
     L.stgn_drift_status.argtypes = [vp, C.POINTER(C.c_double), _u32p, vp]
@@ -371,7 +374,7 @@ class StreamTGN:
         if getattr(self, "_h", None):
             self._L.stgn_destroy(self._h)
             self._h = None
-            self._ws = None
+            self._ws = self._head_ws = None
 
     def __del__(self):
         try:
@@ -428,6 +431,18 @@ class StreamTGN:
         w = np.ascontiguousarray(w, dtype=np.float32)
         assert w.shape == (2 * self.cfg.d_emb,)
         self._check(self._L.stgn_set_predictor(self._h, _ptr(w), float(b)))
+
+    def set_predictor_mlp(self, w1, b1, w2, b2, activation="relu"):
+        """The head act([h_u | h_v] w1 + b1) . w2 + b2: w1 [2 d_emb, hidden], b1 and w2 [hidden]; activation as in linear."""
+        w1, b1, w2 = (np.ascontiguousarray(a, dtype=np.float32) for a in (w1, b1, w2))
+        hidden = w1.shape[1]
+        assert w1.shape == (2 * self.cfg.d_emb, hidden) and b1.shape == (hidden,) and w2.shape == (hidden,)
+        n = C.c_size_t(0)
+        self._check(self._L.stgn_predictor_mlp_workspace(self._h, hidden, C.byref(n)))
+        ws = self._torch.empty(n.value + 256, dtype=self._torch.uint8, device=self.device)
+        self._check(self._L.stgn_set_predictor_mlp(self._h, hidden, ACTIVATIONS[activation], _ptr(w1), _ptr(b1), _ptr(w2), float(b2),
+                                                   C.c_void_p((ws.data_ptr() + 255) & ~255), n.value))
+        self._head_ws = ws
 
     def predict_batch(self, src, dst, ts, at_edge_time=False):
         """Link scores of edges that have not been ingested yet: numpy in, numpy out (synchronises), or

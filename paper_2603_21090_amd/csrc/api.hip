@@ -1,5 +1,6 @@
 // extern "C" boundary and host orchestration: argument checks, workspace layout, parameter
 // packing, launch order of one incremental step.  No arithmetic of the method runs here.
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -46,7 +47,9 @@ struct stgn_ctx {
   int parity = 0;                   // staging block and dirty-flag array of the next batch
   int last_par = 0;                 // state set of the batch enqueued last
   bool idle = true;                 // nothing was enqueued since the library last synchronised `stream`
-  bool have_predictor = false;      // stgn_set_predictor was called
+  bool have_predictor = false;      // stgn_set_predictor or stgn_set_predictor_mlp was called
+  // the head with a hidden layer, in the caller's workspace (hidden = 0: the linear head)
+  struct Mlp { uint32_t hidden = 0; int activation = 0; float *w1, *b1, *w2, *b2, *pairs, *hid; void* ws; } mlp;
   std::string err;
   uint64_t host_edges = 0;          // upper bound of edges enqueued so far
   bool host_t_known = true;         // host knows the last ingested timestamp
@@ -852,6 +855,72 @@ int stgn_maintain(stgn_ctx* ctx, double delta_max, double alpha, int* action, ui
   return STGN_OK;
 }
 
+// The head's parameters, the pairs and hidden rows of max_batch edges, and what its two products need for any smaller batch.
+static size_t mlp_layout(const stgn_config& c, uint32_t hidden, char* base, stgn_ctx::Mlp* m) {
+  Bump b{base};
+  const size_t d2 = 2 * (size_t)c.d_emb, n = c.max_batch;
+  m->w1 = b.take<float>(d2 * hidden); m->b1 = b.take<float>(hidden); m->w2 = b.take<float>(hidden); m->b2 = b.take<float>(1);
+  m->pairs = b.take<float>(n * d2); m->hid = b.take<float>(n * hidden);
+  size_t most = 0;
+  for (uint32_t i = 1; i <= c.max_batch; ++i) {
+    LinearArgs a{};
+    a.rows = (int)i; a.d_in = (int)d2; a.d_out = (int)hidden;
+    most = std::max(most, linear_bytes(a, STGN_F32));
+    a.d_in = (int)hidden; a.d_out = 1;
+    most = std::max(most, linear_bytes(a, STGN_F32));
+  }
+  m->ws = b.take<char>(most);
+  return (b.off + 255) & ~(size_t)255;
+}
+
+// scores of n pairs: two dense products
+static hipError_t mlp_scores(const stgn_ctx* ctx, uint32_t n, float* scores) {
+  const stgn_ctx::Mlp& m = ctx->mlp;
+  LinearArgs a{};
+  a.x = m.pairs; a.w = m.w1; a.bias = m.b1; a.y = m.hid; a.act = m.activation;
+  a.rows = (int)n; a.d_in = (int)(2 * ctx->cfg.d_emb); a.d_out = (int)m.hidden;
+  a.ld_x = a.d_in; a.ld_w = a.ld_y = a.d_out;
+  if (const hipError_t e = launch_linear(a, STGN_F32, m.ws, ctx->stream)) return e;
+  LinearArgs b{};
+  b.x = m.hid; b.w = m.w2; b.bias = m.b2; b.y = scores;
+  b.rows = (int)n; b.d_in = (int)m.hidden; b.d_out = 1;
+  b.ld_x = b.d_in; b.ld_w = b.ld_y = 1;
+  return launch_linear(b, STGN_F32, m.ws, ctx->stream);
+}
+
+int stgn_predictor_mlp_workspace(stgn_ctx* ctx, uint32_t hidden, size_t* device_bytes) {
+  if (!ctx) return STGN_E_INVALID_ARG;
+  if (!device_bytes) return fail(ctx, STGN_E_INVALID_ARG, "NULL device_bytes");
+  if (hidden == 0 || hidden > STGN_MAX_HIDDEN) return fail(ctx, STGN_E_INVALID_ARG, "hidden out of range");
+  stgn_ctx::Mlp m;
+  *device_bytes = mlp_layout(ctx->cfg, hidden, nullptr, &m);
+  return STGN_OK;
+}
+
+int stgn_set_predictor_mlp(stgn_ctx* ctx, uint32_t hidden, uint32_t activation, const float* w1, const float* b1, const float* w2, float b2,
+                           void* device_workspace, size_t device_bytes) {
+  if (!ctx) return STGN_E_INVALID_ARG;
+  if (hidden == 0 || hidden > STGN_MAX_HIDDEN) return fail(ctx, STGN_E_INVALID_ARG, "hidden out of range");
+  if (activation > STGN_ACT_SILU) return fail(ctx, STGN_E_INVALID_ARG, "unknown activation");
+  if (!w1 || !b1 || !w2) return fail(ctx, STGN_E_INVALID_ARG, "NULL weights");
+  stgn_ctx::Mlp m;
+  if (!device_workspace || (reinterpret_cast<uintptr_t>(device_workspace) & 255) ||
+      device_bytes < mlp_layout(ctx->cfg, hidden, static_cast<char*>(device_workspace), &m))
+    return fail(ctx, STGN_E_WORKSPACE, "workspace missing, misaligned or too small (stgn_predictor_mlp_workspace)");
+  m.hidden = hidden;
+  m.activation = (int)activation;
+  const size_t d2 = 2 * (size_t)ctx->cfg.d_emb;
+  // ordered after predictions already enqueued, before those that follow
+  HIPCHK(ctx, hipStreamSynchronize(ctx->stream));
+  HIPCHK(ctx, hipMemcpy(m.w1, w1, d2 * hidden * sizeof(float), hipMemcpyHostToDevice));
+  HIPCHK(ctx, hipMemcpy(m.b1, b1, hidden * sizeof(float), hipMemcpyHostToDevice));
+  HIPCHK(ctx, hipMemcpy(m.w2, w2, hidden * sizeof(float), hipMemcpyHostToDevice));
+  HIPCHK(ctx, hipMemcpy(m.b2, &b2, sizeof(float), hipMemcpyHostToDevice));
+  ctx->mlp = m;
+  ctx->have_predictor = true;
+  return STGN_OK;
+}
+
 int stgn_set_predictor(stgn_ctx* ctx, const float* w, float b) {
   if (!ctx) return STGN_E_INVALID_ARG;
   if (!w) return fail(ctx, STGN_E_INVALID_ARG, "NULL weights");
@@ -861,6 +930,7 @@ int stgn_set_predictor(stgn_ctx* ctx, const float* w, float b) {
   // ordered after predictions already enqueued, before those that follow
   HIPCHK(ctx, hipStreamSynchronize(ctx->stream));
   HIPCHK(ctx, hipMemcpy(ctx->d.pred_w, wb.data(), wb.size() * sizeof(float), hipMemcpyHostToDevice));
+  ctx->mlp.hidden = 0;
   ctx->have_predictor = true;
   return STGN_OK;
 }
@@ -874,6 +944,16 @@ static hipError_t times_clear_of_scores(const Dev& d, hipStream_t s, uint32_t n,
   const hipError_t e = hipMemcpyAsync(d.pred_ts, *ts, (size_t)n * sizeof(double), hipMemcpyDefault, s);
   *ts = d.pred_ts;
   return e;
+}
+
+// Scores of n edges on device arrays.  (With a hidden layer the ids and times have been read before the first score is written.)
+static hipError_t launch_scores(stgn_ctx* ctx, uint32_t n, const uint32_t* src, const uint32_t* dst, const double* ts, int at_edge_time,
+                                float* scores) {
+  const bool mlp = ctx->mlp.hidden != 0;
+  if (at_edge_time) launch_layer_scores(ctx->d, ctx->stream, n, src, dst, ts, mlp ? ctx->mlp.pairs : scores, mlp);
+  else if (mlp) launch_pair_rows(ctx->d, ctx->stream, n, src, dst, ctx->mlp.pairs);
+  else launch_predict_head(ctx->d, ctx->stream, n, src, dst, scores);
+  return mlp ? mlp_scores(ctx, n, scores) : hipSuccess;
 }
 
 int stgn_predict_batch(stgn_ctx* ctx, uint32_t n, const uint32_t* src, const uint32_t* dst, const double* ts,
@@ -898,11 +978,10 @@ int stgn_predict_batch(stgn_ctx* ctx, uint32_t n, const uint32_t* src, const uin
     dsrc = d.pred_src; ddst = d.pred_dst; dts = d.pred_ts; dout = d.pred_scores;
   }
   ctx->idle = false;
-  if (at_edge_time) HIPCHK(ctx, times_clear_of_scores(d, s, n, dout, &dts));
+  if (at_edge_time && !ctx->mlp.hidden) HIPCHK(ctx, times_clear_of_scores(d, s, n, dout, &dts));
   {
     Scope t(ctx, KC_PREDICT);
-    if (at_edge_time) launch_layer_scores(d, s, n, dsrc, ddst, dts, dout);
-    else launch_predict_head(d, s, n, dsrc, ddst, dout);
+    HIPCHK(ctx, launch_scores(ctx, n, dsrc, ddst, dts, at_edge_time, dout));
   }
   HIPCHK(ctx, hipGetLastError());
   if (!inputs_on_device) {
@@ -936,9 +1015,8 @@ int stgn_predict_batch_static(stgn_ctx* ctx, uint32_t n, const uint32_t* src, co
   // the same kernels as stgn_predict_batch, on the caller's own arrays
   hipStream_t s = ctx->stream;
   ctx->idle = false;
-  if (at_edge_time) HIPCHK(ctx, times_clear_of_scores(ctx->d, s, n, scores, &ts));
-  if (at_edge_time) launch_layer_scores(ctx->d, s, n, src, dst, ts, scores);
-  else launch_predict_head(ctx->d, s, n, src, dst, scores);
+  if (at_edge_time && !ctx->mlp.hidden) HIPCHK(ctx, times_clear_of_scores(ctx->d, s, n, scores, &ts));
+  HIPCHK(ctx, launch_scores(ctx, n, src, dst, ts, at_edge_time, scores));
   HIPCHK(ctx, hipGetLastError());
   return STGN_OK;
 }

@@ -95,6 +95,23 @@ __global__ __launch_bounds__(256) void predict_head_kernel(Dev d, uint32_t n, co
   }
 }
 
+// pairs [h_u | h_v] of the cached final-layer rows, one wave an edge (NaN where an id is out of range)
+__global__ __launch_bounds__(256) void pair_rows_kernel(Dev d, uint32_t n, const uint32_t* __restrict__ src,
+                                                        const uint32_t* __restrict__ dst, float* __restrict__ pairs) {
+  const uint32_t lane = threadIdx.x & 63u, i = blockIdx.x * 4u + (threadIdx.x >> 6), de = d.d_emb;
+  if (i >= n) return;
+  const uint32_t u = src[i], v = dst[i];
+  const bool ok = u < d.N && v < d.N;
+  const Table HL = d.H[d.layers];
+  const float* hu = HL.base + (size_t)(ok ? u : 0u) * HL.ld;
+  const float* hv = HL.base + (size_t)(ok ? v : 0u) * HL.ld;
+  float* pair = pairs + (size_t)i * 2u * de;
+  for (uint32_t c = lane; c < de; c += 64) {
+    pair[c] = ok ? hu[c] : __builtin_nanf("");
+    pair[de + c] = ok ? hv[c] : __builtin_nanf("");
+  }
+}
+
 LaunchArgs make_args(const Dev& d, uint32_t layer) {
   const LayerDev& L = d.L[layer];
   LaunchArgs a{};
@@ -160,19 +177,23 @@ void launch_layer(const Dev& d, hipStream_t s, uint32_t layer, const uint32_t* r
   go_heads(a);
 }
 
-// link scores of n edges at their own times: the final layer for the 2 n roots
+// link scores of n edges at their own times, or with `pairs` their rows [h_u | h_v]: the final layer for the 2 n roots
 void launch_layer_scores(const Dev& d, hipStream_t s, uint32_t n, const uint32_t* src, const uint32_t* dst, const double* ts,
-                         float* scores) {
+                         float* scores, bool pairs) {
   LaunchArgs a = make_args(d, d.layers - 1);
   a.roots = true;                                             // (at their own times; q and qt, which do not depend on the time, are read back where a query cache is kept)
   a.k.root_src = src; a.k.root_dst = dst; a.k.root_ts = ts; a.k.nodes = d.N;
-  a.k.head = d.pred_w; a.k.scores = scores;
+  a.k.head = pairs ? nullptr : d.pred_w; a.k.scores = scores;
   a.s = s; a.rows = nullptr; a.cp = nullptr; a.cm = 2 * n; a.set_attr = false;
   go_heads(a);
 }
 
 void launch_predict_head(const Dev& d, hipStream_t s, uint32_t n, const uint32_t* src, const uint32_t* dst, float* scores) {
   hipLaunchKernelGGL(predict_head_kernel, dim3((n + 3) / 4), dim3(256), 0, s, d, n, src, dst, scores);
+}
+
+void launch_pair_rows(const Dev& d, hipStream_t s, uint32_t n, const uint32_t* src, const uint32_t* dst, float* pairs) {
+  hipLaunchKernelGGL(pair_rows_kernel, dim3((n + 3) / 4), dim3(256), 0, s, d, n, src, dst, pairs);
 }
 
 hipError_t launch_gather_rows(const Dev& d, hipStream_t s, uint32_t layer, uint32_t n, const uint32_t* nodes, float* out) {

@@ -135,7 +135,8 @@ struct LayerArgs {
   // root-node inference (read by the ROOTS variants only): list row r is the source (r even) or destination (r odd) of edge
   // r / 2, queried at the edge's time instead of the node's last-interaction time; an id past `nodes` is a dead
   // row.  The rows are not stored: their tile holds both ends of its eight edges, and the link score
-  // y = h_u . head[0 : d) + h_v . head[d : 2d) + head[2d] leaves the kernel in their place (NaN with a dead end).
+  // y = h_u . head[0 : d) + h_v . head[d : 2d) + head[2d] leaves the kernel in their place (NaN with a dead end).  With another
+  // head (`head` null) the pairs [h_u | h_v] leave it instead, 2 d_emb floats an edge at `scores` (NaN with a dead end).
   // One launch for what took three (roots listed, rows stored, rows read back by the head): 4,000 candidates on
   // 100,000 nodes 35.1 -> 29.9 us, 28.1 with variants of their own (ROOTS), 25.2 with a lane group per key slot.
   const uint32_t *root_src, *root_dst; const double* root_ts; uint32_t nodes;
@@ -1266,9 +1267,19 @@ void layer_body(const LayerArgs& a, const uint32_t* __restrict__ rows, const uin
         const float* hu = Hs + 2u * e * ldh;
         const float* hv = hu + ldh;
         float acc = 0.0f;
+        const bool ok = nodes_s[2u * e] != 0xFFFFFFFFu && nodes_s[2u * e + 1u] != 0xFFFFFFFFu;
+        if (a.head == nullptr) {
+          if (2u * i < n) {
+            float* pair = a.scores + (size_t)i * 2u * a.d_emb;
+            for (uint32_t c = lane; c < a.d_emb; c += 64) {
+              pair[c] = ok ? hu[c] : __builtin_nanf("");
+              pair[a.d_emb + c] = ok ? hv[c] : __builtin_nanf("");
+            }
+          }
+          continue;
+        }
         for (uint32_t c = lane; c < a.d_emb; c += 64) acc = fmaf(hu[c], a.head[c], fmaf(hv[c], a.head[a.d_emb + c], acc));
         for (int off = 32; off > 0; off >>= 1) acc += __shfl_xor(acc, off);
-        const bool ok = nodes_s[2u * e] != 0xFFFFFFFFu && nodes_s[2u * e + 1u] != 0xFFFFFFFFu;
         if (lane == 0 && 2u * i < n) a.scores[i] = ok ? acc + a.head[2u * a.d_emb] : __builtin_nanf("");
       }
     }

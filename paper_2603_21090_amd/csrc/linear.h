@@ -43,7 +43,7 @@ __device__ inline float logistic(float z) {
 
 template <class T, int ACT>
 __device__ inline float act_value(float z) {
-  if constexpr (ACT == ACT_RELU) return z > 0.f ? z : 0.f;
+  if constexpr (ACT == ACT_RELU) return z < 0.f ? 0.f : z;         // (a NaN stays one)
   if constexpr (ACT == ACT_GELU) {
     float share, bell;
     normal_share<T>(z, share, bell);
@@ -452,7 +452,7 @@ hipError_t product(Product a, void* part, hipStream_t s) {
   hipError_t e = hipErrorInvalidValue;
   if constexpr (sizeof(T) == 2) {
     if (p.bm == 256) e = launch(large_product_kernel<T, L_ROWS, R_ROWS>, grid, 512, s, a);
-    else if (p.bn == 128) e = launch(product_kernel<T, 128, 128, 2, 2, 2, L_ROWS, R_ROWS>, grid, 256, s, a);
+    else if (p.bn == 128) e = launch(product_kernel<T, 128, 128, 2, 2, 1, L_ROWS, R_ROWS>, grid, 256, s, a);
     else if (p.bm == 128) e = launch(product_kernel<T, 128, 64, 4, 1, 2, L_ROWS, R_ROWS>, grid, 256, s, a);
   } else {
     if (p.bm == 32) e = launch(product_kernel<T, 32, 32, 2, 2, 3, L_ROWS, R_ROWS>, grid, 256, s, a);

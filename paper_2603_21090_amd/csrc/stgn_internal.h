@@ -303,7 +303,8 @@ void launch_gather_times(const Dev& d, hipStream_t s, uint32_t n, const uint32_t
 // link scores of n edges: at their own times (the final layer for their 2n ends, scores out of the same launch), or from
 // the cached final-layer rows
 void launch_layer_scores(const Dev& d, hipStream_t s, uint32_t n, const uint32_t* src, const uint32_t* dst, const double* ts,
-                         float* scores);
+                         float* scores, bool pairs);
+void launch_pair_rows(const Dev& d, hipStream_t s, uint32_t n, const uint32_t* src, const uint32_t* dst, float* pairs);
 void launch_predict_head(const Dev& d, hipStream_t s, uint32_t n, const uint32_t* src, const uint32_t* dst, float* scores);
 void launch_init_state(const Dev& d, hipStream_t s);
 void launch_zero(float* p, size_t n, hipStream_t s);
