@@ -83,17 +83,20 @@ template <class T, int DP, int NB, class Row>
 __device__ inline void load_cols(typename Elem<T>::Frag (&f)[NB][DP / Elem<T>::KF], Row row, int d, uint32_t flip = 0) {
   constexpr int KF = Elem<T>::KF, E = Elem<T>::E;
   const int g = (threadIdx.x & 63) >> 4;
+  by_end(row_end<T>(d), [&](auto e) {
 #pragma unroll
-  for (int c = 0; c < NB; ++c) {
-    const T* p = row(c);
+    for (int c = 0; c < NB; ++c) {
+      const T* p = row(c);
 #pragma unroll
-    for (int k = 0; k < DP / KF; ++k) {
-      const int at = k * KF + E * g;
-      u32x4 v = p != nullptr ? load16(p + at, d - at) : u32x4{0, 0, 0, 0};
-      if (flip) v ^= flip;
-      f[c][k] = __builtin_bit_cast(typename Elem<T>::Frag, v);
+      for (int k = 0; k < DP / KF; ++k) {
+        const int at = k * KF + E * g;
+        u32x4 v = {0, 0, 0, 0};
+        if (p != nullptr && at < d) v = load16<T, decltype(e)::value>(p + at, d - at);
+        if (flip) v ^= flip;
+        f[c][k] = __builtin_bit_cast(typename Elem<T>::Frag, v);
+      }
     }
-  }
+  });
 }
 
 __device__ inline float over_groups_max(float x) {
@@ -194,11 +197,12 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void forward_kernel(A
   StreamMove<T, BK, DP, WAVES * 64> mk, mv;
   int kt = k0 / 16 * 16, buf = 0;
   run_of(at.run, runs, BK, kt, k1);
-  mk.start(row_of<T>(a.k, a.sk, b, kt, hk), a.sk.row, a.d);
-  mv.start(row_of<T>(a.v, a.sv, b, kt, hk), a.sv.row, a.d);
+  const RowEnd end = row_end<T>(a.d);
+  mk.start_rows(row_of<T>(a.k, a.sk, b, kt, hk), a.sk.row, a.d);
+  mv.start_rows(row_of<T>(a.v, a.sv, b, kt, hk), a.sv.row, a.d);
   if (kt < k1) {
-    mk.fetch(l.kn - kt);
-    mv.fetch(l.kn - kt);
+    mk.fetch(l.kn - kt, end);
+    mv.fetch(l.kn - kt, end);
     mk.store(ks[0]);
     mv.store(vs[0]);
   }
@@ -206,8 +210,8 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void forward_kernel(A
     __syncthreads();                                          // this tile is there, and nobody reads the other buffer any more
     const bool more = kt + BK < k1;
     if (more) {
-      mk.fetch(l.kn - kt - BK);
-      mv.fetch(l.kn - kt - BK);
+      mk.fetch(l.kn - kt - BK, end);
+      mv.fetch(l.kn - kt - BK, end);
     }
     if (kt < w1 && kt + BK > w0) {
       floatx4 s[KB][NB];
@@ -358,11 +362,12 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void query_grad_kerne
   int kt = k0 / 16 * 16, buf = 0;
   const bool one_tile = sizeof(T) == 2 && kt < k1 && k1 - kt <= BK;
   run_of(pos.run, runs, BK, kt, k1);
-  mk.start(row_of<T>(a.k, a.sk, b, kt, hk), a.sk.row, a.d);
-  mv.start(row_of<T>(a.v, a.sv, b, kt, hk), a.sv.row, a.d);
+  const RowEnd end = row_end<T>(a.d);
+  mk.start_rows(row_of<T>(a.k, a.sk, b, kt, hk), a.sk.row, a.d);
+  mv.start_rows(row_of<T>(a.v, a.sv, b, kt, hk), a.sv.row, a.d);
   if (kt < k1) {
-    mk.fetch(l.kn - kt);
-    mv.fetch(l.kn - kt);
+    mk.fetch(l.kn - kt, end);
+    mv.fetch(l.kn - kt, end);
     mk.store(ks[0]);
     mv.store(vs[0]);
   }
@@ -379,7 +384,7 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void query_grad_kerne
 #pragma unroll
     for (int k = 0; k < DP / El::KF; ++k) {
       const int from = k * El::KF + El::E * g;
-      const typename El::Frag f = __builtin_bit_cast(typename El::Frag, any ? load16(o + from, a.d - from) : u32x4{0, 0, 0, 0});
+      const typename El::Frag f = __builtin_bit_cast(typename El::Frag, any && from < a.d ? load16(o + from, a.d - from, end) : u32x4{0, 0, 0, 0});
 #pragma unroll
       for (int e = 0; e < El::E; ++e) sum = fmaf((float)df[c][k][e], (float)f[e], sum);
     }
@@ -448,8 +453,8 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void query_grad_kerne
     __syncthreads();
     const bool more = kt + BK < k1;
     if (more) {
-      mk.fetch(l.kn - kt - BK);
-      mv.fetch(l.kn - kt - BK);
+      mk.fetch(l.kn - kt - BK, end);
+      mv.fetch(l.kn - kt - BK, end);
     }
     if (kt < w1 && kt + BK > w0) {
       const bool partial = kt < all0 || kt + BK > all1;
@@ -494,25 +499,34 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void query_grad_kerne
   }
 }
 
-// Rows (query, head) of one list and key head on their way into LDS.  A tile holds whole queries where the heads that share a key
-// head divide it: then a thread's pieces keep their heads and advance by a tile's queries.  Other numbers of heads take a division a piece.
+// Rows (query, head) of one list and key head on their way into LDS.  Where the heads that share a key head divide the rows between a
+// thread's pieces, its pieces keep their heads and advance by a tile's queries.  Other numbers of heads take a division a piece.
 template <class T, int BQ, int DP, int THREADS>
-struct RowMove {
-  static constexpr int E = Elem<T>::E, PER_ROW = DP / E, NP = BQ * PER_ROW / THREADS, APART = THREADS / PER_ROW;
-  u32x4 r[NP];
-  __device__ inline void fetch(const AttnArgs& a, const void* base, const Strides& st, int b, int hk, int rt, int r1) {
-    const int t = (int)threadIdx.x, c = t % PER_ROW * E, count = a.d - c;
+struct RowMove : StreamMove<T, BQ, DP, THREADS> {
+  using Base = StreamMove<T, BQ, DP, THREADS>;
+  static __device__ inline bool steady(const AttnArgs& a) { return a.group_shift >= 0 && a.group <= Base::APART; }
+  __device__ inline void start_queries(const AttnArgs& a, const void* base, const Strides& st, int b, int hk, int rt) {
+    if (!steady(a)) return;                                   // (rt: the first row of a query)
+    const int row = rt + (int)threadIdx.x / Base::PER_ROW, q = row >> a.group_shift;
+    this->start(row_of<T>(base, st, b, q, hk * a.group + row - (q << a.group_shift)), (int64_t)(Base::APART >> a.group_shift) * st.row,
+                (int64_t)(BQ >> a.group_shift) * st.row, a.d);
+  }
+  __device__ inline void fetch_queries(const AttnArgs& a, const void* base, const Strides& st, int b, int hk, int rt, int r1, RowEnd end) {
+    if (steady(a)) {
+      this->fetch(r1 - rt, end);
+      return;
+    }
+    const int c = (int)threadIdx.x % Base::PER_ROW * Base::E, count = a.d - c;
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int row = rt + t / PER_ROW + i * APART;
-      r[i] = u32x4{0, 0, 0, 0};
+    for (int i = 0; i < Base::NP; ++i) {
+      const int row = rt + (int)threadIdx.x / Base::PER_ROW + i * Base::APART;
+      this->r[i] = u32x4{0, 0, 0, 0};
       if (count > 0 && row < r1) {
-        const int q = a.group_shift >= 0 ? row >> a.group_shift : query_of(a, row);
-        r[i] = load16(row_of<T>(base, st, b, q, hk * a.group + row - q * a.group) + c, count);
+        const int q = query_of(a, row);
+        this->r[i] = load16(row_of<T>(base, st, b, q, hk * a.group + row - q * a.group) + c, count, end);
       }
     }
   }
-  __device__ inline void store(T* tile) const { store_placed<T, BQ, DP, THREADS>(tile, r); }
 };
 
 // dk, dv: keys and values in registers, queries and dout stream
@@ -560,9 +574,12 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void key_grad_kernel(AttnArgs a, i
   int mlo = 0, mhi = 0;
   int rt = q0 * a.group, r1 = q1 * a.group, buf = 0;
   run_of(pos.run, runs, BQ, rt, r1);
+  const RowEnd end = row_end<T>(a.d);
+  mq.start_queries(a, a.q, a.sq, b, hk, rt);
+  md.start_queries(a, a.dout, a.sdo, b, hk, rt);
   auto fetch = [&](int rt) {
-    mq.fetch(a, a.q, a.sq, b, hk, rt, r1);
-    md.fetch(a, a.dout, a.sdo, b, hk, rt, r1);
+    mq.fetch_queries(a, a.q, a.sq, b, hk, rt, r1, end);
+    md.fetch_queries(a, a.dout, a.sdo, b, hk, rt, r1, end);
     if ((int)threadIdx.x < BQ) {
       const int r = rt + (int)threadIdx.x, i = query_of(a, r), head = hk * a.group + r - i * a.group;
       ml = INFINITY;                                          // a row that sees nothing has no probability
@@ -592,6 +609,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void key_grad_kernel(AttnArgs a, i
     const T *qt = qs[buf], *gt = gs[buf];
 #pragma unroll
     for (int y = 0; y < BQ / 16; y += PB) {
+      if (rt + y * 16 >= r1) break;                           // (the last tile's rows behind the end)
       floatx4 s[PB][NB], dp[PB][NB];
 #pragma unroll
       for (int u = 0; u < PB; ++u) {
@@ -760,12 +778,14 @@ hipError_t sum_runs(const AttnArgs& a, void* out, void* second, int len, int gro
 }
 
 // How many rows or keys a workgroup takes.  16-bit types: 128 queries, four waves of 32; the dk/dv kernel keeps twice the operands and
-// sums a wave, so eight waves of 16 keys (four of 32 in 479 registers, one wave a SIMD: 1,323 us where these take 874; four of 32 with the values
+// sums a wave, so eight waves of 16 keys (four of 32 in 479 registers, one wave a SIMD: 1,323 us where these take 880; four of 32 with the values
 // in LDS: as long as these).  fp32: 64, four waves
 // of 16.
 template <class T, int DP>
 struct Shape {
   static constexpr int NB = sizeof(T) == 4 || DP > 128 ? 1 : 2, BQ = stream_rows<T, DP>();
+  // rows between two barriers: twice as many where one workgroup has the CU to itself and its waves wait for each other (880 -> 845 us)
+  static constexpr int KBQ = sizeof(T) == 2 && DP == 128 ? 128 : BQ;
   static constexpr int KW = sizeof(T) == 2 && DP <= 128 ? 8 : 4, OCC = DP <= 128 ? 2 : 1;
   static int64_t query_tiles(const AttnArgs& a) { return ((int64_t)a.q_len * a.group + 64 * NB - 1) / (64 * NB); }
   static int64_t key_tiles(const AttnArgs& a) { return ((int64_t)a.k_len + 16 * KW - 1) / (16 * KW); }
@@ -807,7 +827,7 @@ hipError_t backward(AttnArgs a, void* ws, hipStream_t s) {
     if (e == hipSuccess && rq > 1) e = sum_runs<T>(a, a.dq, nullptr, a.q_len, a.group, rq, part, s);
   }
   if (e == hipSuccess && a.k_len) {
-    e = launch(key_grad_kernel<T, DP, 1, Sh::KW, Sh::BQ, Sh::OCC>, Sh::key_tiles(a) * Sh::pairs(a) * rk, Sh::KW * 64, s, a, rk, part);
+    e = launch(key_grad_kernel<T, DP, 1, Sh::KW, Sh::KBQ, Sh::OCC>, Sh::key_tiles(a) * Sh::pairs(a) * rk, Sh::KW * 64, s, a, rk, part);
     if (e == hipSuccess && rk > 1) e = sum_runs<T>(a, a.dk, a.dv, a.k_len, 1, rk, part, s);
   }
   return e;

@@ -136,16 +136,19 @@ __global__ __launch_bounds__(256) void rows_forward_kernel(AttnArgs a, RowPlan p
   const T* kp = row_of<T>(a.k, a.sk, b, 0, hk) + at;
   const T* vp = row_of<T>(a.v, a.sv, b, 0, hk) + at;
   u32x4 kr[U], vr[U];
+  const RowEnd end = row_end<T>(a.d);
   auto fetch = [&](int base) {
+    by_end(end, [&](auto e) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int j = base + u * G + slot;
-      kr[u] = vr[u] = u32x4{0, 0, 0, 0};
-      if (j < k1 && at < a.d) {
-        kr[u] = load16(kp + (int64_t)j * a.sk.row, a.d - at);
-        vr[u] = load16(vp + (int64_t)j * a.sv.row, a.d - at);
+      for (int u = 0; u < U; ++u) {
+        const int j = base + u * G + slot;
+        kr[u] = vr[u] = u32x4{0, 0, 0, 0};
+        if (j < k1 && at < a.d) {
+          kr[u] = load16<T, decltype(e)::value>(kp + (int64_t)j * a.sk.row, a.d - at);
+          vr[u] = load16<T, decltype(e)::value>(vp + (int64_t)j * a.sv.row, a.d - at);
+        }
       }
-    }
+    });
   };
   int base = k0 + (WIDE ? wave * STEP : 0);
   if (base < k1) fetch(base);                                 // (with the rows on their way too: one wait for a short list)
@@ -156,7 +159,7 @@ __global__ __launch_bounds__(256) void rows_forward_kernel(AttnArgs a, RowPlan p
   for (int r = 0; r < R; ++r) {
     const int i = query_of(a, r);
     u32x4 raw = {0, 0, 0, 0};
-    if (r < rows && i < l.qn && at < a.d) raw = load16(row_of<T>(a.q, a.sq, b, i, hk * a.group + r - i * a.group) + at, a.d - at);
+    if (r < rows && i < l.qn && at < a.d) raw = load16(row_of<T>(a.q, a.sq, b, i, hk * a.group + r - i * a.group) + at, a.d - at, end);
     spread<T>(raw, q[r]);
     x[r].clear();
   }
@@ -276,16 +279,19 @@ __global__ __launch_bounds__(256) void rows_grad_kernel(AttnArgs a, RowPlan plan
   const T* kp = row_of<T>(a.k, a.sk, b, 0, hk) + at;
   const T* vp = row_of<T>(a.v, a.sv, b, 0, hk) + at;
   u32x4 kr[U], vr[U];
+  const RowEnd end = row_end<T>(a.d);
   auto fetch = [&](int base) {
+    by_end(end, [&](auto e) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int j = base + u * G + slot;
-      kr[u] = vr[u] = u32x4{0, 0, 0, 0};
-      if (j >= k0 && j < k1 && at < a.d) {
-        kr[u] = load16(kp + (int64_t)j * a.sk.row, a.d - at);
-        vr[u] = load16(vp + (int64_t)j * a.sv.row, a.d - at);
+      for (int u = 0; u < U; ++u) {
+        const int j = base + u * G + slot;
+        kr[u] = vr[u] = u32x4{0, 0, 0, 0};
+        if (j >= k0 && j < k1 && at < a.d) {
+          kr[u] = load16<T, decltype(e)::value>(kp + (int64_t)j * a.sk.row, a.d - at);
+          vr[u] = load16<T, decltype(e)::value>(vp + (int64_t)j * a.sv.row, a.d - at);
+        }
       }
-    }
+    });
   };
   int base = first + (WIDE ? wave * STEP : 0);
   if (base < last) fetch(base);                               // (with the rows on their way too: one wait for a short list)
@@ -299,9 +305,9 @@ __global__ __launch_bounds__(256) void rows_grad_kernel(AttnArgs a, RowPlan plan
     if (hi[r] > lo[r]) {
       lse2[r] = a.lse[((int64_t)b * a.heads + head) * a.q_len + i] * kLog2e;
       if (at < a.d) {
-        rq = load16(row_of<T>(a.q, a.sq, b, i, head) + at, a.d - at);
-        rd = load16(row_of<T>(a.dout, a.sdo, b, i, head) + at, a.d - at);
-        ro = load16(row_of<T>(a.out, a.so, b, i, head) + at, a.d - at);
+        rq = load16(row_of<T>(a.q, a.sq, b, i, head) + at, a.d - at, end);
+        rd = load16(row_of<T>(a.dout, a.sdo, b, i, head) + at, a.d - at, end);
+        ro = load16(row_of<T>(a.out, a.so, b, i, head) + at, a.d - at, end);
       }
     }
     float o[E];

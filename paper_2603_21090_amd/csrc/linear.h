@@ -160,11 +160,12 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product a) {
   TileMove<T, L_ROWS ? BN : BK, L_ROWS ? BK : BN, THREADS> ml[DEPTH];
   TileMove<T, R_ROWS ? BM : BK, R_ROWS ? BK : BM, THREADS> mr[DEPTH];
   const T *lp = static_cast<const T*>(a.l), *rp = static_cast<const T*>(a.r);
+  const RowEnd el = row_end<T>(L_ROWS ? a.k : a.n), er = row_end<T>(R_ROWS ? a.k : a.m);
   auto fetch = [&](int d, int k) {
-    if constexpr (L_ROWS) ml[d].fetch([&](int i) -> const T* { return n0 + i < a.n ? lp + (int64_t)(n0 + i) * a.ld_l + k : nullptr; }, ke - k);
-    else ml[d].fetch([&](int i) -> const T* { return k + i < ke ? lp + (int64_t)(k + i) * a.ld_l + n0 : nullptr; }, a.n - n0);
-    if constexpr (R_ROWS) mr[d].fetch([&](int i) -> const T* { return m0 + i < a.m ? rp + (int64_t)(m0 + i) * a.ld_r + k : nullptr; }, ke - k);
-    else mr[d].fetch([&](int i) -> const T* { return k + i < ke ? rp + (int64_t)(k + i) * a.ld_r + m0 : nullptr; }, a.m - m0);
+    if constexpr (L_ROWS) ml[d].fetch([&](int i) -> const T* { return n0 + i < a.n ? lp + (int64_t)(n0 + i) * a.ld_l + k : nullptr; }, ke - k, el);
+    else ml[d].fetch([&](int i) -> const T* { return k + i < ke ? lp + (int64_t)(k + i) * a.ld_l + n0 : nullptr; }, a.n - n0, el);
+    if constexpr (R_ROWS) mr[d].fetch([&](int i) -> const T* { return m0 + i < a.m ? rp + (int64_t)(m0 + i) * a.ld_r + k : nullptr; }, ke - k, er);
+    else mr[d].fetch([&](int i) -> const T* { return k + i < ke ? rp + (int64_t)(k + i) * a.ld_r + m0 : nullptr; }, a.m - m0, er);
   };
 
   floatx4 acc[NB][MB];

@@ -14,6 +14,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace stgn {
 
 typedef float floatx4 __attribute__((ext_vector_type(4)));
@@ -139,17 +141,50 @@ __device__ inline typename Elem<T>::Frag placed_cols(const T* tile, int row, int
   }
 }
 
-// 16 bytes at p of which `count` elements exist (the rest zero)
+// How the rows that a kernel reads in pieces of 16 bytes end: with a whole piece; with a part of one (WIDE: the row's last 16 bytes are
+// read instead and moved down, one load without a branch); or the row is shorter than a piece and its elements are read one by one.
+enum RowEnd { kWhole, kWide, kShort };
 template <class T>
+__device__ inline RowEnd row_end(int width) { return width % Elem<T>::E == 0 ? kWhole : width > Elem<T>::E ? kWide : kShort; }
+
+// v's last bytes, `bytes` of them dropped at the front, zeros behind
+template <class T>
+__device__ inline u32x4 moved_down(u32x4 v, int bytes) {
+  v = bytes & 8 ? u32x4{v[2], v[3], 0u, 0u} : v;
+  v = bytes & 4 ? u32x4{v[1], v[2], v[3], 0u} : v;
+  if constexpr (sizeof(T) == 2)
+    v = bytes & 2 ? u32x4{__builtin_amdgcn_alignbyte(v[1], v[0], 2), __builtin_amdgcn_alignbyte(v[2], v[1], 2),
+                          __builtin_amdgcn_alignbyte(v[3], v[2], 2), v[3] >> 16} : v;
+  return v;
+}
+
+// 16 bytes at p of which `count` elements (one at least) are the row's last ones, or all; the rest zeros
+template <class T, RowEnd END>
 __device__ inline u32x4 load16(const T* p, int count) {
   constexpr int E = Elem<T>::E;
-  if (count >= E) return *reinterpret_cast<const u32x4_any*>(p);
+  if constexpr (END == kWhole) return *reinterpret_cast<const u32x4_any*>(p);
+  if constexpr (END == kWide) {
+    const int missing = count < E ? E - count : 0;
+    return moved_down<T>(*reinterpret_cast<const u32x4_any*>(p - missing), missing * (int)sizeof(T));
+  }
   union { T e[E]; u32x4 v; } u;
   u.v = u32x4{0, 0, 0, 0};
 #pragma unroll
-  for (int j = 0; j < E - 1; ++j)
+  for (int j = 0; j < E; ++j)
     if (j < count) u.e[j] = p[j];
   return u.v;
+}
+// ... the same for a row of any width
+template <class T>
+__device__ inline u32x4 load16(const T* p, int count, RowEnd end) {
+  return end == kWhole ? load16<T, kWhole>(p, count) : end == kWide ? load16<T, kWide>(p, count) : load16<T, kShort>(p, count);
+}
+// f(std::integral_constant<RowEnd, end>): a copy of f's loads per kind, none with another kind's branches between them
+template <class F>
+__device__ inline void by_end(RowEnd end, F f) {
+  if (end == kWhole) f(std::integral_constant<RowEnd, kWhole>());
+  else if (end == kWide) f(std::integral_constant<RowEnd, kWide>());
+  else f(std::integral_constant<RowEnd, kShort>());
 }
 
 // four sums as elements col .. col + 3 of a row of `cols` elements
@@ -192,17 +227,19 @@ struct TileMove {
   static constexpr int E = Elem<T>::E, PIECES = ROWS * COLS / E, NP = (PIECES + THREADS - 1) / THREADS;
   u32x4 r[NP];
 
-  // row(i): the address of the tile's row i, or null if there is none.  cols: elements a row has from column 0 of the tile.
+  // row(i): the address of the tile's row i, or null if there is none.  cols: elements a row has from column 0 of the tile, to its end.
   template <class Row>
-  __device__ inline void fetch(Row row, int cols) {
+  __device__ inline void fetch(Row row, int cols, RowEnd end) {
+    by_end(end, [&](auto e) {
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int p = (int)threadIdx.x + i * THREADS, c = p % (COLS / E) * E;
-      r[i] = u32x4{0, 0, 0, 0};
-      if (PIECES % THREADS != 0 && p >= PIECES) continue;
-      const T* at = row(p / (COLS / E));
-      if (at != nullptr && c < cols) r[i] = load16(at + c, cols - c);
-    }
+      for (int i = 0; i < NP; ++i) {
+        const int p = (int)threadIdx.x + i * THREADS, c = p % (COLS / E) * E;
+        r[i] = u32x4{0, 0, 0, 0};
+        if (PIECES % THREADS != 0 && p >= PIECES) continue;
+        const T* at = row(p / (COLS / E));
+        if (at != nullptr && c < cols) r[i] = load16<T, decltype(e)::value>(at + c, cols - c);
+      }
+    });
   }
   __device__ inline void store(T* tile, int stride) const {
 #pragma unroll
@@ -225,31 +262,38 @@ __device__ inline void store_placed(T* tile, const u32x4 (&r)[NP]) {
   }
 }
 
-// The same for consecutive tiles of a matrix whose rows lie `stride` apart: addresses are computed once and advance by a tile.
+// The same for consecutive tiles of a matrix: addresses are computed once and advance by a tile.
 template <class T, int ROWS, int COLS, int THREADS>
 struct StreamMove {
   static constexpr int E = Elem<T>::E, PER_ROW = COLS / E, NP = ROWS * PER_ROW / THREADS, APART = THREADS / PER_ROW;
   static_assert(ROWS * PER_ROW % THREADS == 0 && THREADS % PER_ROW == 0, "every thread carries whole pieces of one column");
   const T* at;                                                // this thread's first piece of the next tile
-  int64_t stride;
+  int64_t apart, step;                                        // elements from one of its pieces to the next, from tile to tile
   int row, count;                                             // its row in the tile; elements the matrix has from its column on
   u32x4 r[NP];
 
-  __device__ inline void start(const T* base, int64_t stride_, int cols) {
-    const int t = (int)threadIdx.x, c = t % PER_ROW * E;
-    row = t / PER_ROW;
+  // first: the address of this thread's row threadIdx.x / PER_ROW of the first tile
+  __device__ inline void start(const T* first, int64_t apart_, int64_t step_, int cols) {
+    const int c = (int)threadIdx.x % PER_ROW * E;
+    row = (int)threadIdx.x / PER_ROW;
     count = cols - c;
-    stride = stride_;
-    at = base + row * stride_ + c;
+    at = first + c;
+    apart = apart_;
+    step = step_;
+  }
+  __device__ inline void start_rows(const T* base, int64_t stride, int cols) {
+    start(base + (int64_t)((int)threadIdx.x / PER_ROW) * stride, APART * stride, ROWS * stride, cols);
   }
   // rows: how many the matrix has from the tile's first row on (the same for all threads)
-  __device__ inline void fetch(int rows) {
+  __device__ inline void fetch(int rows, RowEnd end) {
+    by_end(end, [&](auto e) {
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      r[i] = u32x4{0, 0, 0, 0};
-      if (count > 0 && (rows >= ROWS || row + i * APART < rows)) r[i] = load16(at + i * APART * stride, count);
-    }
-    at += ROWS * stride;
+      for (int i = 0; i < NP; ++i) {
+        r[i] = u32x4{0, 0, 0, 0};
+        if (count > 0 && (rows >= ROWS || row + i * APART < rows)) r[i] = load16<T, decltype(e)::value>(at + i * apart, count);
+      }
+    });
+    at += step;
   }
   __device__ inline void store(T* tile) const { store_placed<T, ROWS, COLS, THREADS>(tile, r); }
 };
