@@ -148,7 +148,7 @@ inline int runs_for(int64_t workgroups, int64_t streamed) {
 // ---- forward
 // The softmax needs some reference score per row, not the largest one: it moves only when a score exceeds it by more than 2^kLazy, which is
 // rare after the first tiles, and the accumulators are rescaled only then.
-template <class T, int DP, int NB, int WAVES>
+template <class T, int DP, int NB, int WAVES, bool SKIP>
 __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void forward_kernel(AttnArgs a, int runs, float* part) {
   using El = Elem<T>;
   constexpr int BK = stream_rows<T, DP>(), S = lds_stride<T>(DP), ROWS = WAVES * NB * 16, KB = BK / 16, DB = DP / 16;
@@ -221,6 +221,7 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void forward_kernel(A
         for (int c = 0; c < NB; ++c) s[y][c] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < DP / El::KF; ++k) {
+          if (SKIP && k > 0 && k * El::KF >= a.d) break;
           const typename El::Frag f = placed_rows<T, DP>(ks[buf], y * 16, k * El::KF);
 #pragma unroll
           for (int c = 0; c < NB; ++c) s[y][c] = El::mma(f, qf[c][k], s[y][c]);
@@ -284,6 +285,7 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void forward_kernel(A
         }
 #pragma unroll
         for (int x = 0; x < DB; ++x) {
+          if (SKIP && x > 0 && x * 16 >= a.d) break;
           const typename El::Frag f = placed_cols<T, DP>(vs[buf], y * 16, x * 16);
 #pragma unroll
           for (int c = 0; c < NB; ++c) o[x][c] = El::mma(f, pf[c], o[x][c]);
@@ -326,7 +328,7 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void forward_kernel(A
 // registers, keys and values stream.  With 16-bit types, o is rounded; where a tile holds all keys of the list, delta is the sum of p dp
 // instead, from the unrounded weights: a short list's delta is not small beside its dp (lists of 10 to 30 keys in bf16: dq 0.27 % off, 0.24 %
 // with it; half of that is the rounding of dq itself).
-template <class T, int DP, int NB, int WAVES>
+template <class T, int DP, int NB, int WAVES, bool SKIP>
 __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void query_grad_kernel(AttnArgs a, int runs, float* part) {
   using El = Elem<T>;
   constexpr int BK = stream_rows<T, DP>(), S = lds_stride<T>(DP), ROWS = WAVES * NB * 16, DB = DP / 16, PB = El::PB;
@@ -398,6 +400,7 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void query_grad_kerne
       for (int c = 0; c < NB; ++c) p[u][c] = dp[u][c] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < DP / El::KF; ++k) {
+        if (SKIP && k > 0 && k * El::KF >= a.d) break;
         const typename El::Frag kf = placed_rows<T, DP>(ks[buf], (y + u) * 16, k * El::KF), vf = placed_rows<T, DP>(vs[buf], (y + u) * 16, k * El::KF);
 #pragma unroll
         for (int c = 0; c < NB; ++c) {
@@ -472,6 +475,7 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void query_grad_kerne
         }
 #pragma unroll
         for (int x = 0; x < DB; ++x) {
+          if (SKIP && x > 0 && x * 16 >= a.d) break;
           const typename El::Frag kf = placed_cols<T, DP>(ks[buf], y * 16, x * 16);
 #pragma unroll
           for (int c = 0; c < NB; ++c) dq[x][c] = El::mma(kf, f[c], dq[x][c]);
@@ -530,7 +534,7 @@ struct RowMove : StreamMove<T, BQ, DP, THREADS> {
 };
 
 // dk, dv: keys and values in registers, queries and dout stream
-template <class T, int DP, int NB, int WAVES, int BQ, int OCC>
+template <class T, int DP, int NB, int WAVES, int BQ, int OCC, bool SKIP>
 __global__ __launch_bounds__(WAVES * 64, OCC) void key_grad_kernel(AttnArgs a, int runs, float* part) {
   using El = Elem<T>;
   constexpr int S = lds_stride<T>(DP), KEYS = WAVES * NB * 16, DB = DP / 16, PB = El::PB;
@@ -617,6 +621,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void key_grad_kernel(AttnArgs a, i
         for (int c = 0; c < NB; ++c) s[u][c] = dp[u][c] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < DP / El::KF; ++k) {
+          if (SKIP && k > 0 && k * El::KF >= a.d) break;
           const typename El::Frag qf = placed_rows<T, DP>(qt, (y + u) * 16, k * El::KF), df = placed_rows<T, DP>(gt, (y + u) * 16, k * El::KF);
 #pragma unroll
           for (int c = 0; c < NB; ++c) {
@@ -655,6 +660,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void key_grad_kernel(AttnArgs a, i
       }
 #pragma unroll
       for (int x = 0; x < DB; ++x) {
+        if (SKIP && x > 0 && x * 16 >= a.d) break;
         const typename El::Frag df = placed_cols<T, DP>(gt, y * 16, x * 16), qf = placed_cols<T, DP>(qt, y * 16, x * 16);
 #pragma unroll
         for (int c = 0; c < NB; ++c) {
@@ -786,7 +792,10 @@ struct Shape {
   static constexpr int NB = sizeof(T) == 4 || DP > 128 ? 1 : 2, BQ = stream_rows<T, DP>();
   // rows between two barriers: twice as many where one workgroup has the CU to itself and its waves wait for each other (880 -> 845 us)
   static constexpr int KBQ = sizeof(T) == 2 && DP == 128 ? 128 : BQ;
-  static constexpr int KW = sizeof(T) == 2 && DP <= 128 ? 8 : 4, OCC = DP <= 128 ? 2 : 1;
+  static constexpr int KW = sizeof(T) == 2 && DP <= 128 ? 8 : 4, OCC = DP > 128 ? 1 : sizeof(T) == 2 && DP == 64 ? 4 : 2;
+  // Heads of up to three quarters of DP numbers have kernels that ask before every product whether it is all padding (80 of 128: fp32 a quarter
+  // less time, bf16 a tenth); wider ones would only pay for the question (4 to 15 %).
+  static bool skips(const AttnArgs& a) { return a.d * 4 <= DP * 3; }
   static int64_t query_tiles(const AttnArgs& a) { return ((int64_t)a.q_len * a.group + 64 * NB - 1) / (64 * NB); }
   static int64_t key_tiles(const AttnArgs& a) { return ((int64_t)a.k_len + 16 * KW - 1) / (16 * KW); }
   static int64_t pairs(const AttnArgs& a) { return (int64_t)a.lists * a.kv_heads; }
@@ -810,7 +819,8 @@ template <class T, int DP>
 hipError_t forward(const AttnArgs& a, float* part, hipStream_t s) {
   using Sh = Shape<T, DP>;
   const int runs = Sh::query_runs(a);
-  const hipError_t e = launch(forward_kernel<T, DP, Sh::NB, 4>, Sh::query_tiles(a) * Sh::pairs(a) * runs, 256, s, a, runs, part);
+  const auto kernel = Sh::skips(a) ? forward_kernel<T, DP, Sh::NB, 4, true> : forward_kernel<T, DP, Sh::NB, 4, false>;
+  const hipError_t e = launch(kernel, Sh::query_tiles(a) * Sh::pairs(a) * runs, 256, s, a, runs, part);
   if (e != hipSuccess || runs == 1) return e;
   return launch(join_kernel<T>, join_grid(Sh::pairs(a) * a.q_len * a.group, runs), 256, s, a, runs, (const float*)part);
 }
@@ -823,11 +833,13 @@ hipError_t backward(AttnArgs a, void* ws, hipStream_t s) {
   const int rq = Sh::query_runs(a), rk = Sh::key_runs(a);
   hipError_t e = hipSuccess;
   if (a.q_len) {
-    e = launch(query_grad_kernel<T, DP, Sh::NB, 4>, Sh::query_tiles(a) * Sh::pairs(a) * rq, 256, s, a, rq, part);
+    const auto kernel = Sh::skips(a) ? query_grad_kernel<T, DP, Sh::NB, 4, true> : query_grad_kernel<T, DP, Sh::NB, 4, false>;
+    e = launch(kernel, Sh::query_tiles(a) * Sh::pairs(a) * rq, 256, s, a, rq, part);
     if (e == hipSuccess && rq > 1) e = sum_runs<T>(a, a.dq, nullptr, a.q_len, a.group, rq, part, s);
   }
   if (e == hipSuccess && a.k_len) {
-    e = launch(key_grad_kernel<T, DP, 1, Sh::KW, Sh::KBQ, Sh::OCC>, Sh::key_tiles(a) * Sh::pairs(a) * rk, Sh::KW * 64, s, a, rk, part);
+    const auto kernel = Sh::skips(a) ? key_grad_kernel<T, DP, 1, Sh::KW, Sh::KBQ, Sh::OCC, true> : key_grad_kernel<T, DP, 1, Sh::KW, Sh::KBQ, Sh::OCC, false>;
+    e = launch(kernel, Sh::key_tiles(a) * Sh::pairs(a) * rk, Sh::KW * 64, s, a, rk, part);
     if (e == hipSuccess && rk > 1) e = sum_runs<T>(a, a.dk, a.dv, a.k_len, 1, rk, part, s);
   }
   return e;
