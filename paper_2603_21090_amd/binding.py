@@ -212,7 +212,8 @@ def _run_operator(ask, call, args, grad, device):
         size, ws = n.value, None
         if size:
             ws = torch.empty(size, dtype=torch.uint8, device=device)
-        rc = call(args, ws.data_ptr() if size else None, size, torch.cuda.current_stream().cuda_stream)
+        # (the handle alone: building a Stream object around it takes as long as the launch)
+        rc = call(args, ws.data_ptr() if size else None, size, torch._C._cuda_getCurrentRawStream(device.index))
     if rc:
         raise StgnError(rc, load_library().stgn_last_error(None).decode())
 
@@ -271,6 +272,8 @@ def _attention_call(q, k, v, q_lens, k_lens, causal, window, scale):
     if q.dim() != 4 or k.dim() != 4:
         raise ValueError("q, k and v must be [lists, rows, heads, numbers]")
     (lists, q_len, heads, d), (_, k_len, kv_heads, _) = q.shape, k.shape
+    if d < 1 or window < 0:
+        raise ValueError("a head has one number at least, a window is 0 or more")
     shape = (lists, k_len, kv_heads, d)
     where = [0, 0, _expect("q", q, q, q.shape), _expect("k", k, q, shape), _expect("v", v, q, shape)]
     for at, t in enumerate((q_lens, k_lens)):

@@ -157,15 +157,16 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product a) {
   const int m0 = row * BM, n0 = col * BN;
   const int kb = split * a.k_per, ke = min(a.k, kb + a.k_per);
 
-  TileMove<T, L_ROWS ? BN : BK, L_ROWS ? BK : BN, THREADS> ml[DEPTH];
-  TileMove<T, R_ROWS ? BM : BK, R_ROWS ? BK : BM, THREADS> mr[DEPTH];
-  const T *lp = static_cast<const T*>(a.l), *rp = static_cast<const T*>(a.r);
-  const RowEnd el = row_end<T>(L_ROWS ? a.k : a.n), er = row_end<T>(R_ROWS ? a.k : a.m);
+  using MoveL = ProductMove<T, BN, BK, THREADS, L_ROWS>;
+  using MoveR = ProductMove<T, BM, BK, THREADS, R_ROWS>;
+  MoveL ml;
+  MoveR mr;
+  ml.start(a.l, a.ld_l, n0, a.n, kb, ke, a.k);
+  mr.start(a.r, a.ld_r, m0, a.m, kb, ke, a.k);
+  u32x4 rl[DEPTH][MoveL::NP], rr[DEPTH][MoveR::NP];
   auto fetch = [&](int d, int k) {
-    if constexpr (L_ROWS) ml[d].fetch([&](int i) -> const T* { return n0 + i < a.n ? lp + (int64_t)(n0 + i) * a.ld_l + k : nullptr; }, ke - k, el);
-    else ml[d].fetch([&](int i) -> const T* { return k + i < ke ? lp + (int64_t)(k + i) * a.ld_l + n0 : nullptr; }, a.n - n0, el);
-    if constexpr (R_ROWS) mr[d].fetch([&](int i) -> const T* { return m0 + i < a.m ? rp + (int64_t)(m0 + i) * a.ld_r + k : nullptr; }, ke - k, er);
-    else mr[d].fetch([&](int i) -> const T* { return k + i < ke ? rp + (int64_t)(k + i) * a.ld_r + m0 : nullptr; }, a.m - m0, er);
+    ml.fetch(rl[d], k);
+    mr.fetch(rr[d], k);
   };
 
   floatx4 acc[NB][MB];
@@ -183,8 +184,8 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product a) {
       const int k = kt + d * BK;
       if (k >= ke) break;
       __syncthreads();
-      ml[d].store(ls, SL);
-      mr[d].store(rs, SR);
+      MoveL::store(ls, rl[d]);
+      MoveR::store(rs, rr[d]);
       __syncthreads();
       if (k + DEPTH * BK < ke) fetch(d, k + DEPTH * BK);
 #pragma unroll

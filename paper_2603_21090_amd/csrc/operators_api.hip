@@ -163,7 +163,7 @@ int check_attention(const stgn_attention_args* a, bool grad, bool sizes_only) {
   const uint64_t rows = (uint64_t)a->q_len * (a->heads / a->kv_heads);
   if (rows > kMaxRows) return no("q_len times the heads that share a key head out of range");
   const uint64_t pairs = (uint64_t)a->lists * a->kv_heads;
-  if (((rows + 63) / 64) * pairs > kMaxGroups || (((uint64_t)a->k_len + 63) / 64) * pairs > kMaxGroups)
+  if (((rows + 63) / 64) * pairs > kMaxGroups / 2 || (((uint64_t)a->k_len + 63) / 64) * pairs > kMaxGroups / 2)   // (of up to 512 threads)
     return no("the lists have more tiles than a launch");
   if (sizes_only) return STGN_OK;
   if (!(a->scale == a->scale) || a->scale - a->scale != 0.0f) return no("scale must be finite");

@@ -220,34 +220,49 @@ __device__ inline floatx4 load4(const T* row, int col, int cols) {
   return v;
 }
 
-// A tile of ROWS x COLS elements on its way from global memory through registers into LDS; every thread of THREADS carries
-// NP pieces of 16 bytes.  Rows and columns that the matrix does not have are zeros: what a caller keeps there is never read.
-template <class T, int ROWS, int COLS, int THREADS>
-struct TileMove {
-  static constexpr int E = Elem<T>::E, PIECES = ROWS * COLS / E, NP = (PIECES + THREADS - 1) / THREADS;
-  u32x4 r[NP];
+// An operand of a product on its way from global memory through registers into LDS, tile after tile along the summed index k: LINES of
+// the output's rows or columns, BK elements of k.  ALONG: k runs along the matrix's rows, a tile is [LINES][BK]; else it has a row per k, a tile is
+// [BK][LINES].  Every thread carries NP pieces of 16 bytes.  Lines and elements that the matrix does not have are zeros: what lies there
+// is never read.
+template <class T, int LINES, int BK, int THREADS, bool ALONG>
+struct ProductMove {
+  static constexpr int E = Elem<T>::E, ROWS = ALONG ? LINES : BK, PER_ROW = (ALONG ? BK : LINES) / E, PIECES = ROWS * PER_ROW;
+  static constexpr int NP = (PIECES + THREADS - 1) / THREADS;
+  static constexpr bool STEADY = THREADS % PER_ROW == 0;      // a thread's pieces lie below each other
+  static constexpr int STRIDE = lds_stride<T>(ALONG ? BK : LINES);
+  const T* base;                                              // the tile's first element
+  int64_t ld;
+  int lines, end;                                             // lines from the tile's first on; k that the sum ends in front of
+  RowEnd row;
+  static __device__ inline int row_of(int i) { return STEADY ? (int)threadIdx.x / PER_ROW + i * (THREADS / PER_ROW) : ((int)threadIdx.x + i * THREADS) / PER_ROW; }
+  static __device__ inline int col_of(int i) { return (STEADY ? (int)threadIdx.x : (int)threadIdx.x + i * THREADS) % PER_ROW * E; }
 
-  // row(i): the address of the tile's row i, or null if there is none.  cols: elements a row has from column 0 of the tile, to its end.
-  template <class Row>
-  __device__ inline void fetch(Row row, int cols, RowEnd end) {
-    by_end(end, [&](auto e) {
+  __device__ inline void start(const void* matrix, int64_t ld_, int first, int total_lines, int k, int end_, int total_k) {
+    base = static_cast<const T*>(matrix) + (ALONG ? (int64_t)first * ld_ + k : (int64_t)k * ld_ + first);
+    ld = ld_;
+    lines = total_lines - first;
+    end = end_;
+    row = row_end<T>(ALONG ? total_k : total_lines);
+  }
+  // the tile at k, which is the next one
+  __device__ inline void fetch(u32x4 (&r)[NP], int k) {
+    const int rows = ALONG ? lines : end - k, cols = ALONG ? end - k : lines;
+    auto each = [&](auto load) {
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
-        const int p = (int)threadIdx.x + i * THREADS, c = p % (COLS / E) * E;
+        const int x = row_of(i), c = col_of(i);
         r[i] = u32x4{0, 0, 0, 0};
-        if (PIECES % THREADS != 0 && p >= PIECES) continue;
-        const T* at = row(p / (COLS / E));
-        if (at != nullptr && c < cols) r[i] = load16<T, decltype(e)::value>(at + c, cols - c);
+        if ((PIECES % THREADS == 0 || x < ROWS) && x < rows && c < cols) r[i] = load(base + (int64_t)x * ld + c, cols - c);
       }
-    });
+    };
+    if (cols >= (ALONG ? BK : LINES)) each([](const T* p, int) { return *reinterpret_cast<const u32x4_any*>(p); });
+    else by_end(row, [&](auto e) { each([](const T* p, int count) { return load16<T, decltype(e)::value>(p, count); }); });
+    base += ALONG ? BK : BK * ld;
   }
-  __device__ inline void store(T* tile, int stride) const {
+  static __device__ inline void store(T* tile, const u32x4 (&r)[NP]) {
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int p = (int)threadIdx.x + i * THREADS;
-      if (PIECES % THREADS != 0 && p >= PIECES) continue;
-      *reinterpret_cast<u32x4*>(tile + p / (COLS / E) * stride + p % (COLS / E) * E) = r[i];
-    }
+    for (int i = 0; i < NP; ++i)
+      if (PIECES % THREADS == 0 || row_of(i) < ROWS) *reinterpret_cast<u32x4*>(tile + row_of(i) * STRIDE + col_of(i)) = r[i];
   }
 };
 
@@ -262,7 +277,7 @@ __device__ inline void store_placed(T* tile, const u32x4 (&r)[NP]) {
   }
 }
 
-// The same for consecutive tiles of a matrix: addresses are computed once and advance by a tile.
+// ROWS x COLS elements of a matrix on their way into LDS, tile after tile down its rows: addresses are computed once and advance by a tile.
 template <class T, int ROWS, int COLS, int THREADS>
 struct StreamMove {
   static constexpr int E = Elem<T>::E, PER_ROW = COLS / E, NP = ROWS * PER_ROW / THREADS, APART = THREADS / PER_ROW;

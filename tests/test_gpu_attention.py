@@ -169,3 +169,26 @@ def test_gradients_against_differences():
         best = (4 * slopes[1] - slopes[0]) / 3                # the h^2 term taken out; what is left is below the two slopes' distance
         noise = 2 * 2.0 ** -24 * 60 * 2.0 ** 7 * 8            # rounding of the weights: u times 60 rows' worth of |out . dout|, over h
         assert abs(best - (grads[at].double() * dirn.double()).sum().item()) <= abs(slopes[0] - slopes[1]) + noise
+
+
+@pytest.mark.parametrize("ql,kl", [(1, 3000), (200, 200)])
+def test_calls_at_the_same_time_on_two_streams(ql, kl):
+    """Both in flight, again and again, each with buffers of its own: the bits of a call alone."""
+    sides, kept = [torch.cuda.Stream(), torch.cuda.Stream()], []
+    for n in range(2):
+        q, k, v, do, _, _ = make(4, ql, kl, 4, 2, 64, False, torch.bfloat16, seed=n)
+        Q, K, V, DO = on_gpu(q, k, v, do)
+        out, lse = binding.attention(Q, K, V, causal=True)
+        kept.append((Q, K, V, DO, out, lse, binding.attention_grad(DO, Q, K, V, out, lse, causal=True)))
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for n, side in enumerate(sides):
+            with torch.cuda.stream(side):
+                Q, K, V, DO, out, lse, _ = kept[n]
+                got[n].append(binding.attention(Q, K, V, causal=True) + binding.attention_grad(DO, Q, K, V, out, lse, causal=True))
+    torch.cuda.synchronize()
+    for n in range(2):
+        want = (kept[n][4], kept[n][5]) + tuple(kept[n][6])
+        for res in got[n]:
+            assert all(torch.equal(a, b) for a, b in zip(res, want))

@@ -110,7 +110,8 @@ def test_messages_belong_to_the_thread(lib):
     lambda x, w: binding.linear(x[:1].expand(4, 6), w), lambda x, w: binding.linear_grad(torch.ones(4, 8), x, w, activation="gelu"),
     lambda x, w: binding.linear_grad(torch.ones(3, 8), x, w),
     lambda x, w: binding.attention(x, x, x), lambda x, w: binding.attention(x[None, None], x[None, None], w[None, None]),
-    lambda x, w: binding.attention(*(x[None, None],) * 3, k_lens=torch.ones(1)), lambda x, w: binding.attention(*(x[None, None],) * 3),
+    lambda x, w: binding.attention(*(x[None, None],) * 3, causal=True, window=-1), lambda x, w: binding.attention(*(x[None, None, :, :0],) * 3),
+    lambda x, w: binding.linear(x, w, activation="tanh"), lambda x, w: binding.attention(*(x[None, None],) * 3, k_lens=torch.ones(1)), lambda x, w: binding.attention(*(x[None, None],) * 3),
     lambda x, w: binding.attention_grad(*(x[None, None],) * 5, torch.ones(1, 4, 2)),
 ])
 def test_binding_refuses(lib, call):
