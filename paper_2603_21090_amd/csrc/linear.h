@@ -360,12 +360,13 @@ __global__ __launch_bounds__(256) void dz_kernel(LinearGradArgs a, T* dz, int64_
       acc += v;
     }
   }
-  if (!sums) return;
+  if (!a.db) return;
   wsum[wave][lane] = acc;
   __syncthreads();
   if (wave == 0 && n < a.d_out) {
     const floatx4 v = (wsum[0][lane] + wsum[1][lane]) + (wsum[2][lane] + wsum[3][lane]);
-    store4(sums + (int64_t)chunk * a.d_out, n, a.d_out, v);
+    if (rows_per >= a.rows) store4(static_cast<T*>(a.db), n, a.d_out, v);       // all rows: no second launch
+    else store4(sums + (int64_t)chunk * a.d_out, n, a.d_out, v);
   }
 }
 
@@ -488,14 +489,14 @@ GradLayout layout_of(const LinearGradArgs& a) {
   g.ld_dz = up(a.d_out, 16 / sizeof(T));
   const int64_t cols = (a.d_out + 255) / 256;
   int64_t chunks = (1024 + cols - 1) / cols;
-  const int64_t most = (a.rows + 15) / 16;
+  const int64_t most = a.rows <= 64 ? 1 : (a.rows + 15) / 16;
   if (chunks > most) chunks = most;
   if (chunks < 1) chunks = 1;
   g.rows_per = (int)((a.rows + chunks - 1) / chunks);
   if (g.rows_per < 1) g.rows_per = 1;
   g.chunks = (int)chunks;
   g.sums = a.act != ACT_NONE ? (size_t)up((int64_t)a.rows * g.ld_dz * sizeof(T), 256) : 0;
-  g.part = g.sums + (a.db ? (size_t)up((int64_t)g.chunks * a.d_out * sizeof(float), 256) : 0);
+  g.part = g.sums + (a.db && g.chunks > 1 ? (size_t)up((int64_t)g.chunks * a.d_out * sizeof(float), 256) : 0);
   const size_t px = a.dx ? part_bytes<T>(a.rows, a.d_in, a.d_out, true, true) : 0, pw = a.dw ? part_bytes<T>(a.d_in, a.d_out, a.rows, false, false) : 0;
   g.total = g.part + (px > pw ? px : pw);
   return g;
@@ -506,9 +507,9 @@ hipError_t backward(const LinearGradArgs& f, void* ws, hipStream_t s) {
   const GradLayout g = layout_of<T>(f);
   char* base = static_cast<char*>(ws);
   T* dz = f.act != ACT_NONE ? reinterpret_cast<T*>(base) : nullptr;
-  float* sums = f.db ? reinterpret_cast<float*>(base + g.sums) : nullptr;
+  float* sums = f.db && g.chunks > 1 ? reinterpret_cast<float*>(base + g.sums) : nullptr;
   hipError_t e = hipSuccess;
-  if (dz || sums) {
+  if (dz || f.db) {
     e = launch(dz_kernel<T>, (int64_t)g.chunks * ((f.d_out + 255) / 256), 256, s, f, dz, g.ld_dz, sums, g.rows_per);
     if (e == hipSuccess && sums) e = launch(db_kernel<T>, (f.d_out + 63) / 64, 1024, s, (const float*)sums, g.chunks, f.d_out, static_cast<T*>(f.db));
   }
