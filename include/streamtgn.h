@@ -340,7 +340,8 @@ int stgn_linear_grad(const stgn_linear_args *args, void *device_workspace, size_
  * list; values outside 0 .. q_len or k_len count as the nearer end.  Keys and values behind a list's end are not read.  Queries and dout rows
  * behind its end are not read either; their out and dq rows, and the dk and dv rows behind the keys' end, are zeros, their lse
  * -infinity.  A masked key inside its list's length may hold anything finite.
- * d_head <= 256, kv_heads divides heads; lists, q_len, k_len may be 0.
+ * d_head <= 256, kv_heads divides heads; lists, q_len, k_len may be 0; q_len, k_len <= 2^29, q_len * heads / kv_heads <= 2^30, and
+ * lists * kv_heads times the tiles of 64 rows or keys of a list < 2^23.
  * The gradient reads q, k, v, out, lse (as the forward call wrote them) and dout, and recomputes the softmax weights. */
 typedef struct {
   uint32_t dtype, causal, window;
@@ -356,7 +357,8 @@ typedef struct {
   void *dq, *dk, *dv;
 } stgn_attention_args;
 
-/* Workspace bytes of the forward call and of the gradient (each nullable), from dtype and sizes alone. */
+/* Workspace bytes of the forward call and of the gradient (each nullable), from dtype, sizes, causal and window; no pointer is
+ * followed. */
 int stgn_attention_workspace(const stgn_attention_args *args, size_t *forward_bytes, size_t *grad_bytes);
 int stgn_attention(const stgn_attention_args *args, void *device_workspace, size_t device_bytes, void *hip_stream);
 int stgn_attention_grad(const stgn_attention_args *args, void *device_workspace, size_t device_bytes, void *hip_stream);

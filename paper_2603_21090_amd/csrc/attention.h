@@ -560,6 +560,8 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void key_grad_kernel(AttnArgs a, i
     }
   }
   if (j0 >= l.kn) q1 = 0;
+  q0 = min(q0, l.qn);
+  q1 = max(q1, 0);
   const bool whole_tile = j0 + KEYS <= l.kn;
 
   typename El::Frag kf[NB][DP / El::KF], vf[NB][DP / El::KF];

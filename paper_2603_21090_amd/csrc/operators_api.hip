@@ -69,6 +69,7 @@ int check_workspace(size_t need, const void* ws, size_t bytes) {
   return STGN_OK;
 }
 
+constexpr uint64_t kMaxLen = 1u << 29;                        // sums of a position, a length and a window stay 32-bit numbers
 constexpr uint64_t kMaxRows = 1u << 30, kMaxWidth = 1u << 24, kMaxLd = 1ull << 40;
 constexpr uint64_t kMaxGroups = (1ull << 24) - 1;             // workgroups of 256 threads a launch may hold
 
@@ -159,11 +160,11 @@ int check_attention(const stgn_attention_args* a, bool grad, bool sizes_only) {
   if (a->heads > 65535) return no("heads out of range");
   if (a->causal > 1) return no("causal must be 0 or 1");
   if (a->window && !a->causal) return no("a window needs causal = 1");
-  if (a->lists > kMaxRows || a->q_len > kMaxRows || a->k_len > kMaxRows || a->window > kMaxRows) return no("lists, q_len, k_len or window out of range");
+  if (a->lists > kMaxRows || a->q_len > kMaxLen || a->k_len > kMaxLen) return no("lists, q_len or k_len out of range");
   const uint64_t rows = (uint64_t)a->q_len * (a->heads / a->kv_heads);
   if (rows > kMaxRows) return no("q_len times the heads that share a key head out of range");
   const uint64_t pairs = (uint64_t)a->lists * a->kv_heads;
-  if (((rows + 63) / 64) * pairs > kMaxGroups / 2 || (((uint64_t)a->k_len + 63) / 64) * pairs > kMaxGroups / 2)   // (of up to 512 threads)
+  if (pairs > kMaxGroups / 2 || ((rows + 63) / 64) * pairs > kMaxGroups / 2 || (((uint64_t)a->k_len + 63) / 64) * pairs > kMaxGroups / 2)   // (of up to 512 threads)
     return no("the lists have more tiles than a launch");
   if (sizes_only) return STGN_OK;
   if (!(a->scale == a->scale) || a->scale - a->scale != 0.0f) return no("scale must be finite");
@@ -221,7 +222,7 @@ AttnArgs attention_args(const stgn_attention_args* a) {
   t.lists = (int)a->lists; t.q_len = (int)a->q_len; t.k_len = (int)a->k_len;
   t.heads = (int)a->heads; t.kv_heads = (int)a->kv_heads; t.group = (int)(a->heads / a->kv_heads); t.d = (int)a->d_head;
   t.group_shift = (t.group & (t.group - 1)) == 0 ? __builtin_ctz((unsigned)t.group) : -1;
-  t.causal = (int)a->causal; t.window = (int)a->window; t.scale = a->scale;
+  t.causal = (int)a->causal; t.window = (int)(a->window < a->k_len ? a->window : a->k_len); t.scale = a->scale;
   return t;
 }
 
@@ -273,7 +274,7 @@ int stgn_attention_grad(const stgn_attention_args* args, void* device_workspace,
   if (const int rc = check_attention(args, true, false)) return rc;
   const AttnArgs a = attention_args(args);
   if (const int rc = check_workspace(attention_grad_bytes(a, (int)args->dtype), device_workspace, device_bytes)) return rc;
-  if (a.lists == 0) return STGN_OK;
+  if (a.lists == 0 || (a.q_len == 0 && a.k_len == 0)) return STGN_OK;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   if (few_rows(a, (int)args->dtype, true)) return finish(STGN_BY_TYPE(args->dtype, attention_rows_grad, a, device_workspace, s));
   return finish(STGN_BY_TYPE(args->dtype, attention_grad, a, device_workspace, s));

@@ -16,7 +16,9 @@ SHAPES = [
     (2, 65, 65, 4, 2, 100, True, 0, True), (2, 100, 37, 2, 1, 64, True, 0, True), (2, 37, 100, 2, 1, 33, True, 20, True),
     (1, 200, 200, 3, 3, 128, True, 0, False), (1, 200, 200, 3, 1, 96, False, 0, False), (2, 130, 190, 2, 2, 7, False, 0, True),
     (2, 150, 150, 4, 1, 72, True, 1, True), (1, 300, 300, 2, 1, 64, True, 64, True), (1, 70, 90, 1, 1, 200, True, 0, True),
-    (1, 129, 257, 2, 2, 256, False, 0, True),
+    (1, 129, 257, 2, 2, 256, False, 0, True), (2, 90, 20, 8, 1, 40, True, 5, True), (1, 3, 400, 24, 2, 48, True, 9, False),
+    (1, 20, 30, 16, 1, 100, True, 0, False), (2, 70, 300, 10, 2, 130, True, 50, True), (1, 2, 1500, 40, 1, 64, True, 0, False),
+    (1, 700, 9, 4, 2, 33, False, 0, False), (1, 5, 2500, 8, 2, 80, True, 600, True),
 ]
 
 

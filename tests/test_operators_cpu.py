@@ -57,7 +57,7 @@ def test_linear_grad_refuses(lib, bad):
 
 
 MASKS = [dict(dtype=3), dict(d_head=0), dict(d_head=257), dict(heads=0), dict(kv_heads=0), dict(heads=5), dict(causal=2), dict(window=3),
-         dict(lists=(1 << 30) + 1), dict(q_len=(1 << 30) + 1), dict(k_len=(1 << 30) + 1), dict(scale=float("nan")), dict(scale=float("inf")),
+         dict(lists=(1 << 30) + 1), dict(q_len=(1 << 29) + 1), dict(k_len=(1 << 29) + 1), dict(q_len=0, k_len=0, lists=1 << 23), dict(scale=float("nan")), dict(scale=float("inf")),
          dict(q=None), dict(k=None), dict(v=None), dict(out=None), dict(lse=None), dict(q=(3 << 20) + 1), dict(lse=(7 << 20) + 2),
          dict(q_lens=(1 << 20) + 2), dict(k_row=1 << 41), dict(lists=1 << 26, q_len=64)]
 
