@@ -216,12 +216,17 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product a) {
 // padded (two buffers of both operands are 128 KB); piece p (16 bytes) of row r lies at p ^ turn(r), which spreads what one read touches
 // over the banks: eight rows of a fragment along k, four rows of a transposed one.  Rows and columns past the edge repeat the last
 // ones and are not stored; k has whole tiles.
-template <class T, bool ROWS>
+// The column side's fragments come in pairs: of 32 columns the first holds 8 q + 0 .. 3 (q = 0 .. 3) and the second 8 q + 4 .. 7, so that a
+// lane's two accumulators are eight neighbouring outputs, and four lanes 64 bytes of a row.
+template <class T, bool ROWS, bool PAIRS>
 struct LargeMove {                                            // ROWS: [256 lines][64 of k], else [64 of k][256 lines]
   const T* at[4];
   u32x4 r[4];
   int64_t step;
-  static __device__ inline int turn(int row) { return ROWS ? row & 7 : ((row & 3) << 1) | (row & 8); }
+  static __device__ inline int turn(int row) {
+    if (PAIRS) return ROWS ? ((row >> 2) & 6) | ((row >> 1) & 1) : (row & 3) << 2;
+    return ROWS ? row & 7 : ((row & 3) << 1) | (row & 8);
+  }
   __device__ inline void start(const T* base, int64_t ld, int first, int lines, int k) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -245,11 +250,21 @@ struct LargeMove {                                            // ROWS: [256 line
       *reinterpret_cast<u32x4*>(tile + (p - piece + (piece ^ turn(row))) * 8) = r[i];
     }
   }
-  // fragment of 16 lines from `line`, elements k .. k + 31 of the tile
+  // fragment of 16 lines from `line` (PAIRS: of a pair's 32 lines, the first's or the second's), elements k .. k + 31 of the tile
   static __device__ inline typename Elem<T>::Frag frag(const T* tile, int line, int k) {
     const int lane = threadIdx.x & 63, g = lane >> 4, i = lane & 15;
-    if constexpr (ROWS) {
-      return *reinterpret_cast<const typename Elem<T>::Frag*>(tile + (line + i) * 64 + ((k / 8 + g) ^ (i & 7)) * 8);
+    if constexpr (PAIRS) {
+      const int pair = line & ~31, second = (line >> 4) & 1;
+      if constexpr (ROWS) {
+        const int r = 8 * (i >> 2) + 4 * second + (i & 3);
+        return *reinterpret_cast<const typename Elem<T>::Frag*>(tile + (pair + r) * 64 + ((k / 8 + g) ^ turn(r)) * 8);
+      } else {
+        const int row = k + 8 * g + (i >> 2);
+        const T* p = tile + row * 256 + ((pair / 8 + (i & 3)) ^ turn(row)) * 8 + 4 * second;
+        return join_transposed<T>(read_transposed(p), read_transposed(p + 4 * 256));
+      }
+    } else if constexpr (ROWS) {
+      return *reinterpret_cast<const typename Elem<T>::Frag*>(tile + (line + i) * 64 + ((k / 8 + g) ^ turn(i)) * 8);
     } else {
       const int row = k + 8 * g + (i >> 2);                   // and four further on: the same turn
       const T* p = tile + row * 256 + ((line / 8 + ((i & 3) >> 1)) ^ turn(row)) * 8 + (i & 1) * 4;
@@ -264,15 +279,14 @@ __global__ __launch_bounds__(512) void large_product_kernel(Product a) {
   __shared__ __attribute__((aligned(16))) T ls[2][TILE], rs[2][TILE];
   const int wave = threadIdx.x >> 6, wm = wave % 4 * 64, wn = wave / 4 * 128;
   const unsigned tm = (unsigned)(a.m + 255) / 256, tn = (unsigned)(a.n + 255) / 256;
-  const int split = (int)(blockIdx.x / (tm * tn));
   int row, col;
-  tile_of(blockIdx.x % (tm * tn), tm, tn, row, col);
-  const int m0 = row * 256, n0 = col * 256, kb = split * a.k_per, tiles = (min(a.k, kb + a.k_per) - kb) / BK;
+  tile_of(blockIdx.x, tm, tn, row, col);
+  const int m0 = row * 256, n0 = col * 256, tiles = a.k / BK;
 
-  LargeMove<T, L_ROWS> ml;
-  LargeMove<T, R_ROWS> mr;
-  ml.start(static_cast<const T*>(a.l), a.ld_l, n0, a.n, kb);
-  mr.start(static_cast<const T*>(a.r), a.ld_r, m0, a.m, kb);
+  LargeMove<T, L_ROWS, true> ml;
+  LargeMove<T, R_ROWS, false> mr;
+  ml.start(static_cast<const T*>(a.l), a.ld_l, n0, a.n, 0);
+  mr.start(static_cast<const T*>(a.r), a.ld_r, m0, a.m, 0);
   floatx4 acc[NB][MB];
 #pragma unroll
   for (int x = 0; x < NB; ++x)
@@ -308,7 +322,31 @@ __global__ __launch_bounds__(512) void large_product_kernel(Product a) {
       mr.store(rs[(t + 1) & 1]);
     }
   }
-  finish_tile<T, NB, MB>(a, split, m0 + wm, n0 + wn, acc);
+
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int y = 0; y < MB; ++y) {
+    __builtin_amdgcn_sched_barrier(0);
+    const int64_t m = m0 + wm + y * 16 + (lane & 15);
+    if (m >= a.m) continue;
+    auto each = [&](auto f) {
+#pragma unroll
+      for (int x = 0; x < NB; x += 2) {
+        const int n = n0 + wn + x * 16 + 8 * (lane >> 4);
+        if (n < a.n) f(n, acc[x][y], acc[x + 1][y]);
+      }
+    };
+    if (a.bias) each([&](int n, floatx4& u, floatx4& v) { add8(static_cast<const T*>(a.bias), n, a.n, u, v); });
+    if (a.pre) each([&](int n, floatx4& u, floatx4& v) { store8(static_cast<T*>(a.pre) + m * a.ld_pre, n, a.n, u, v); });
+    switch (a.act) {
+      case ACT_RELU: each([&](int, floatx4& u, floatx4& v) { activate<T, ACT_RELU>(u); activate<T, ACT_RELU>(v); }); break;
+      case ACT_GELU: each([&](int, floatx4& u, floatx4& v) { activate<T, ACT_GELU>(u); activate<T, ACT_GELU>(v); }); break;
+      case ACT_SILU: each([&](int, floatx4& u, floatx4& v) { activate<T, ACT_SILU>(u); activate<T, ACT_SILU>(v); }); break;
+      default: break;
+    }
+    if (a.residual) each([&](int n, floatx4& u, floatx4& v) { add8(static_cast<const T*>(a.residual) + m * a.ld_res, n, a.n, u, v); });
+    each([&](int n, floatx4& u, floatx4& v) { store8(static_cast<T*>(a.out) + m * a.ld_out, n, a.n, u, v); });
+  }
 }
 
 // Sums of the splits, in their order, and the epilogue: four outputs a thread, or where the splits are many four outputs a lane, the four

@@ -220,6 +220,31 @@ __device__ inline floatx4 load4(const T* row, int col, int cols) {
   return v;
 }
 
+// eight neighbouring elements of 16-bit types: 16 bytes a lane
+template <class T>
+__device__ inline void add8(const T* row, int col, int cols, floatx4& u, floatx4& v) {
+  if (col + 8 <= cols) {
+    const typename Elem<T>::Frag f = __builtin_bit_cast(typename Elem<T>::Frag, *reinterpret_cast<const u32x4_any*>(row + col));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { u[j] += (float)f[j]; v[j] += (float)f[j + 4]; }
+  } else {
+    u += load4(row, col, cols);
+    if (col + 4 < cols) v += load4(row, col + 4, cols);
+  }
+}
+template <class T>
+__device__ inline void store8(T* row, int col, int cols, const floatx4& u, const floatx4& v) {
+  if (col + 8 <= cols) {
+    typename Elem<T>::Frag f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { f[j] = (T)u[j]; f[j + 4] = (T)v[j]; }
+    *reinterpret_cast<u32x4_any*>(row + col) = __builtin_bit_cast(u32x4_any, f);
+  } else {
+    store4(row, col, cols, u);
+    if (col + 4 < cols) store4(row, col + 4, cols, v);
+  }
+}
+
 // An operand of a product on its way from global memory through registers into LDS, tile after tile along the summed index k: LINES of
 // the output's rows or columns, BK elements of k.  ALONG: k runs along the matrix's rows, a tile is [LINES][BK]; else it has a row per k, a tile is
 // [BK][LINES].  Every thread carries NP pieces of 16 bytes.  Lines and elements that the matrix does not have are zeros: what lies there

@@ -114,3 +114,28 @@ def test_the_same_bits_again_on_another_stream_and_in_a_graph(dt):
         torch.cuda.synchronize()
         for a, c in zip(kept, eager):
             assert torch.equal(a, c)
+
+
+# products of many tiles: 256 x 256 (16-bit types, whole tiles of k; edges in both directions), 128 rows by 128, 112, 96 and 64 columns
+LARGE = [(4100, 64, 4104), (3970, 192, 4360), (4000, 100, 1030), (33000, 20, 112), (33000, 33, 96), (33000, 20, 40), (20000, 70, 200)]
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=str)
+@pytest.mark.parametrize("size", LARGE, ids=str)
+def test_forward_of_many_tiles(size, dt):
+    x, w, b, r, _ = make(*size, dt)
+    y, z = refs.linear(x, w, b, "gelu", r)
+    got = binding.linear(x.cuda(), w.cuda(), bias=b.cuda(), activation="gelu", residual=r.cuda(), keep_pre=True)
+    refs.within(got[0], y, "y")
+    refs.within(got[1], z, "pre")
+    refs.within(binding.linear(x.cuda(), w.cuda()), refs.linear(x, w, None, "none", None)[0], "no epilogue")
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=str)
+@pytest.mark.parametrize("size", [(4100, 4099, 64), (128, 4104, 4112), (192, 4360, 3976), (20000, 372, 200), (17000, 300, 420), (4000, 1030, 100)], ids=str)
+def test_gradients_of_many_tiles(size, dt):
+    """dx with an odd width, dW from whole tiles of k, long sums cut for 128-row tiles."""
+    x, w, b, z, dy = make(*size, dt)
+    got = binding.linear_grad(dy.cuda(), x.cuda(), w.cuda(), activation="relu", pre=z.cuda())
+    for g, want, what in zip(got, refs.linear_grad(dy, x, w, "relu", z), ("dx", "dw", "db")):
+        refs.within(g, want, what)
