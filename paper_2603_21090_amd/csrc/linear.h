@@ -387,15 +387,26 @@ __global__ __launch_bounds__(256) void dz_kernel(LinearGradArgs a, T* dz, int64_
   const int64_t m1 = min((int64_t)a.rows, (int64_t)(chunk + 1) * rows_per);
   floatx4 acc = {0.f, 0.f, 0.f, 0.f};
   if (n < a.d_out) {
-    for (int64_t m = (int64_t)chunk * rows_per + wave; m < m1; m += 4) {
-      floatx4 v = load4(static_cast<const T*>(a.dy) + m * a.ld_dy, n, a.d_out);
-      if (dz) {
-        const floatx4 z = load4(static_cast<const T*>(a.pre) + m * a.ld_pre, n, a.d_out);
+    constexpr int U = 4;                                      // rows requested at once
+    for (int64_t m = (int64_t)chunk * rows_per + wave; m < m1; m += 4 * U) {
+      floatx4 v[U], z[U];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] *= act_slope<T>(a.act, z[j]);
-        store4(dz + m * ld_dz, n, a.d_out, v);
+      for (int u = 0; u < U; ++u) {
+        v[u] = z[u] = floatx4{0.f, 0.f, 0.f, 0.f};
+        if (m + 4 * u >= m1) continue;
+        v[u] = load4(static_cast<const T*>(a.dy) + (m + 4 * u) * a.ld_dy, n, a.d_out);
+        if (dz) z[u] = load4(static_cast<const T*>(a.pre) + (m + 4 * u) * a.ld_pre, n, a.d_out);
       }
-      acc += v;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (m + 4 * u >= m1) continue;
+        if (dz) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[u][j] *= act_slope<T>(a.act, z[u][j]);
+          store4(dz + (m + 4 * u) * ld_dz, n, a.d_out, v[u]);
+        }
+        acc += v[u];
+      }
     }
   }
   if (!a.db) return;
@@ -413,8 +424,10 @@ __global__ __launch_bounds__(1024) void db_kernel(const float* sums, int chunks,
   __shared__ float wsum[16][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (int)blockIdx.x * 64 + lane;
   float acc = 0.f;
-  if (c < n)
+  if (c < n) {
+#pragma unroll 8
     for (int i = wave; i < chunks; i += 16) acc += sums[(int64_t)i * n + c];
+  }
   wsum[wave][lane] = acc;
   __syncthreads();
   if (wave == 0 && c < n) {
