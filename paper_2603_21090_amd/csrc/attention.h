@@ -247,13 +247,12 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void forward_kernel(A
         for (int y = 0; y < KB; ++y)
 #pragma unroll
           for (int u = 0; u < 4; ++u) top[c] = fmaxf(top[c], s[y][c][u]);
-        top[c] = over_groups_max(top[c]) * scale2;
-        grows |= top[c] > m[c] + kLazy;
+        grows |= top[c] * scale2 > m[c] + kLazy;              // (a lane's own scores: the row's largest is among them in some lane)
       }
       if (__any(grows)) {
 #pragma unroll
         for (int c = 0; c < NB; ++c) {
-          const float next = fmaxf(m[c], top[c]);
+          const float next = fmaxf(m[c], over_groups_max(top[c]) * scale2);
           const float shrink = __builtin_amdgcn_exp2f(m[c] - (next == -INFINITY ? 0.f : next));
           m[c] = next;
           sum[c] *= shrink;

@@ -144,11 +144,12 @@ template <class T> constexpr int kTileK = 128 / (int)sizeof(T);    // 64 16-bit 
 // DEPTH tiles of k are on their way in registers while one is multiplied: where tiles are small and few, what a tile takes is the wait
 // for memory (13 x 4,096 x 11,008 in bf16: 26.6 us with one, 19.9 with three).
 template <class T, int BM, int BN, int WM, int WN, int DEPTH, bool L_ROWS, bool R_ROWS>
-__global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product a) {
+__global__ __launch_bounds__(WM * WN * 64, 2) void product_kernel(Product a) {
   using El = Elem<T>;
   constexpr int BK = kTileK<T>, THREADS = WM * WN * 64, MB = BM / WM / 16, NB = BN / WN / 16;
   constexpr int SL = lds_stride<T>(L_ROWS ? BK : BN), SR = lds_stride<T>(R_ROWS ? BK : BM);
-  __shared__ __attribute__((aligned(16))) T ls[(L_ROWS ? BN : BK) * SL], rs[(R_ROWS ? BM : BK) * SR];
+  constexpr int BUFS = DEPTH == 1 ? 2 : 1;
+  __shared__ __attribute__((aligned(16))) T ls[BUFS][(L_ROWS ? BN : BK) * SL], rs[BUFS][(R_ROWS ? BM : BK) * SR];
   const int wave = threadIdx.x >> 6, wm = wave % WM * MB * 16, wn = wave / WM * NB * 16;
   const unsigned tm = (unsigned)(a.m + BM - 1) / BM, tn = (unsigned)(a.n + BN - 1) / BN;
   const int split = (int)(blockIdx.x / (tm * tn));
@@ -175,36 +176,58 @@ __global__ __launch_bounds__(WM * WN * 64) void product_kernel(Product a) {
 #pragma unroll
     for (int y = 0; y < MB; ++y) acc[x][y] = floatx4{0.f, 0.f, 0.f, 0.f};
 
+  auto multiply = [&](const T* l, const T* r) {
 #pragma unroll
-  for (int d = 0; d < DEPTH; ++d)
-    if (kb + d * BK < ke) fetch(d, kb + d * BK);
-  for (int kt = kb; kt < ke; kt += DEPTH * BK) {
+    for (int s = 0; s < BK; s += El::KF) {
+      typename El::Frag lf[NB], rf[MB];
 #pragma unroll
-    for (int d = 0; d < DEPTH; ++d) {
-      const int k = kt + d * BK;
-      if (k >= ke) break;
+      for (int x = 0; x < NB; ++x) {
+        if constexpr (L_ROWS) lf[x] = frag_rows(l, SL, wn + x * 16, s);
+        else lf[x] = frag_cols<T, false>(l, SL, s, wn + x * 16);
+      }
+#pragma unroll
+      for (int y = 0; y < MB; ++y) {
+        if constexpr (R_ROWS) rf[y] = frag_rows(r, SR, wm + y * 16, s);
+        else rf[y] = frag_cols<T, false>(r, SR, s, wm + y * 16);
+      }
+#pragma unroll
+      for (int x = 0; x < NB; ++x)
+#pragma unroll
+        for (int y = 0; y < MB; ++y) acc[x][y] = El::mma(lf[x], rf[y], acc[x][y]);
+    }
+  };
+  if constexpr (DEPTH == 1) {                                 // two buffers in LDS, one barrier a tile
+    if (kb < ke) {
+      fetch(0, kb);
+      MoveL::store(ls[0], rl[0]);
+      MoveR::store(rs[0], rr[0]);
+    }
+    int buf = 0;
+    for (int k = kb; k < ke; k += BK, buf ^= 1) {
       __syncthreads();
-      MoveL::store(ls, rl[d]);
-      MoveR::store(rs, rr[d]);
-      __syncthreads();
-      if (k + DEPTH * BK < ke) fetch(d, k + DEPTH * BK);
+      const bool more = k + BK < ke;
+      if (more) fetch(0, k + BK);
+      multiply(ls[buf], rs[buf]);
+      if (more) {
+        MoveL::store(ls[buf ^ 1], rl[0]);
+        MoveR::store(rs[buf ^ 1], rr[0]);
+      }
+    }
+  } else {
 #pragma unroll
-      for (int s = 0; s < BK; s += El::KF) {
-        typename El::Frag lf[NB], rf[MB];
+    for (int d = 0; d < DEPTH; ++d)
+      if (kb + d * BK < ke) fetch(d, kb + d * BK);
+    for (int kt = kb; kt < ke; kt += DEPTH * BK) {
 #pragma unroll
-        for (int x = 0; x < NB; ++x) {
-          if constexpr (L_ROWS) lf[x] = frag_rows(ls, SL, wn + x * 16, s);
-          else lf[x] = frag_cols<T, false>(ls, SL, s, wn + x * 16);
-        }
-#pragma unroll
-        for (int y = 0; y < MB; ++y) {
-          if constexpr (R_ROWS) rf[y] = frag_rows(rs, SR, wm + y * 16, s);
-          else rf[y] = frag_cols<T, false>(rs, SR, s, wm + y * 16);
-        }
-#pragma unroll
-        for (int x = 0; x < NB; ++x)
-#pragma unroll
-          for (int y = 0; y < MB; ++y) acc[x][y] = El::mma(lf[x], rf[y], acc[x][y]);
+      for (int d = 0; d < DEPTH; ++d) {
+        const int k = kt + d * BK;
+        if (k >= ke) break;
+        __syncthreads();
+        MoveL::store(ls[0], rl[d]);
+        MoveR::store(rs[0], rr[d]);
+        __syncthreads();
+        if (k + DEPTH * BK < ke) fetch(d, k + DEPTH * BK);
+        multiply(ls[0], rs[0]);
       }
     }
   }
