@@ -169,6 +169,11 @@ __global__ __launch_bounds__(256) void rows_forward_kernel(AttnArgs a, RowPlan p
     float s[R][U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+      if (!WIDE && base + u * G >= k1) {                      // (the same for all lanes)
+#pragma unroll
+        for (int r = 0; r < R; ++r) s[r][u] = -INFINITY;
+        continue;
+      }
       float f[E];
       spread<T>(kr[u], f);
       const int j = base + u * G + slot;
@@ -196,6 +201,7 @@ __global__ __launch_bounds__(256) void rows_forward_kernel(AttnArgs a, RowPlan p
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+      if (!WIDE && base + u * G >= k1) continue;
       float f[E];
       spread<T>(vr[u], f);
 #pragma unroll
@@ -422,15 +428,18 @@ inline size_t row_part_bytes(const AttnArgs& a, bool grad) {
 template <class T, int L, int R, bool GRAD>
 hipError_t rows_launch(const AttnArgs& a, float* part, hipStream_t s) {
   constexpr int U = R >= 8 ? 2 : 4;                           // (more rows, fewer registers for keys in flight)
+  // short fp32 lists' gradients: eight, all keys of most lists at once (40,000 lists of twenty, heads of 50: 318 -> 300 us; the forward call
+  // loses a sixth by it)
+  constexpr int US = GRAD && R == 1 && sizeof(T) == 4 ? 8 : U;
   const RowPlan p = row_plan(a);
   const int64_t units = (int64_t)a.lists * a.kv_heads, rows = (int64_t)a.q_len * a.group;
   hipError_t e;
   if constexpr (GRAD)
     e = wide_rows(a) ? launch(rows_grad_kernel<T, L, R, U, true>, units * p.splits, 256, s, a, p, part)
-                     : launch(rows_grad_kernel<T, L, R, U, false>, (units + 3) / 4, 256, s, a, p, part);
+                     : launch(rows_grad_kernel<T, L, R, US, false>, (units + 3) / 4, 256, s, a, p, part);
   else
     e = wide_rows(a) ? launch(rows_forward_kernel<T, L, R, U, true>, units * p.splits, 256, s, a, p, part)
-                     : launch(rows_forward_kernel<T, L, R, U, false>, (units + 3) / 4, 256, s, a, p, part);
+                     : launch(rows_forward_kernel<T, L, R, US, false>, (units + 3) / 4, 256, s, a, p, part);
   if (e != hipSuccess || p.splits == 1) return e;
   if constexpr (GRAD) return sum_runs<T>(a, a.dq, nullptr, a.q_len, a.group, p.splits, part, s);
   else return launch(join_kernel<T>, join_grid(units * rows, p.splits), 256, s, a, p.splits, (const float*)part);
