@@ -311,7 +311,8 @@ enum { STGN_ACT_NONE = 0, STGN_ACT_RELU = 1, STGN_ACT_GELU = 2 /* z Phi(z), by e
  * whose pointer is NULL is not computed (the residual's is dy).  relu's slope at 0 is 0.
  * x: [rows x d_in]; w: [d_in x d_out]; bias, db: [d_out]; residual, y, pre, dy: [rows x d_out]; rows lie ld_* elements apart, the
  * numbers of a row side by side; dx and dw are dense.  bias and residual may be NULL.  rows may be 0 (dw and db are then
- * zeros), d_in and d_out lie in 1 .. 2^24.  Outputs overlap nothing, except that y may be the residual itself. */
+ * zeros), d_in and d_out lie in 1 .. 2^24.  Outputs overlap nothing, except that y may be the residual itself; x, residual, y and pre of equal
+ * ld_* may be different columns of one matrix. */
 typedef struct {
   uint32_t dtype, activation;
   uint32_t rows, d_in, d_out;

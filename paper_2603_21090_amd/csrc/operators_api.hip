@@ -59,6 +59,11 @@ Span span_of(const void* p, uint64_t rows, uint64_t width, uint64_t ld, size_t e
   return {static_cast<const char*>(p), p && rows && width ? ((rows - 1) * ld + width) * es : 0};
 }
 bool meet(const Span& x, const Span& y) { return x.n && y.n && x.a < y.a + y.n && y.a < x.a + x.n; }
+// rows of x and y, both `ld` bytes apart, whose columns lie side by side in one wider matrix
+bool beside(const Span& x, size_t x_width, const Span& y, size_t y_width, size_t ld) {
+  const size_t to_y = y.a >= x.a ? (size_t)(y.a - x.a) % ld : (ld - (size_t)(x.a - y.a) % ld) % ld;
+  return to_y >= x_width && to_y + y_width <= ld;
+}
 
 int finish(hipError_t e) { return e == hipSuccess ? STGN_OK : fail_operator(STGN_E_DEVICE, hipGetErrorString(e)); }
 
@@ -99,7 +104,13 @@ int check_linear(const stgn_linear_args* a, bool grad, bool sizes_only) {
     const Span y = span_of(a->y, a->rows, a->d_out, a->ld_y, es), p = span_of(a->pre, a->rows, a->d_out, a->ld_pre, es),
                b = span_of(a->bias, 1, a->d_out, 0, es), r = span_of(a->residual, a->rows, a->d_out, a->ld_residual, es);
     const bool in_place = a->residual == a->y && a->ld_residual == a->ld_y;
-    if (meet(y, x) || meet(y, w) || meet(y, b) || meet(y, p) || meet(p, x) || meet(p, w) || meet(p, b) || meet(p, r) || (!in_place && meet(y, r)))
+    // (matrices of rows the same distance apart may be columns of one)
+    const auto hit = [&](const Span& s, uint64_t sw, uint64_t sl, const Span& t, uint64_t tw, uint64_t tl) {
+      return meet(s, t) && !(sl == tl && beside(s, sw * es, t, tw * es, sl * es));
+    };
+    const uint64_t in = a->d_in, n = a->d_out;
+    if (hit(y, n, a->ld_y, x, in, a->ld_x) || hit(y, n, a->ld_y, p, n, a->ld_pre) || hit(p, n, a->ld_pre, x, in, a->ld_x) ||
+        hit(p, n, a->ld_pre, r, n, a->ld_residual) || (!in_place && hit(y, n, a->ld_y, r, n, a->ld_residual)) || meet(y, w) || meet(y, b) || meet(p, w) || meet(p, b))
       return no("an output overlaps an input or the other output (y may be exactly the residual)");
     return STGN_OK;
   }

@@ -139,3 +139,29 @@ def test_gradients_of_many_tiles(size, dt):
     got = binding.linear_grad(dy.cuda(), x.cuda(), w.cuda(), activation="relu", pre=z.cuda())
     for g, want, what in zip(got, refs.linear_grad(dy, x, w, "relu", z), ("dx", "dw", "db")):
         refs.within(g, want, what)
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=str)
+@pytest.mark.parametrize("size", [(90, 77, 45), (3, 2000, 65), (4200, 128, 4104)], ids=str)
+def test_columns_of_one_matrix(size, dt):
+    """x, pre, residual and y (in the residual's place) as columns of one matrix: the columns between them stay as they were."""
+    import ctypes as C
+    rows, d_in, d_out = size
+    x, w, b, r, _ = make(*size, dt)
+    ld, at = d_in + 2 * d_out + 5, (1, d_in + 3, d_in + d_out + 4)
+    m = torch.full((rows, ld), 7.0, dtype=dt, device="cuda")
+    m[:, at[0]:at[0] + d_in], m[:, at[2]:at[2] + d_out] = x.cuda(), r.cuda()
+    w, b = w.cuda(), b.cuda()
+    p = [m.data_ptr() + c * m.element_size() for c in at]
+    a = binding.LinearArgs(dtype=TYPES.index(dt), activation=3, rows=rows, d_in=d_in, d_out=d_out, ld_x=ld, ld_w=d_out, ld_residual=ld, ld_y=ld, ld_pre=ld,
+                           x=p[0], w=w.data_ptr(), bias=b.data_ptr(), residual=p[2], y=p[2], pre=p[1])
+    lib, n = binding.load_library(), C.c_size_t(0)
+    assert lib.stgn_linear_workspace(C.byref(a), C.byref(n), None) == 0
+    ws = torch.empty(n.value, dtype=torch.uint8, device="cuda")
+    assert lib.stgn_linear(C.byref(a), ws.data_ptr() if n.value else None, n.value, torch.cuda.current_stream().cuda_stream) == 0, lib.stgn_last_error(None)
+    y, z = refs.linear(x, w.cpu(), b.cpu(), "silu", r)
+    refs.within(m[:, at[2]:at[2] + d_out], y, "y")
+    refs.within(m[:, at[1]:at[1] + d_out], z, "pre")
+    assert torch.equal(m[:, at[0]:at[0] + d_in].cpu(), x)
+    for c in (0, at[0] + d_in, at[0] + d_in + 1, at[1] + d_out):
+        assert (m[:, c] == 7).all()
