@@ -199,8 +199,9 @@ int check_attention(const stgn_attention_args* a, bool grad, bool sizes_only) {
   const Span q = reach(a->q, a->q_len, a->heads, a->q_list, a->q_row, a->q_head), k = reach(a->k, a->k_len, a->kv_heads, a->k_list, a->k_row, a->k_head),
              v = reach(a->v, a->k_len, a->kv_heads, a->v_list, a->v_row, a->v_head);
   const Span o = reach(a->out, a->q_len, a->heads, a->out_list, a->out_row, a->out_head), lse = span_of(a->lse, 1, nq, 0, 4);
+  const Span ql = span_of(a->q_lens, 1, a->lists, 0, 4), kl = span_of(a->k_lens, 1, a->lists, 0, 4);
   if (!grad) {
-    for (const Span& s : {q, k, v})
+    for (const Span& s : {q, k, v, ql, kl})
       if (meet(o, s) || meet(lse, s)) return no("an output overlaps an input");
     if (meet(o, lse)) return no("out and lse overlap");
     if (have_q && !apart(a->lists, a->out_list, a->q_len, a->out_row, a->heads, a->out_head, a->d_head)) return no("two numbers of out share a place");
@@ -212,7 +213,7 @@ int check_attention(const stgn_attention_args* a, bool grad, bool sizes_only) {
   const Span d = reach(a->dout, a->q_len, a->heads, a->dout_list, a->dout_row, a->dout_head);
   const Span out[] = {span_of(a->dq, 1, nq * a->d_head, 0, es), span_of(a->dk, 1, nk * a->d_head, 0, es), span_of(a->dv, 1, nk * a->d_head, 0, es)};
   for (int i = 0; i < 3; ++i) {
-    for (const Span& s : {q, k, v, o, lse, d})
+    for (const Span& s : {q, k, v, o, lse, d, ql, kl})
       if (meet(out[i], s)) return no("a gradient overlaps an input");
     for (int j = 0; j < i; ++j)
       if (meet(out[i], out[j])) return no("two gradients overlap");

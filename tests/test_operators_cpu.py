@@ -75,6 +75,34 @@ def test_attention_grad_refuses(lib, bad):
     assert lib.stgn_last_error(None)
 
 
+@pytest.mark.parametrize("bad", [dict(x=1 << 20, y=(1 << 20) + 126), dict(x=1 << 20, y=(1 << 20) + 2 * 65), dict(y=1 << 20, x=(1 << 20) + 62),
+                                 dict(x=1 << 20, y=(1 << 20) + 2 * 96 * 7 + 126), dict(x=1 << 20, y=(1 << 20) + 128, ld_y=97),
+                                 dict(pre=1 << 20, residual=(1 << 20) + 2, ld_pre=96, ld_residual=96)], ids=str)
+def test_columns_of_one_matrix_that_overlap_are_refused(lib, bad):
+    assert lib.stgn_linear(C.byref(linear_args(**{**dict(ld_x=96, ld_y=96), **bad})), None, 0, None) == INVALID
+    assert b"overlaps" in lib.stgn_last_error(None)
+
+
+def test_lengths_are_inputs_that_outputs_may_not_overlap(lib):
+    for bad in (dict(out=1 << 20), dict(lse=2 << 20), dict(lse=(2 << 20) + 4)):
+        assert lib.stgn_attention(C.byref(attention_args(**bad)), None, 0, None) == INVALID
+    for bad in (dict(dq=1 << 20), dict(dk=2 << 20), dict(dv=(1 << 20) + 4)):
+        assert lib.stgn_attention_grad(C.byref(attention_args(**bad)), None, 0, None) == INVALID
+
+
+def test_a_failed_create_is_told_to_threads_without_failures(lib):
+    import threading
+    seen, n = [], C.c_size_t(0)
+
+    def other():
+        seen.append((lib.stgn_query_workspace(None, C.byref(n)), lib.stgn_last_error(None)))
+    for read in (other, lambda: seen.append(lib.stgn_last_error(None))):
+        t = threading.Thread(target=read)
+        t.start()
+        t.join()
+    assert seen[0][0] == INVALID and seen[0][1] and seen[1] == seen[0][1]
+
+
 def test_null_arguments_and_workspaces(lib):
     n = C.c_size_t(0)
     for op, args in (("linear", linear_args(activation=2)), ("attention", attention_args())):
