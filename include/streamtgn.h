@@ -336,7 +336,7 @@ int stgn_linear_grad(const stgn_linear_args *args, void *device_workspace, size_
  * w of those.  s_ij = scale q_i . k_j, lse_i = log sum_j exp s_ij, out_i = sum_j exp(s_ij - lse_i) v_j.  A query that sees no key
  * has out = 0, lse = -infinity and gives no gradient.
  * q, out, dout: [lists x q_len x heads x d_head], k, v: [lists x k_len x kv_heads x d_head], element strides for list, row and head
- * (inputs: 0 is the same for all; no two numbers of out share a place), the numbers of a head side by side; query head h reads key
+ * (inputs: 0 is the same for all; no two numbers of out share a place, and none lies between the first and the last of an input), the numbers of a head side by side; query head h reads key
  * head h / (heads / kv_heads).  dq (as q) and dk, dv (as k) are dense; lse: dense fp32 [lists x heads x q_len].  q_lens, k_lens: int32 [lists], NULL: q_len, k_len for every
  * list; values outside 0 .. q_len or k_len count as the nearer end.  Keys and values behind a list's end are not read.  Queries and dout rows
  * behind its end are not read either; their out and dq rows, and the dk and dv rows behind the keys' end, are zeros, their lse

@@ -18,7 +18,8 @@ namespace {
 const char* const kClassNames[KC_COUNT] = {"stage_sort", "memory_update", "apply", "plan", "expand", "compact",
                                            "layer", "gather_rows", "noop", "project", "predict", "bucket_rows"};
 
-thread_local std::string g_create_error;   // of the thread's last failed call without a context
+std::string g_create_error;
+thread_local std::string t_error;   // of the thread's last failed call without a context
 
 constexpr size_t kRowIoBytes = 1u << 20;   // pinned block of stgn_ctx::row_io
 
@@ -78,7 +79,7 @@ struct stgn_ctx {
 namespace {
 
 int fail(stgn_ctx* c, int code, const std::string& msg) {
-  if (c) c->err = msg; else g_create_error = msg;
+  if (c) c->err = msg; else t_error = g_create_error = msg;
   return code;
 }
 
@@ -491,7 +492,7 @@ int sync_and_poll(stgn_ctx* ctx) {
 }  // namespace
 
 int stgn::fail_operator(int code, const char* why) {
-  g_create_error = why;
+  t_error = why;
   return code;
 }
 
@@ -507,7 +508,9 @@ int stgn_probe_gather(const float* table, uint64_t n_rows, uint32_t row_bytes, c
   return hipGetLastError() == hipSuccess ? STGN_OK : STGN_E_DEVICE;
 }
 
-const char* stgn_last_error(const stgn_ctx* ctx) { return ctx ? ctx->err.c_str() : g_create_error.c_str(); }
+const char* stgn_last_error(const stgn_ctx* ctx) {
+  return ctx ? ctx->err.c_str() : t_error.empty() ? g_create_error.c_str() : t_error.c_str();
+}
 
 int stgn_query_workspace(const stgn_config* cfg, size_t* device_bytes) {
   std::string why;
@@ -553,7 +556,7 @@ int stgn_create(const stgn_config* cfg, const stgn_weights* w, const float* node
   memset(&ctx->d, 0, sizeof(Dev));
   layout(*cfg, (char*)device_workspace, &ctx->d);
   ctx->stream = (hipStream_t)hip_stream;
-  auto bail = [&](int code) { g_create_error = ctx->err; stgn_destroy(ctx); return code; };
+  auto bail = [&](int code) { t_error = g_create_error = ctx->err; stgn_destroy(ctx); return code; };
 
   ctx->pin_bytes = stage_bytes(*cfg);
   for (int i = 0; i < 2; ++i) {
