@@ -210,7 +210,9 @@ int stgn_set_predictor(stgn_ctx *ctx, const float *w, float b);
  * hidden: 1 .. STGN_MAX_HIDDEN; activation: STGN_ACT_*; w1: host [2 * d_emb x hidden], b1, w2: host [hidden]; copied.  The head's
  * parameters and the rows of a batch lie in a workspace of the caller's on the context's device, 256-byte aligned, of the size
  * stgn_predictor_mlp_workspace tells; it must outlive every prediction until the next stgn_set_predictor or stgn_set_predictor_mlp call, or
- * the context.  The last head set is the one that scores.  May be called again at any time; synchronises the stream. */
+ * the context.  The last head set is the one that scores.  May be called again at any time; synchronises the stream.  A captured prediction
+ * keeps the head, its shape and its workspace, that was set when it was captured; another call with the same workspace, hidden and activation
+ * gives it new parameters. */
 #define STGN_MAX_HIDDEN 4096
 int stgn_predictor_mlp_workspace(stgn_ctx *ctx, uint32_t hidden, size_t *device_bytes);
 int stgn_set_predictor_mlp(stgn_ctx *ctx, uint32_t hidden, uint32_t activation, const float *w1, const float *b1,

@@ -352,6 +352,7 @@ class StreamTGN:
         nbytes = query_workspace(cfg)
         self.workspace_bytes = nbytes
         self._ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+        self._head_ws = {}
         base = (self._ws.data_ptr() + 255) & ~255
         self._stream = stream if stream is not None else torch.cuda.current_stream(self.device)
         w, keep = _marshal_weights(weights, cfg.layers, cfg.d_mem > 0)
@@ -442,10 +443,12 @@ class StreamTGN:
         assert w1.shape == (2 * self.cfg.d_emb, hidden) and b1.shape == (hidden,) and w2.shape == (hidden,)
         n = C.c_size_t(0)
         self._check(self._L.stgn_predictor_mlp_workspace(self._h, hidden, C.byref(n)))
-        ws = self._torch.empty(n.value + 256, dtype=self._torch.uint8, device=self.device)
+        # one workspace a width, kept: captured predictions go on reading it, with the parameters set last for that width
+        ws = self._head_ws.get(hidden)
+        if ws is None:
+            ws = self._head_ws[hidden] = self._torch.empty(n.value + 256, dtype=self._torch.uint8, device=self.device)
         self._check(self._L.stgn_set_predictor_mlp(self._h, hidden, ACTIVATIONS[activation], _ptr(w1), _ptr(b1), _ptr(w2), float(b2),
                                                    C.c_void_p((ws.data_ptr() + 255) & ~255), n.value))
-        self._head_ws = ws
 
     def predict_batch(self, src, dst, ts, at_edge_time=False):
         """Link scores of edges that have not been ingested yet: numpy in, numpy out (synchronises), or

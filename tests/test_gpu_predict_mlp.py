@@ -125,6 +125,36 @@ def test_a_captured_call_follows_the_state(mode):
     g.close()
 
 
+def test_captured_heads_keep_their_width_and_take_new_parameters():
+    w, g, edges = make()
+    side = torch.cuda.Stream()
+    out = torch.zeros(edges[0].shape[0], device="cuda")
+    with torch.cuda.stream(side):
+        st = synth.EdgeStream(w)
+        h = binding.StreamTGN.from_workload(w, synth.make_weights(w), synth.node_features(w), stream=side)
+        for b in range(6):
+            h.ingest_batch(*st.batch(b))
+        h.set_predictor_mlp(*head(w, 24))
+        first = h.predict_batch(*edges)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            h.predict_batch_static(*edges, out=out)
+        h.set_predictor_mlp(*head(w, 100))                    # another width: the captured one's parameters stay
+        filler = [torch.full((1 << 16,), float("nan"), device="cuda") for _ in range(8)]
+        for _ in range(3):
+            graph.replay()
+            side.synchronize()
+            assert torch.equal(out, first)
+        h.set_predictor_mlp(*head(w, 24, seed=5))             # the same: new ones
+        want = h.predict_batch(*edges)
+        graph.replay()
+        side.synchronize()
+        assert torch.equal(out, want) and not torch.equal(out, first)
+        del filler
+    h.close()
+    g.close()
+
+
 def test_refusals():
     w, g, _ = make()
     L, h = binding.load_library(), g._h
