@@ -203,8 +203,8 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void forward_kernel(A
   if (kt < k1) {
     mk.fetch(l.kn - kt, end);
     mv.fetch(l.kn - kt, end);
-    mk.store(ks[0]);
-    mv.store(vs[0]);
+    mk.store(ks[0], end);
+    mv.store(vs[0], end);
   }
   for (; kt < k1; kt += BK, buf ^= 1) {
     __syncthreads();                                          // this tile is there, and nobody reads the other buffer any more
@@ -292,8 +292,8 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void forward_kernel(A
       }
     }
     if (more) {
-      mk.store(ks[buf ^ 1]);
-      mv.store(vs[buf ^ 1]);
+      mk.store(ks[buf ^ 1], end);
+      mv.store(vs[buf ^ 1], end);
     }
   }
 
@@ -369,8 +369,8 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void query_grad_kerne
   if (kt < k1) {
     mk.fetch(l.kn - kt, end);
     mv.fetch(l.kn - kt, end);
-    mk.store(ks[0]);
-    mv.store(vs[0]);
+    mk.store(ks[0], end);
+    mv.store(vs[0], end);
   }
 
   const float scale2 = a.scale * kLog2e;
@@ -482,8 +482,8 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void query_grad_kerne
       }
     }
     if (more) {
-      mk.store(ks[buf ^ 1]);
-      mv.store(vs[buf ^ 1]);
+      mk.store(ks[buf ^ 1], end);
+      mv.store(vs[buf ^ 1], end);
     }
   }
 #pragma unroll
@@ -526,7 +526,9 @@ struct RowMove : StreamMove<T, BQ, DP, THREADS> {
       this->r[i] = u32x4{0, 0, 0, 0};
       if (count > 0 && row < r1) {
         const int q = query_of(a, row);
-        this->r[i] = load16(row_of<T>(base, st, b, q, hk * a.group + row - q * a.group) + c, count, end);
+        const T* p = row_of<T>(base, st, b, q, hk * a.group + row - q * a.group) + c;
+        if (end == kShort) this->r[i] = load16<T, kShort>(p, count);
+        else this->r[i] = *reinterpret_cast<const u32x4_any*>(p - (end == kWide ? Base::early(count) : 0));
       }
     }
   }
@@ -598,8 +600,8 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void key_grad_kernel(AttnArgs a, i
     }
   };
   auto store = [&](int buf) {
-    mq.store(qs[buf]);
-    md.store(gs[buf]);
+    mq.store(qs[buf], end, a.d - (int)threadIdx.x % mq.PER_ROW * El::E);
+    md.store(gs[buf], end, a.d - (int)threadIdx.x % md.PER_ROW * El::E);
     if ((int)threadIdx.x < BQ) { lses[buf][threadIdx.x] = ml; deltas[buf][threadIdx.x] = mt; los[buf][threadIdx.x] = mlo; his[buf][threadIdx.x] = mhi; }
   };
   if (rt < r1) {
@@ -791,7 +793,8 @@ hipError_t sum_runs(const AttnArgs& a, void* out, void* second, int len, int gro
 template <class T, int DP>
 struct Shape {
   static constexpr int NB = sizeof(T) == 4 || DP > 128 ? 1 : 2, BQ = stream_rows<T, DP>();
-  // rows between two barriers: twice as many where one workgroup has the CU to itself and its waves wait for each other (880 -> 845 us)
+  // rows between two barriers: twice as many where one workgroup has the CU to itself and its waves wait for each other (4 x 4,096 causal,
+  // 16 heads on 4: the gradient 1,435 -> 1,342 us)
   static constexpr int KBQ = sizeof(T) == 2 && DP == 128 ? 128 : BQ;
   static constexpr int KW = sizeof(T) == 2 && DP <= 128 ? 8 : 4, OCC = DP > 128 ? 1 : sizeof(T) == 2 && DP == 64 ? 4 : 2;
   // Heads of up to three quarters of DP numbers have kernels that ask before every product whether it is all padding (80 of 128: fp32 a quarter

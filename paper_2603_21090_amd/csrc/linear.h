@@ -20,7 +20,7 @@ enum { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };
 
 // Phi(z), the normal distribution's share below z, and e^(-z^2/2).  16-bit types: Phi(-|z|) = poly(t) e^(-z^2/2) / 2, t = 1 / (1 + 0.3275911
 // |z| / sqrt 2) (Abramowitz & Stegun 7.1.26, 1.5e-7 off at most; the tail keeps its size: 0.07 % off at -4).  erff takes several times
-// the instructions on every output: 8,192 x 4,096 x 4,096 in bf16 spent 90 of its 534 us on them.
+// the instructions on every output: 90 us more for 8,192 x 4,096 x 4,096 in bf16.
 template <class T>
 __device__ inline void normal_share(float z, float& share, float& bell) {
   if constexpr (sizeof(T) == 4) {
@@ -142,9 +142,10 @@ __device__ inline void tile_of(unsigned id, unsigned tm, unsigned tn, int& row, 
 template <class T> constexpr int kTileK = 128 / (int)sizeof(T);    // 64 16-bit numbers, 32 floats: 128 bytes
 
 // DEPTH tiles of k are on their way in registers while one is multiplied: where tiles are small and few, what a tile takes is the wait
-// for memory (13 x 4,096 x 11,008 in bf16: 26.6 us with one, 19.9 with three).
+// for memory (13 x 4,096 x 11,008 in bf16: 26.6 us with one, 19.9 with three).  Large ones have one on its way and two in LDS, so that a
+// barrier a tile is enough.  Small tiles run four workgroups a CU: 128 registers.
 template <class T, int BM, int BN, int WM, int WN, int DEPTH, bool L_ROWS, bool R_ROWS>
-__global__ __launch_bounds__(WM * WN * 64, 2) void product_kernel(Product a) {
+__global__ __launch_bounds__(WM * WN * 64, BM * BN <= 64 * 64 ? 4 : 2) void product_kernel(Product a) {
   using El = Elem<T>;
   constexpr int BK = kTileK<T>, THREADS = WM * WN * 64, MB = BM / WM / 16, NB = BN / WN / 16;
   constexpr int SL = lds_stride<T>(L_ROWS ? BK : BN), SR = lds_stride<T>(R_ROWS ? BK : BM);
@@ -199,8 +200,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void product_kernel(Product a) {
   if constexpr (DEPTH == 1) {                                 // two buffers in LDS, one barrier a tile
     if (kb < ke) {
       fetch(0, kb);
-      MoveL::store(ls[0], rl[0]);
-      MoveR::store(rs[0], rr[0]);
+      ml.store(ls[0], rl[0]);
+      mr.store(rs[0], rr[0]);
     }
     int buf = 0;
     for (int k = kb; k < ke; k += BK, buf ^= 1) {
@@ -209,8 +210,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void product_kernel(Product a) {
       if (more) fetch(0, k + BK);
       multiply(ls[buf], rs[buf]);
       if (more) {
-        MoveL::store(ls[buf ^ 1], rl[0]);
-        MoveR::store(rs[buf ^ 1], rr[0]);
+        ml.store(ls[buf ^ 1], rl[0]);
+        mr.store(rs[buf ^ 1], rr[0]);
       }
     }
   } else {
@@ -223,8 +224,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void product_kernel(Product a) {
         const int k = kt + d * BK;
         if (k >= ke) break;
         __syncthreads();
-        MoveL::store(ls[0], rl[d]);
-        MoveR::store(rs[0], rr[d]);
+        ml.store(ls[0], rl[d]);
+        mr.store(rs[0], rr[d]);
         __syncthreads();
         if (k + DEPTH * BK < ke) fetch(d, k + DEPTH * BK);
         multiply(ls[0], rs[0]);
@@ -466,8 +467,8 @@ struct Plan { int bm, bn, splits, k_per; };
 
 // Tiles of a product:
 //   256 x 256  16-bit types, 256 such tiles or more, k of whole tiles, rows per k of whole pieces of 16 bytes
-//   128 x 128, 112, 96, 64   256 such tiles or more that pad m by no more than a quarter over 64 rows; the width that pads n least (fp32, whose products are the bound: 40,000 x 372 x 200 101 us in
-//              tiles of 128 columns, 89 in 112; 16-bit: 64 columns where n has no more, or 128 would pad a quarter more)
+//   128 x 128, 112, 96, 64   256 such tiles or more that pad m by no more than a quarter over 64 rows; the width that pads n least (fp32, whose products are the bound: 40,000 x 372 x 200 97 us in
+//              tiles of 128 columns, 87 in 112; 16-bit: 64 columns where n has no more, or 128 would pad a quarter more)
 //              The same with k split, eight tiles of k a split at least, where that makes 384 workgroups or more.
 //   64 x 64    everything smaller, k split while there are fewer than 1,024 workgroups, four tiles of k a split at least.
 //   32 x 32    fp32 where those are fewer than 256: a wave's 32 x 32 outputs of 200 terms are 3 us of matrix instructions.
