@@ -470,7 +470,9 @@ struct Plan { int bm, bn, splits, k_per; };
 //   128 x 128, 112, 96, 64   256 such tiles or more that pad m by no more than a quarter over 64 rows; the width that pads n least (fp32, whose products are the bound: 40,000 x 372 x 200 97 us in
 //              tiles of 128 columns, 87 in 112; 16-bit: 64 columns where n has no more, or 128 would pad a quarter more)
 //              The same with k split, eight tiles of k a split at least, where that makes 384 workgroups or more.
-//   64 x 64    everything smaller, k split while there are fewer than 1,024 workgroups, four tiles of k a split at least.
+//   64 x 64    everything smaller, k split while there are fewer than 1,024 workgroups, eight tiles of k a split at least: joining takes 4 to 8
+//              us, a tile of k 0.4 to 0.8 (bf16 1,500 x 1,000 x 800 in one split 14.5 us, in three of five tiles 20.0; 700 x 2,000 x 1,500 in one
+//              30.0, in three of eleven 22.7).
 //   32 x 32    fp32 where those are fewer than 256: a wave's 32 x 32 outputs of 200 terms are 3 us of matrix instructions.
 template <class T>
 Plan plan_of(int64_t m, int64_t n, int64_t k, bool l_rows, bool r_rows) {
@@ -505,10 +507,10 @@ Plan plan_of(int64_t m, int64_t n, int64_t k, bool l_rows, bool r_rows) {
     }
   }
   p.bm = p.bn = 64;
-  split(1024, 4);
+  split(1024, 8);
   if (sizeof(T) == 4 && tiles_of(64, 64) * p.splits < 256) {
     p.bm = p.bn = 32;
-    split(1024, 4);
+    split(1024, 8);
   }
   return p;
 }
