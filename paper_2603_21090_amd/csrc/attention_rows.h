@@ -133,22 +133,25 @@ __global__ __launch_bounds__(256) void rows_forward_kernel(AttnArgs a, RowPlan p
     k1 = min(k1, (split + 1) * plan.per);
   }
   const float scale2 = a.scale * kLog2e;
-  const T* kp = row_of<T>(a.k, a.sk, b, 0, hk) + at;
-  const T* vp = row_of<T>(a.v, a.sv, b, 0, hk) + at;
-  u32x4 kr[U], vr[U];
   const RowEnd end = row_end<T>(a.d);
+  const int early = end == kWide && at < a.d ? max(E - (a.d - at), 0) : 0;                 // elements in front of the head's last part that its piece holds
+  const T* kp = row_of<T>(a.k, a.sk, b, 0, hk) + at - early;
+  const T* vp = row_of<T>(a.v, a.sv, b, 0, hk) + at - early;
+  u32x4 kr[U], vr[U];
   auto fetch = [&](int base) {
-    by_end(end, [&](auto e) {
+    auto each = [&](auto load) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int j = base + u * G + slot;
         kr[u] = vr[u] = u32x4{0, 0, 0, 0};
         if (j < k1 && at < a.d) {
-          kr[u] = load16<T, decltype(e)::value>(kp + (int64_t)j * a.sk.row, a.d - at);
-          vr[u] = load16<T, decltype(e)::value>(vp + (int64_t)j * a.sv.row, a.d - at);
+          kr[u] = load(kp + (int64_t)j * a.sk.row);
+          vr[u] = load(vp + (int64_t)j * a.sv.row);
         }
       }
-    });
+    };
+    if (end != kShort) each([](const T* p) { return *reinterpret_cast<const u32x4_any*>(p); });
+    else each([&](const T* p) { return load16<T, kShort>(p, a.d - at); });
   };
   int base = k0 + (WIDE ? wave * STEP : 0);
   if (base < k1) fetch(base);                                 // (with the rows on their way too: one wait for a short list)
@@ -165,6 +168,12 @@ __global__ __launch_bounds__(256) void rows_forward_kernel(AttnArgs a, RowPlan p
   }
 
   while (base < k1) {
+    if (end == kWide)
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        kr[u] = moved_down<T>(kr[u], early * (int)sizeof(T));
+        vr[u] = moved_down<T>(vr[u], early * (int)sizeof(T));
+      }
     const bool partial = base < all0 || base + STEP > min(all1, k1);
     float s[R][U];
 #pragma unroll
@@ -282,22 +291,25 @@ __global__ __launch_bounds__(256) void rows_grad_kernel(AttnArgs a, RowPlan plan
   }
   const int first = WIDE ? split * plan.per : 0, last = WIDE ? min(a.k_len, (split + 1) * plan.per) : a.k_len;
   k1 = min(k1, last);                                         // (the next run's keys: zeros here, which add nothing to dq)
-  const T* kp = row_of<T>(a.k, a.sk, b, 0, hk) + at;
-  const T* vp = row_of<T>(a.v, a.sv, b, 0, hk) + at;
-  u32x4 kr[U], vr[U];
   const RowEnd end = row_end<T>(a.d);
+  const int early = end == kWide && at < a.d ? max(E - (a.d - at), 0) : 0;                 // elements in front of the head's last part that its piece holds
+  const T* kp = row_of<T>(a.k, a.sk, b, 0, hk) + at - early;
+  const T* vp = row_of<T>(a.v, a.sv, b, 0, hk) + at - early;
+  u32x4 kr[U], vr[U];
   auto fetch = [&](int base) {
-    by_end(end, [&](auto e) {
+    auto each = [&](auto load) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int j = base + u * G + slot;
         kr[u] = vr[u] = u32x4{0, 0, 0, 0};
         if (j >= k0 && j < k1 && at < a.d) {
-          kr[u] = load16<T, decltype(e)::value>(kp + (int64_t)j * a.sk.row, a.d - at);
-          vr[u] = load16<T, decltype(e)::value>(vp + (int64_t)j * a.sv.row, a.d - at);
+          kr[u] = load(kp + (int64_t)j * a.sk.row);
+          vr[u] = load(vp + (int64_t)j * a.sv.row);
         }
       }
-    });
+    };
+    if (end != kShort) each([](const T* p) { return *reinterpret_cast<const u32x4_any*>(p); });
+    else each([&](const T* p) { return load16<T, kShort>(p, a.d - at); });
   };
   int base = first + (WIDE ? wave * STEP : 0);
   if (base < last) fetch(base);                               // (with the rows on their way too: one wait for a short list)
@@ -329,6 +341,12 @@ __global__ __launch_bounds__(256) void rows_grad_kernel(AttnArgs a, RowPlan plan
   T *dk = static_cast<T*>(a.dk) + out0, *dv = static_cast<T*>(a.dv) + out0;
 
   while (base < last) {
+    if (end == kWide)
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        kr[u] = moved_down<T>(kr[u], early * (int)sizeof(T));
+        vr[u] = moved_down<T>(vr[u], early * (int)sizeof(T));
+      }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int j = base + u * G + slot;
