@@ -28,6 +28,7 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 // rows of odd widths start anywhere: global memory takes wide accesses at any element's address
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32_any __attribute__((aligned(2), may_alias));
 
 template <class T> struct Elem;
 
