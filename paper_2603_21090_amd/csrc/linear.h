@@ -317,10 +317,12 @@ __global__ __launch_bounds__(512) void large_product_kernel(Product a) {
 #pragma unroll
     for (int y = 0; y < MB; ++y) acc[x][y] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  ml.fetch();
-  mr.fetch();
-  ml.store(ls[0]);
-  mr.store(rs[0]);
+  if (tiles > 0) {
+    ml.fetch();
+    mr.fetch();
+    ml.store(ls[0]);
+    mr.store(rs[0]);
+  }
   for (int t = 0; t < tiles; ++t) {
     __syncthreads();                                          // tile t is there, and nobody reads the other buffer any more
     const bool more = t + 1 < tiles;
@@ -466,7 +468,8 @@ inline int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 struct Plan { int bm, bn, splits, k_per; };
 
 // Tiles of a product:
-//   256 x 256  16-bit types, 256 such tiles or more, k of whole tiles, rows per k of whole pieces of 16 bytes
+//   256 x 256  16-bit types, 256 such tiles or more, k of whole tiles (one at least: dW of no rows has none and reads nothing), rows per k
+//              of whole pieces of 16 bytes
 //   128 x 128, 112, 96, 64   256 such tiles or more that pad m by no more than a quarter over 64 rows; the width that pads n least (fp32, whose products are the bound: 40,000 x 372 x 200 97 us in
 //              tiles of 128 columns, 87 in 112; 16-bit: 64 columns where n has no more, or 128 would pad a quarter more)
 //              The same with k split, eight tiles of k a split at least, where that makes 384 workgroups or more.
@@ -478,7 +481,7 @@ template <class T>
 Plan plan_of(int64_t m, int64_t n, int64_t k, bool l_rows, bool r_rows) {
   constexpr int BK = kTileK<T>;
   const auto tiles_of = [&](int64_t bm, int64_t bn) { return ((m + bm - 1) / bm) * ((n + bn - 1) / bn); };
-  const bool whole = sizeof(T) == 2 && k % 64 == 0 && (l_rows || n % 8 == 0) && (r_rows || m % 8 == 0);
+  const bool whole = sizeof(T) == 2 && k > 0 && k % 64 == 0 && (l_rows || n % 8 == 0) && (r_rows || m % 8 == 0);
   Plan p{256, 256, 1, (int)up(k < BK ? BK : k, BK)};
   if (whole && tiles_of(256, 256) >= 256) return p;
   p.bm = 128;

@@ -165,3 +165,15 @@ def test_columns_of_one_matrix(size, dt):
     assert torch.equal(m[:, at[0]:at[0] + d_in].cpu(), x)
     for c in (0, at[0] + d_in, at[0] + d_in + 1, at[1] + d_out):
         assert (m[:, c] == 7).all()
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=str)
+@pytest.mark.parametrize("d_in,d_out", [(4096, 4096), (4104, 4160), (6000, 200)])
+@pytest.mark.parametrize("name", ["none", "gelu"])
+def test_no_rows_of_wide_layers(name, d_in, d_out, dt):
+    """Outputs of many tiles from sums of nothing: zeros, and no operand is read (empty tensors have no address)."""
+    x, w = torch.empty(0, d_in, dtype=dt, device="cuda"), torch.ones(d_in, d_out, dtype=dt, device="cuda")
+    z = torch.empty(0, d_out, dtype=dt, device="cuda")
+    dx, dw, db = binding.linear_grad(z, x, w, activation=name, pre=z if name != "none" else None)
+    assert dx.shape == (0, d_in) and dw.shape == w.shape and not dw.any() and db.shape == (d_out,) and not db.any()
+    assert binding.linear(x, w, activation=name).shape == (0, d_out)
