@@ -474,7 +474,7 @@ hipError_t rows_launch(const AttnArgs& a, float* part, hipStream_t s) {
   else
     e = wide_rows(a) ? launch(rows_forward_kernel<T, L, R, U, true>, units * p.splits, 256, s, a, p, part)
                      : launch(rows_forward_kernel<T, L, R, US, false>, (units + 3) / 4, 256, s, a, p, part);
-  if (e != hipSuccess || p.splits == 1) return e;
+  if (e != hipSuccess || p.splits == 1 || rows == 0) return e;      // (no queries: dk and dv are zeros, and there is no dq to add up)
   if constexpr (GRAD) return sum_runs<T>(a, a.dq, nullptr, a.q_len, a.group, p.splits, part, s);
   else return launch(join_kernel<T>, join_grid(units * rows, p.splits), 256, s, a, p.splits, (const float*)part);
 }

@@ -194,3 +194,15 @@ def test_calls_at_the_same_time_on_two_streams(ql, kl):
         want = (kept[n][4], kept[n][5]) + tuple(kept[n][6])
         for res in got[n]:
             assert all(torch.equal(a, b) for a, b in zip(res, want))
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=str)
+@pytest.mark.parametrize("lists,kl,kv,group", [(2, 300, 2, 1), (1, 5000, 1, 4), (3, 129, 2, 2)])
+def test_no_queries_over_keys(lists, kl, kv, group, dt):
+    """Lists of any length without queries: zeros as gradients, nothing else (5,000 and 300 keys are cut into runs, 129 are not)."""
+    q = torch.zeros(lists, 0, kv * group, 40, dtype=dt, device="cuda")
+    k = torch.ones(lists, kl, kv, 40, dtype=dt, device="cuda")
+    out, lse = binding.attention(q, k, k)
+    assert out.shape == q.shape and lse.shape == (lists, kv * group, 0)
+    dq, dk, dv = binding.attention_grad(q, q, k, k, out, lse)
+    assert dq.shape == q.shape and dk.shape == dv.shape == k.shape and not dk.any() and not dv.any()
