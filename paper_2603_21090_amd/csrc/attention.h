@@ -422,7 +422,9 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void query_grad_kerne
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int j = kt + (y + u) * 16 + 4 * g + e;
-            p[u][c][e] = j >= lo[c] && j < hi[c] ? p[u][c][e] : 0.f;
+            const bool sees = j >= lo[c] && j < hi[c];
+            p[u][c][e] = sees ? p[u][c][e] : 0.f;
+            dp[u][c][e] = sees ? dp[u][c][e] : 0.f;           // (a masked value may be the type's largest: zero times an infinite product)
           }
     }
   };
@@ -645,7 +647,9 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void key_grad_kernel(AttnArgs a, i
             float p = __builtin_amdgcn_exp2f(fmaf(s[u][c][e], scale2, -ls[e]));      // (2^kShift times)
             if (partial) {
               const int j = jw + c * 16;
-              p = j >= los[buf][at + e] && j < his[buf][at + e] ? p : 0.f;
+              const bool sees = j >= los[buf][at + e] && j < his[buf][at + e];
+              p = sees ? p : 0.f;
+              dp[u][c][e] = sees ? dp[u][c][e] : 0.f;         // (as in the dq kernel)
             }
             s[u][c][e] = p;
             float ds = p * (dp[u][c][e] - dl[e]);

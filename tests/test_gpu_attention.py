@@ -206,3 +206,21 @@ def test_no_queries_over_keys(lists, kl, kv, group, dt):
     assert out.shape == q.shape and lse.shape == (lists, kv * group, 0)
     dq, dk, dv = binding.attention_grad(q, q, k, k, out, lse)
     assert dq.shape == q.shape and dk.shape == dv.shape == k.shape and not dk.any() and not dv.any()
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=str)
+@pytest.mark.parametrize("ql,kl,window,kv,d", [(1, 90, 5, 2, 64), (3, 400, 9, 2, 50), (10, 40, 4, 2, 64), (10, 40, 4, 1, 33), (40, 90, 7, 2, 64),
+                                               (130, 700, 20, 2, 128), (20, 50, 3, 2, 200)])
+def test_masked_keys_hold_the_type_s_largest_numbers(ql, kl, window, kv, d, dt):
+    """Keys in front of every query's window hold the largest and the lowest numbers of the type: their products with dout and the queries
+    are infinite or not numbers, and belong to no pair that counts."""
+    q, k, v, do, _, _ = make(3, ql, kl, 2, kv, d, False, dt)
+    kn, qn = torch.tensor([kl, kl - 3, kl - 1], dtype=torch.int32), torch.tensor([ql, max(ql - 2, 1), ql], dtype=torch.int32)
+    unseen = ~refs.visible(3, ql, kl, qn, kn, True, window).any(1)
+    assert unseen.any(1).all()
+    most = torch.finfo(dt).max
+    for t in (k, v):
+        t[unseen] = most
+        t[..., 1::2][unseen] = -most
+        t[:, ::2][unseen[:, ::2]] = -most                     # (every other key: sums of one sign)
+    check(q, k, v, do, qn, kn, True, window)
