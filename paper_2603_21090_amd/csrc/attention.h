@@ -28,13 +28,58 @@ namespace attn {
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // Softmax weights as fp16 factors are taken 2^14 times: a weight of a long list is a small number, and below 2^-14 fp16 has
-// fewer bits (5,000 keys: dv 0.5 % off).  None exceeds 1, so none overflows.  (ds has no such bound and is taken as it is.)
+// fewer bits (5,000 keys: dv 0.5 % off).  None exceeds 1, so none overflows.
 template <class T> constexpr float kShift = std::is_same<T, _Float16>::value ? 14.f : 0.f;
 template <class T> constexpr float kUnshift = kShift<T> != 0.f ? 1.f / 16384.f : 1.f;
 
 // In the forward call the reference score may lag the largest one by kLazy powers of two (see there): 2^7 times there.
 template <class T> constexpr float kShiftLazy = kShift<T> / 2.f;
 constexpr float kLazy = 8.f;
+
+__device__ inline float over_groups_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ inline float over_groups_sum(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+// ds has no such bound: beside dout of a mean over many rows it falls below fp16's numbers (4,000 keys, dout of 2^-14: its terms lose all bits), and
+// beside large dout and values it passes 65,504.  As an fp16 factor it is taken a power of two times that belongs to the column of the
+// accumulators (a row of dq, a key of dk): 2^64 times at first, and where a factor would pass 2^15 only so often that the largest lies above 2^8,
+// the sums so far being taken along.  What is 2^-22 of the column's largest keeps all bits, and no term is off by more than 2^-33 of that one.
+// (3 lists of up to 1,777, window 512, 6 heads of 80 on 2: dq, dk and dv 82.1 -> 85.3 us.)
+template <class T> constexpr bool kFitted = std::is_same<T, _Float16>::value;
+__device__ inline float exponent_of(float power_of_two) { return (float)((int)(__builtin_bit_cast(uint32_t, power_of_two) >> 23) - 127); }
+template <int NB>
+struct Fit {
+  float times[NB];
+  __device__ inline Fit() {
+#pragma unroll
+    for (int c = 0; c < NB; ++c) times[c] = 0x1p64f;
+  }
+  // 1 / times: both are powers of two
+  __device__ inline float undo(int c) const { return __builtin_bit_cast(float, 0x7F000000u - __builtin_bit_cast(uint32_t, times[c])); }
+  // top: the largest |ds| that this lane adds to column c next, as often as they are taken; sums(c, by): the column's factors and sums are to be
+  // taken `by` times
+  template <class F>
+  __device__ inline void take(const float (&top)[NB], F sums) {
+    bool grows = false;
+#pragma unroll
+    for (int c = 0; c < NB; ++c) grows |= top[c] > 0x1p15f;
+    if (!__any(grows)) return;
+#pragma unroll
+    for (int c = 0; c < NB; ++c) {
+      const float most = over_groups_max(top[c]);             // of the four lane groups that share the column
+      if (!(most > 0x1p15f)) continue;
+      const uint32_t power = __builtin_bit_cast(uint32_t, most) >> 23;               // most lies in 2^(power - 127) and twice that
+      const float by = __builtin_bit_cast(float, (262u - power) << 23);
+      times[c] *= by;
+      sums(c, by);
+    }
+  }
+};
 
 // rows of a streamed tile: two buffers of two tiles of 64 x 128 16-bit numbers are 68 KB, two workgroups a CU
 template <class T, int DP>
@@ -97,15 +142,6 @@ __device__ inline void load_cols(typename Elem<T>::Frag (&f)[NB][DP / Elem<T>::K
       }
     }
   });
-}
-
-__device__ inline float over_groups_max(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
-}
-__device__ inline float over_groups_sum(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
 }
 
 // what fits a CU at once: two workgroups, or one of eight waves whose rows are 128 numbers
@@ -453,6 +489,10 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void query_grad_kerne
   for (int x = 0; x < DB; ++x)
 #pragma unroll
     for (int c = 0; c < NB; ++c) dq[x][c] = floatx4{0.f, 0.f, 0.f, 0.f};
+  Fit<NB> fit;                                                // (the weights' exponents carry its powers: they are for ds alone here)
+#pragma unroll
+  for (int c = 0; c < NB; ++c)
+    if constexpr (kFitted<T>) lse2[c] -= exponent_of(fit.times[c]);
   for (; kt < k1; kt += BK, buf ^= 1) {
     __syncthreads();
     const bool more = kt + BK < k1;
@@ -467,13 +507,29 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void query_grad_kerne
         floatx4 p[PB][NB], dp[PB][NB];
         weights(y, p, dp, partial);
         typename El::Frag f[NB];
+        floatx4 ds[NB][PB];
 #pragma unroll
-        for (int c = 0; c < NB; ++c) {
-          floatx4 ds[PB];
+        for (int c = 0; c < NB; ++c)
 #pragma unroll
-          for (int u = 0; u < PB; ++u) ds[u] = p[u][c] * (dp[u][c] - delta[c]);
-          f[c] = pack<T>(ds);
+          for (int u = 0; u < PB; ++u) ds[c][u] = p[u][c] * (dp[u][c] - delta[c]);
+        if constexpr (kFitted<T>) {
+          float top[NB] = {};
+#pragma unroll
+          for (int c = 0; c < NB; ++c)
+#pragma unroll
+            for (int u = 0; u < PB; ++u)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) top[c] = fmaxf(top[c], fabsf(ds[c][u][e]));
+          fit.take(top, [&](int c, float by) {
+            lse2[c] -= exponent_of(by);
+#pragma unroll
+            for (int u = 0; u < PB; ++u) ds[c][u] *= by;
+#pragma unroll
+            for (int x = 0; x < DB; ++x) dq[x][c] *= by;
+          });
         }
+#pragma unroll
+        for (int c = 0; c < NB; ++c) f[c] = pack<T>(ds[c]);
 #pragma unroll
         for (int x = 0; x < DB; ++x) {
           if (SKIP && x > 0 && x * 16 >= a.d) break;
@@ -492,15 +548,16 @@ __global__ __launch_bounds__(WAVES * 64, DP > 128 ? 1 : 2) void query_grad_kerne
   for (int c = 0; c < NB; ++c) {
     if (r[c] >= rows) continue;
     const bool any = hi[c] > lo[c];
+    const float by = kFitted<T> ? a.scale * fit.undo(c) : a.scale;
     if (runs > 1) {
       float* p = part + (((int64_t)(b * a.kv_heads + hk) * runs + pos.run) * rows + r[c]) * a.d;
 #pragma unroll
-      for (int x = 0; x < DB; ++x) store4(p, x * 16 + 4 * g, a.d, any ? dq[x][c] * a.scale : floatx4{0.f, 0.f, 0.f, 0.f});
+      for (int x = 0; x < DB; ++x) store4(p, x * 16 + 4 * g, a.d, any ? dq[x][c] * by : floatx4{0.f, 0.f, 0.f, 0.f});
       continue;
     }
     T* row = dense_row<T>(a, a.dq, a.q_len, a.heads, b, qi[c], head[c]);
 #pragma unroll
-    for (int x = 0; x < DB; ++x) store4(row, x * 16 + 4 * g, a.d, any ? dq[x][c] * a.scale : floatx4{0.f, 0.f, 0.f, 0.f});
+    for (int x = 0; x < DB; ++x) store4(row, x * 16 + 4 * g, a.d, any ? dq[x][c] * by : floatx4{0.f, 0.f, 0.f, 0.f});
   }
 }
 
@@ -577,6 +634,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void key_grad_kernel(AttnArgs a, i
   for (int x = 0; x < DB; ++x)
 #pragma unroll
     for (int c = 0; c < NB; ++c) dk[x][c] = dv[x][c] = floatx4{0.f, 0.f, 0.f, 0.f};
+  Fit<NB> fit;
 
   RowMove<T, BQ, DP, WAVES * 64> mq, md;
   float ml = 0.f, mt = 0.f;
@@ -652,10 +710,26 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void key_grad_kernel(AttnArgs a, i
               dp[u][c][e] = sees ? dp[u][c][e] : 0.f;         // (as in the dq kernel)
             }
             s[u][c][e] = p;
-            float ds = p * (dp[u][c][e] - dl[e]);
-            if constexpr (kShift<T> != 0.f) ds *= kUnshift<T>;
-            dp[u][c][e] = ds;
+            dp[u][c][e] = p * (dp[u][c][e] - dl[e]);
           }
+      }
+      if constexpr (kFitted<T>) {
+        float top[NB] = {};
+#pragma unroll
+        for (int c = 0; c < NB; ++c)
+#pragma unroll
+          for (int u = 0; u < PB; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              dp[u][c][e] *= fit.times[c];
+              top[c] = fmaxf(top[c], fabsf(dp[u][c][e]));
+            }
+        fit.take(top, [&](int c, float by) {
+#pragma unroll
+          for (int u = 0; u < PB; ++u) dp[u][c] *= by;
+#pragma unroll
+          for (int x = 0; x < DB; ++x) dk[x][c] *= by;
+        });
       }
 #pragma unroll
       for (int c = 0; c < NB; ++c) {
@@ -682,12 +756,13 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void key_grad_kernel(AttnArgs a, i
   for (int c = 0; c < NB; ++c) {
     const int j = jw + c * 16;
     if (j >= a.k_len) continue;
+    const float by = kFitted<T> ? a.scale * kUnshift<T> * fit.undo(c) : a.scale;
     if (runs > 1) {                                           // dk's runs, then dv's
       const int64_t unit = (int64_t)b * a.kv_heads + hk, kept = (int64_t)a.lists * a.kv_heads * runs * a.k_len * a.d;
       float* p = part + ((unit * runs + pos.run) * a.k_len + j) * a.d;
 #pragma unroll
       for (int x = 0; x < DB; ++x) {
-        store4(p, x * 16 + 4 * g, a.d, dk[x][c] * a.scale);
+        store4(p, x * 16 + 4 * g, a.d, dk[x][c] * by);
         store4(p + kept, x * 16 + 4 * g, a.d, kShift<T> != 0.f ? dv[x][c] * kUnshift<T> : dv[x][c]);
       }
       continue;
@@ -696,7 +771,7 @@ __global__ __launch_bounds__(WAVES * 64, OCC) void key_grad_kernel(AttnArgs a, i
     T* vrow = dense_row<T>(a, a.dv, a.k_len, a.kv_heads, b, j, hk);
 #pragma unroll
     for (int x = 0; x < DB; ++x) {
-      store4(krow, x * 16 + 4 * g, a.d, dk[x][c] * a.scale);
+      store4(krow, x * 16 + 4 * g, a.d, dk[x][c] * by);
       store4(vrow, x * 16 + 4 * g, a.d, kShift<T> != 0.f ? dv[x][c] * kUnshift<T> : dv[x][c]);
     }
   }

@@ -224,3 +224,53 @@ def test_masked_keys_hold_the_type_s_largest_numbers(ql, kl, window, kv, d, dt):
         t[..., 1::2][unseen] = -most
         t[:, ::2][unseen[:, ::2]] = -most                     # (every other key: sums of one sign)
     check(q, k, v, do, qn, kn, True, window)
+
+
+def dealt(n, lo, hi):
+    """n powers of two from 2^lo up to 2^hi, each about as often."""
+    return 2.0 ** torch.linspace(lo, hi, n).round()
+
+
+# q_len, k_len, scale, exponents of q, k, v and of dout (of all rows, or first to last)
+MAGNITUDES = [(24, 4000, 0.125, -6, 6, 0, (-14, -14)),        # dq of ds around fp16's smallest number
+              (24, 4000, 0.125, -8, 8, 0, (-18, -18)),        # and below it
+              (300, 4000, 0.125, 6, -6, 0, (-14, -14)),       # dk
+              (24, 20, 2.0 ** -9, 0, 0, 9, (9, 9)),           # ds above fp16's largest
+              (300, 700, 2.0 ** -7, 0, 0, 4, (-14, 9)),       # rows of all magnitudes, growing
+              (300, 700, 2.0 ** -7, 0, 0, 4, (9, -14))]       # and shrinking
+
+
+@pytest.mark.parametrize("ql,kl,scale,eq,ek,ev,edo", MAGNITUDES, ids=str)
+@pytest.mark.parametrize("heads,kv,d", [(2, 1, 64), (1, 1, 100), (1, 1, 160)])
+def test_half_precision_gradients_of_any_magnitude(ql, kl, scale, eq, ek, ev, edo, heads, kv, d):
+    """ds as an fp16 factor keeps its bits whatever its size: one rounding of 2^-11 of each, and 2^-33 of the largest that a sum has met (the
+    factors are scaled until that one lies above 2^8, where fp16's last step is 2^-25).  refs grants the factors fp16's smallest step instead:
+    taken out here, and for the outputs put back."""
+    q, k, v, do, _, _ = make(1, ql, kl, heads, kv, d, False, torch.float32, seed=11)
+    q, k, v = q * 2.0 ** eq, k * 2.0 ** ek, v * 2.0 ** ev
+    do = do * dealt(ql, *edo)[None, :, None, None]
+    q, k, v, do = (t.half() for t in (q, k, v, do))
+    see = refs.visible(1, ql, kl, None, None, False, 0)
+    kept = refs.TINY[torch.float16]
+    try:
+        refs.TINY[torch.float16] = 0.0
+        want = refs.attention(q, k, v, see, scale, do)
+    finally:
+        refs.TINY[torch.float16] = kept
+    heads_first = lambda t: t.double().permute(0, 2, 1, 3)    # noqa: E731
+    Q, DO = heads_first(q), heads_first(do)
+    K, V = (heads_first(t).repeat_interleave(heads // kv, 1) for t in (k, v))
+    p = torch.softmax(scale * (Q @ K.transpose(2, 3)), -1)
+    dp = DO @ V.transpose(2, 3)
+    ds = (p * (dp - (p * dp).sum(-1, keepdim=True))).abs()
+    step = 2.0 ** -33 * scale
+    more = {"dq": (ds.amax(-1, keepdim=True) * K.abs().sum(2, keepdim=True)).permute(0, 2, 1, 3) * step,
+            "dk": (ds.amax(2)[..., None] * Q.abs().sum(2, keepdim=True)).permute(0, 2, 1, 3) * step, "dv": 0.0}
+    if heads > kv:
+        more["dk"] = more["dk"].sum(2, keepdim=True)
+    Qg, Kg, Vg, DOg = on_gpu(q, k, v, do)
+    out, lse = binding.attention(Qg, Kg, Vg, scale=scale)
+    for name, got in zip(("dq", "dk", "dv"), binding.attention_grad(DOg, Qg, Kg, Vg, out, lse, scale=scale)):
+        value, bound = want[name]
+        assert torch.isfinite(value).all() and value.abs().max() < 65504
+        refs.within(got, (value, bound + more[name] + 2 * kept), name)
