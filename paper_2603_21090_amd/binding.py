@@ -437,16 +437,21 @@ class StreamTGN:
         self._check(self._L.stgn_set_predictor(self._h, _ptr(w), float(b)))
 
     def set_predictor_mlp(self, w1, b1, w2, b2, activation="relu"):
-        """The head act([h_u | h_v] w1 + b1) . w2 + b2: w1 [2 d_emb, hidden], b1 and w2 [hidden]; activation as in linear."""
+        """The head act([h_u | h_v] w1 + b1) . w2 + b2: w1 [2 d_emb, hidden], b1 and w2 [hidden]; activation as in linear.  Captured
+        predictions keep their head's width and activation, and follow the parameters set last for those; the workspaces of every width and
+        activation set so far are held until close."""
+        if activation not in ACTIVATIONS:
+            raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}")
         w1, b1, w2 = (np.ascontiguousarray(a, dtype=np.float32) for a in (w1, b1, w2))
         hidden = w1.shape[1]
         assert w1.shape == (2 * self.cfg.d_emb, hidden) and b1.shape == (hidden,) and w2.shape == (hidden,)
         n = C.c_size_t(0)
         self._check(self._L.stgn_predictor_mlp_workspace(self._h, hidden, C.byref(n)))
-        # one workspace a width, kept: captured predictions go on reading it, with the parameters set last for that width
-        ws = self._head_ws.get(hidden)
+        # one workspace a width and activation, kept: captured predictions, which have both in them, go on reading it, with the parameters set
+        # last for that width and activation
+        ws = self._head_ws.get((hidden, activation))
         if ws is None:
-            ws = self._head_ws[hidden] = self._torch.empty(n.value + 256, dtype=self._torch.uint8, device=self.device)
+            ws = self._head_ws[hidden, activation] = self._torch.empty(n.value + 256, dtype=self._torch.uint8, device=self.device)
         self._check(self._L.stgn_set_predictor_mlp(self._h, hidden, ACTIVATIONS[activation], _ptr(w1), _ptr(b1), _ptr(w2), float(b2),
                                                    C.c_void_p((ws.data_ptr() + 255) & ~255), n.value))
 

@@ -173,3 +173,29 @@ def test_refusals():
     with pytest.raises(binding.StgnError):
         g.predict_batch(np.zeros(1, np.uint32), np.ones(1, np.uint32), np.ones(1))             # no head yet
     g.close()
+
+
+def test_captured_heads_keep_their_activation():
+    """A head of the same width with another activation, set after a capture: the captured one's parameters stay."""
+    w, g, edges = make()
+    g.close()
+    side = torch.cuda.Stream()
+    out = torch.zeros(edges[0].shape[0], device="cuda")
+    with torch.cuda.stream(side):
+        st = synth.EdgeStream(w)
+        h = binding.StreamTGN.from_workload(w, synth.make_weights(w), synth.node_features(w), stream=side)
+        for b in range(6):
+            h.ingest_batch(*st.batch(b))
+        h.set_predictor_mlp(*head(w, 24), activation="relu")
+        first = h.predict_batch(*edges)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            h.predict_batch_static(*edges, out=out)
+        h.set_predictor_mlp(*head(w, 24, seed=3), activation="silu")
+        other = h.predict_batch(*edges)
+        for _ in range(3):
+            graph.replay()
+            side.synchronize()
+            assert torch.equal(out, first)
+        assert torch.equal(h.predict_batch(*edges), other) and not torch.equal(other, first)
+    h.close()
