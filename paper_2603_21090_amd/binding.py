@@ -451,7 +451,9 @@ class StreamTGN:
         # last for that width and activation
         ws = self._head_ws.get((hidden, activation))
         if ws is None:
-            ws = self._head_ws[hidden, activation] = self._torch.empty(n.value + 256, dtype=self._torch.uint8, device=self.device)
+            # (from the context's own stream: what ran last in memory that another stream has given back may still be running there)
+            with self._torch.cuda.stream(self._stream):
+                ws = self._head_ws[hidden, activation] = self._torch.empty(n.value + 256, dtype=self._torch.uint8, device=self.device)
         self._check(self._L.stgn_set_predictor_mlp(self._h, hidden, ACTIVATIONS[activation], _ptr(w1), _ptr(b1), _ptr(w2), float(b2),
                                                    C.c_void_p((ws.data_ptr() + 255) & ~255), n.value))
 

@@ -199,3 +199,25 @@ def test_captured_heads_keep_their_activation():
             assert torch.equal(out, first)
         assert torch.equal(h.predict_batch(*edges), other) and not torch.equal(other, first)
     h.close()
+
+
+def test_a_head_set_while_another_stream_is_current():
+    """Memory that the current stream has given back, with work of that stream on it still to come, is not where the head's parameters go."""
+    w, g, edges = make()
+    _, other, _ = make()
+    p = head(w, 64)
+    other.set_predictor_mlp(*p, activation="silu")
+    want = other.predict_batch(*edges)
+    n = C.c_size_t(0)
+    assert binding.load_library().stgn_predictor_mlp_workspace(g._h, 64, C.byref(n)) == 0
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        given_back = torch.empty(n.value + 256, dtype=torch.uint8, device="cuda")
+        torch.cuda._sleep(1 << 24)
+        given_back.fill_(255)
+        del given_back
+        g.set_predictor_mlp(*p, activation="silu")
+    torch.cuda.synchronize()
+    assert torch.equal(g.predict_batch(*edges), want)
+    g.close()
+    other.close()
