@@ -367,7 +367,7 @@ int stgn_attention(const stgn_attention_args *args, void *device_workspace, size
 int stgn_attention_grad(const stgn_attention_args *args, void *device_workspace, size_t device_bytes, void *hip_stream);
 
 /* NULL ctx: message of the thread's last failed call without a context (create, workspace queries, operators), or where none of
- * the thread's has failed, of any thread's last create or query */
+ * the thread's has failed, of any thread's last create or query.  Valid until the thread's next call without a context. */
 const char *stgn_last_error(const stgn_ctx *ctx);
 const char *stgn_version(void);
 

@@ -4,6 +4,7 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <mutex>
 #include <string>
 #include <vector>
 
@@ -18,8 +19,22 @@ namespace {
 const char* const kClassNames[KC_COUNT] = {"stage_sort", "memory_update", "apply", "plan", "expand", "compact",
                                            "layer", "gather_rows", "noop", "project", "predict", "bucket_rows"};
 
-std::string g_create_error;
-thread_local std::string t_error;   // of the thread's last failed call without a context
+// Messages of failed calls without a context: the thread's own, and any thread's last create or query.  Fixed buffers: a failure allocates
+// nothing, and a message that a caller holds is not freed by another thread's failure.
+struct Message {
+  char text[512] = "";
+  void set(const char* m) { snprintf(text, sizeof text, "%s", m); }
+};
+std::mutex g_create_mutex;
+Message g_create_error;             // under the mutex
+thread_local Message t_error;
+thread_local Message t_create_error;   // the copy handed to a thread without failures of its own
+
+void create_failed(const char* m) {
+  t_error.set(m);
+  std::lock_guard<std::mutex> lock(g_create_mutex);
+  g_create_error.set(m);
+}
 
 constexpr size_t kRowIoBytes = 1u << 20;   // pinned block of stgn_ctx::row_io
 
@@ -79,7 +94,7 @@ struct stgn_ctx {
 namespace {
 
 int fail(stgn_ctx* c, int code, const std::string& msg) {
-  if (c) c->err = msg; else t_error = g_create_error = msg;
+  if (c) c->err = msg; else create_failed(msg.c_str());
   return code;
 }
 
@@ -492,7 +507,7 @@ int sync_and_poll(stgn_ctx* ctx) {
 }  // namespace
 
 int stgn::fail_operator(int code, const char* why) {
-  t_error = why;
+  t_error.set(why);
   return code;
 }
 
@@ -509,7 +524,11 @@ int stgn_probe_gather(const float* table, uint64_t n_rows, uint32_t row_bytes, c
 }
 
 const char* stgn_last_error(const stgn_ctx* ctx) {
-  return ctx ? ctx->err.c_str() : t_error.empty() ? g_create_error.c_str() : t_error.c_str();
+  if (ctx) return ctx->err.c_str();
+  if (t_error.text[0]) return t_error.text;
+  std::lock_guard<std::mutex> lock(g_create_mutex);
+  t_create_error = g_create_error;
+  return t_create_error.text;
 }
 
 int stgn_query_workspace(const stgn_config* cfg, size_t* device_bytes) {
@@ -556,7 +575,7 @@ int stgn_create(const stgn_config* cfg, const stgn_weights* w, const float* node
   memset(&ctx->d, 0, sizeof(Dev));
   layout(*cfg, (char*)device_workspace, &ctx->d);
   ctx->stream = (hipStream_t)hip_stream;
-  auto bail = [&](int code) { t_error = g_create_error = ctx->err; stgn_destroy(ctx); return code; };
+  auto bail = [&](int code) { create_failed(ctx->err.c_str()); stgn_destroy(ctx); return code; };
 
   ctx->pin_bytes = stage_bytes(*cfg);
   for (int i = 0; i < 2; ++i) {

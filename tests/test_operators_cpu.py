@@ -172,3 +172,41 @@ def test_the_plain_forms_agree_with_automatic_differentiation():
     got = refs.attention(q, k, v, see, 0.4, do)
     for a, name in zip((out.transpose(1, 2),) + want, ("out", "dq", "dk", "dv")):
         refs.within(a, (got[name][0], torch.full_like(got[name][0], 1e-12)), name)
+
+
+HAMMER = r"""
+import ctypes as C, sys, threading, time
+lib = C.CDLL(sys.argv[1])
+lib.stgn_last_error.restype, lib.stgn_last_error.argtypes = C.c_char_p, [C.c_void_p]
+class Cfg(C.Structure):
+    _fields_ = [("bytes", C.c_uint8 * 256)]
+n, cfg = C.c_size_t(0), Cfg()
+fail = (lambda: lib.stgn_query_workspace(None, C.byref(n)), lambda: lib.stgn_query_workspace(C.byref(cfg), C.byref(n)),
+        lambda: lib.stgn_create(None, None, None, None, C.c_size_t(0), None, None))
+told = set()
+for f in fail:
+    assert f() != 0
+    told.add(lib.stgn_last_error(None))
+assert len(told) >= 2 and all(told)
+end, odd = time.monotonic() + 1.5, []
+def write(f):
+    while time.monotonic() < end:
+        f()
+def read():
+    while time.monotonic() < end:
+        m = lib.stgn_last_error(None)
+        if m not in told:
+            odd.append(m)
+threads = [threading.Thread(target=write, args=(fail[i % 3],)) for i in range(4)] + [threading.Thread(target=read) for _ in range(4)]
+[t.start() for t in threads]
+[t.join() for t in threads]
+assert not odd, odd[:3]
+"""
+
+
+def test_messages_of_failures_in_other_threads_are_whole(lib):
+    """Threads that fail to create, in turn with different messages, while threads without failures read them (in a process of its own)."""
+    import subprocess
+    import sys
+    r = subprocess.run([sys.executable, "-c", HAMMER, binding.LIB_PATH], capture_output=True, text=True, timeout=100)
+    assert r.returncode == 0, r.stderr[-2000:]
