@@ -300,6 +300,7 @@ int stgn_probe_gather(const float *table, uint64_t n_rows, uint32_t row_bytes, c
  *  - device_workspace: the caller's, 256-byte aligned, of the size the _workspace function tells for the same arguments
  *    (0: may be NULL), in use until the stream has executed the call.  Calls that can run at the same time (two streams,
  *    two graphs) need two workspaces.  Nothing in it outlives the call.
+ *  - A tensor reaches over 2^48 bytes at most.
  *  - Results do not depend on timing: the same arguments give the same bits.
  *  - Elements are fp32, bf16 or fp16, one type per call; sums, softmax maxima and sums, and lse are fp32.  With 16-bit types
  *    the factors of a second product (softmax weights, their gradients, dy act'(z)) are rounded to the type.

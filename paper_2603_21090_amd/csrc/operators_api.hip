@@ -58,6 +58,13 @@ struct Span { const char* a; size_t n; };
 Span span_of(const void* p, uint64_t rows, uint64_t width, uint64_t ld, size_t es) {
   return {static_cast<const char*>(p), p && rows && width ? ((rows - 1) * ld + width) * es : 0};
 }
+// Whether elements at these steps reach over more than the 2^48 bytes that a device address can tell apart: below that the spans' ends stay
+// 64-bit numbers, and no overlap is missed.
+bool too_far(uint64_t n0, uint64_t s0, uint64_t n1, uint64_t s1, uint64_t n2, uint64_t s2, uint64_t width, size_t es) {
+  if (!n0 || !n1 || !n2) return false;
+  const unsigned __int128 last = (unsigned __int128)(n0 - 1) * s0 + (unsigned __int128)(n1 - 1) * s1 + (unsigned __int128)(n2 - 1) * s2 + width;
+  return last * es > (unsigned __int128)1 << 48;
+}
 bool meet(const Span& x, const Span& y) { return x.n && y.n && x.a < y.a + y.n && y.a < x.a + x.n; }
 // rows of x and y, both `ld` bytes apart, whose columns lie side by side in one wider matrix
 bool beside(const Span& x, size_t x_width, const Span& y, size_t y_width, size_t ld) {
@@ -95,12 +102,17 @@ int check_linear(const stgn_linear_args* a, bool grad, bool sizes_only) {
     if (!aligned(p, es)) return no("a pointer is not aligned to its element");
   if (a->ld_x < a->d_in || a->ld_w < a->d_out || a->ld_x > kMaxLd || a->ld_w > kMaxLd) return no("ld_x or ld_w below the row's width");
   if (!a->w || (a->rows && !a->x)) return no("NULL x or w");
+  const char* const far = "a matrix reaches over more than 2^48 bytes";
+  const auto wide = [&](uint64_t rows, uint64_t ld, uint64_t width) { return too_far(rows, ld, 1, 0, 1, 0, width, es); };
+  if (wide(a->rows, a->ld_x, a->d_in) || wide(a->d_in, a->ld_w, a->d_out)) return no(far);
   const Span x = span_of(a->x, a->rows, a->d_in, a->ld_x, es), w = span_of(a->w, a->d_in, a->d_out, a->ld_w, es);
   if (!grad) {
     if (a->rows && !a->y) return no("NULL y");
     if (a->ld_y < a->d_out || a->ld_y > kMaxLd) return no("ld_y below the row's width");
     if (a->residual && (a->ld_residual < a->d_out || a->ld_residual > kMaxLd)) return no("ld_residual below the row's width");
     if (a->pre && (a->ld_pre < a->d_out || a->ld_pre > kMaxLd)) return no("ld_pre below the row's width");
+    if (wide(a->rows, a->ld_y, a->d_out) || (a->residual && wide(a->rows, a->ld_residual, a->d_out)) || (a->pre && wide(a->rows, a->ld_pre, a->d_out)))
+      return no(far);
     const Span y = span_of(a->y, a->rows, a->d_out, a->ld_y, es), p = span_of(a->pre, a->rows, a->d_out, a->ld_pre, es),
                b = span_of(a->bias, 1, a->d_out, 0, es), r = span_of(a->residual, a->rows, a->d_out, a->ld_residual, es);
     const bool in_place = a->residual == a->y && a->ld_residual == a->ld_y;
@@ -120,6 +132,7 @@ int check_linear(const stgn_linear_args* a, bool grad, bool sizes_only) {
     if (a->rows && !a->pre) return no("the gradient of an activation needs pre");
     if (a->ld_pre < a->d_out || a->ld_pre > kMaxLd) return no("ld_pre below the row's width");
   }
+  if (wide(a->rows, a->ld_dy, a->d_out) || (a->activation != STGN_ACT_NONE && wide(a->rows, a->ld_pre, a->d_out))) return no(far);
   const Span in[] = {x, w, span_of(a->dy, a->rows, a->d_out, a->ld_dy, es),
                      span_of(a->activation != STGN_ACT_NONE ? a->pre : nullptr, a->rows, a->d_out, a->ld_pre, es)};
   const Span out[] = {span_of(a->dx, a->rows, a->d_in, a->d_in, es), span_of(a->dw, a->d_in, a->d_out, a->d_out, es),
@@ -190,6 +203,13 @@ int check_attention(const stgn_attention_args* a, bool grad, bool sizes_only) {
   const bool have_q = a->lists && a->q_len, have_k = a->lists && a->k_len;
   if (have_q && (!a->q || !a->out || !a->lse)) return no("NULL q, out or lse");
   if (have_k && (!a->k || !a->v)) return no("NULL k or v");
+  const auto beyond = [&](uint64_t len, uint64_t heads, uint64_t sl, uint64_t sr, uint64_t sh) {
+    return too_far(a->lists, sl, len, sr, heads, sh, a->d_head, es);
+  };
+  const char* const far = "a tensor reaches over more than 2^48 bytes";
+  if (beyond(a->q_len, a->heads, a->q_list, a->q_row, a->q_head) || beyond(a->k_len, a->kv_heads, a->k_list, a->k_row, a->k_head) ||
+      beyond(a->k_len, a->kv_heads, a->v_list, a->v_row, a->v_head) || beyond(a->q_len, a->heads, a->out_list, a->out_row, a->out_head))
+    return no(far);
   auto reach = [&](const void* p, uint64_t len, uint64_t heads, uint64_t sl, uint64_t sr, uint64_t sh) {
     Span s{static_cast<const char*>(p), 0};
     if (p && a->lists && len) s.n = ((a->lists - 1) * sl + (len - 1) * sr + (heads - 1) * sh + a->d_head) * es;
@@ -208,6 +228,7 @@ int check_attention(const stgn_attention_args* a, bool grad, bool sizes_only) {
     return STGN_OK;
   }
   if (a->dout_list > kMaxLd || a->dout_row > kMaxLd || a->dout_head > kMaxLd) return no("a stride is out of range");
+  if (beyond(a->q_len, a->heads, a->dout_list, a->dout_row, a->dout_head)) return no(far);
   if (have_q && (!a->dout || !a->dq)) return no("NULL dout or dq");
   if (have_k && (!a->dk || !a->dv)) return no("NULL dk or dv");
   const Span d = reach(a->dout, a->q_len, a->heads, a->dout_list, a->dout_row, a->dout_head);
