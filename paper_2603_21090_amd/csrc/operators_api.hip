@@ -89,6 +89,7 @@ int check_linear(const stgn_linear_args* a, bool grad, bool sizes_only) {
   if (!a) return no("NULL arguments");
   if (a->dtype > STGN_F16) return no("dtype must be STGN_F32, STGN_BF16 or STGN_F16");
   if (a->activation > STGN_ACT_SILU) return no("unknown activation");
+  if (a->reserved) return no("reserved must be 0");
   if (a->rows > kMaxRows) return no("rows out of range");
   if (a->d_in == 0 || a->d_out == 0 || a->d_in > kMaxWidth || a->d_out > kMaxWidth) return no("d_in and d_out must lie in 1 .. 2^24");
   // every product's tiles of 64 x 64 (or its splits, at most 512 more) are one launch

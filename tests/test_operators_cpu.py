@@ -237,3 +237,11 @@ def test_tensors_that_reach_past_every_address_are_refused(lib, bad):
     for call in (lib.stgn_attention, lib.stgn_attention_grad) if not bad.startswith("dout") else (lib.stgn_attention_grad,):
         assert call(C.byref(args), None, 0, None) == INVALID
         assert b"2^48" in lib.stgn_last_error(None)
+
+
+def test_reserved_numbers_are_zero(lib):
+    n = C.c_size_t(0)
+    args = linear_args(reserved=1)
+    for rc in (lib.stgn_linear(C.byref(args), None, 0, None), lib.stgn_linear_grad(C.byref(args), None, 0, None),
+               lib.stgn_linear_workspace(C.byref(args), C.byref(n), None)):
+        assert rc == INVALID and b"reserved" in lib.stgn_last_error(None)
