@@ -274,3 +274,11 @@ def test_half_precision_gradients_of_any_magnitude(ql, kl, scale, eq, ek, ev, ed
         value, bound = want[name]
         assert torch.isfinite(value).all() and value.abs().max() < 65504
         refs.within(got, (value, bound + more[name] + 2 * kept), name)
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=str)
+@pytest.mark.parametrize("ql,kl,heads,kv,d,causal,window", [(60, 9000, 1, 1, 33, False, 0), (9000, 50, 1, 1, 33, False, 0), (30, 8300, 2, 1, 64, True, 0),
+                                                            (8800, 60, 2, 1, 40, True, 0), (40, 8200, 1, 1, 130, False, 0)])
+def test_runs_of_long_streams(ql, kl, heads, kv, d, causal, window, dt):
+    """Few tiles against streams of 8,192 rows and more: sixteen runs and more, joined by the waves of a workgroup."""
+    check(*make(1, ql, kl, heads, kv, d, True, dt), causal, window)
