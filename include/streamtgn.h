@@ -303,7 +303,8 @@ int stgn_probe_gather(const float *table, uint64_t n_rows, uint32_t row_bytes, c
  *  - A tensor reaches over 2^48 bytes at most.
  *  - Results do not depend on timing: the same arguments give the same bits.
  *  - Elements are fp32, bf16 or fp16, one type per call; sums, softmax maxima and sums, and lse are fp32.  With 16-bit types
- *    the factors of a second product (softmax weights, their gradients, dy act'(z)) are rounded to the type.
+ *    the factors of a second product (softmax weights, their gradients, dy act'(z)) are rounded to the type; in fp16 the weights and their
+ *    gradients are scaled by powers of two, so that no magnitude costs them bits, and dy act'(z) is not: past 65,504 it is infinite.
  *  - Errors: STGN_E_INVALID_ARG, STGN_E_WORKSPACE or STGN_E_DEVICE, nothing enqueued; stgn_last_error(NULL) of the same
  *    thread says why. */
 enum { STGN_F32 = 0, STGN_BF16 = 1, STGN_F16 = 2 };

@@ -161,7 +161,8 @@ def probe_gather(table, idx, per_group, out, stream=0):
         raise StgnError(rc)
 
 
-# ---- operators on the caller's tensors: torch device tensors in, new tensors out, on the current stream of their device
+# ---- operators on the caller's tensors: torch device tensors in, new tensors out, on the current stream of their device.  They
+# record nothing for automatic differentiation, whatever their inputs require: the gradients are calls of their own.
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 _dtypes = None
 
@@ -230,7 +231,8 @@ def _linear_sizes(x, w, activation):
 def linear(x, w, bias=None, activation="none", residual=None, keep_pre=False):
     """y = act(x w + bias) + residual (stgn_linear): x [rows, d_in], w [d_in, d_out], bias [d_out], residual [rows, d_out], all
     of one type (float32, bfloat16, float16); activation: "none", "relu", "gelu", "silu".  Returns y, or (y, pre) with
-    keep_pre: the values in front of the activation, which linear_grad needs."""
+    keep_pre: the values in front of the activation, which linear_grad needs.  y has no autograd graph, also where an input
+    requires gradients: linear_grad computes them."""
     import torch
     L = load_library()
     sizes, shape = _linear_sizes(x, w, activation)
@@ -289,7 +291,8 @@ def _attention_call(q, k, v, q_lens, k_lens, causal, window, scale):
 def attention(q, k, v, q_lens=None, k_lens=None, causal=False, window=0, scale=None):
     """Softmax attention (stgn_attention): q [lists, q_len, heads, d], k and v [lists, k_len, kv_heads, d], any strides but for the
     last; q_lens, k_lens: int32 [lists] on the device, None: all rows.  causal aligns the lists at their ends; window: only the last
-    `window` keys up to the query (0: all).  scale: d ** -0.5 by default.  Returns out (as q) and lse [lists, heads, q_len] fp32."""
+    `window` keys up to the query (0: all).  scale: d ** -0.5 by default.  Returns out (as q) and lse [lists, heads, q_len] fp32,
+    without an autograd graph, also where an input requires gradients: attention_grad computes them."""
     import torch
     L = load_library()
     sizes, where = _attention_call(q, k, v, q_lens, k_lens, causal, window, scale)

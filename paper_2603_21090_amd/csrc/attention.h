@@ -866,7 +866,7 @@ hipError_t sum_runs(const AttnArgs& a, void* out, void* second, int len, int gro
 }
 
 // How many rows or keys a workgroup takes.  16-bit types: 128 queries, four waves of 32; the dk/dv kernel keeps twice the operands and
-// sums a wave, so eight waves of 16 keys (four of 32 in 479 registers, one wave a SIMD: 1,323 us where these take 880; four of 32 with the values
+// sums a wave, so eight waves of 16 keys (four of 32 in 479 registers, one wave a SIMD: half as long again; four of 32 with the values
 // in LDS: as long as these).  fp32: 64, four waves
 // of 16.
 template <class T, int DP>

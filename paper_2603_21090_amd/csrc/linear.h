@@ -404,7 +404,9 @@ __global__ __launch_bounds__(256) void join_kernel(Product a) {
   }
 }
 
-// dz = dy act'(z), rounded to T as the operand of the products that follow, and the sums of its columns over a workgroup's rows
+// dz = dy act'(z), rounded to T as the operand of the products that follow (8,192 x 4,096 x 4,096 in bf16, against 64 bits: 0.0023 off in the norm,
+// 0.0017 with a dz of 32 bits, which would take both products twice or on the fp32 units), and the sums of its unrounded columns over a workgroup's
+// rows
 template <class T>
 __global__ __launch_bounds__(256) void dz_kernel(LinearGradArgs a, T* dz, int64_t ld_dz, float* sums, int rows_per) {
   __shared__ floatx4 wsum[4][64];

