@@ -282,3 +282,20 @@ def test_half_precision_gradients_of_any_magnitude(ql, kl, scale, eq, ek, ev, ed
 def test_runs_of_long_streams(ql, kl, heads, kv, d, causal, window, dt):
     """Few tiles against streams of 8,192 rows and more: sixteen runs and more, joined by the waves of a workgroup."""
     check(*make(1, ql, kl, heads, kv, d, True, dt), causal, window)
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=str)
+@pytest.mark.parametrize("ql,kl", [(1, 300), (2, 60), (40, 90)])
+def test_offsets_past_32_bits(ql, kl, dt):
+    """Lists 2^31 + 5 numbers apart, or rows so far apart that the last values lie that far behind the first: everything in one buffer."""
+    q, k, v, do, qn, kn = make(2, ql, kl, 2, 2, 50, True, dt)
+    far = (1 << 31) + 5
+    buffer = torch.empty(far + kl * 2 * 50 + 64, dtype=dt, device="cuda")
+    lists = buffer.as_strided((2, kl, 2, 50), (far, 100, 50, 1), 3)
+    lists.copy_(k.cuda())
+    Q, V, DO, QN, KN = on_gpu(q, v, do, qn, kn)
+    check(q, k, v, do, qn, kn, True, 0, prepared=(Q, lists, V, DO, QN, KN))
+    row = (far - 1000) // kl
+    rows = buffer.as_strided((2, kl, 2, 50), (150, row, 50, 1), 3)
+    rows.copy_(v.cuda())
+    check(q, k, v, do, qn, kn, True, 0, prepared=(Q, k.cuda(), rows, DO, QN, KN))

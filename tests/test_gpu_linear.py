@@ -177,3 +177,20 @@ def test_no_rows_of_wide_layers(name, d_in, d_out, dt):
     dx, dw, db = binding.linear_grad(z, x, w, activation=name, pre=z if name != "none" else None)
     assert dx.shape == (0, d_in) and dw.shape == w.shape and not dw.any() and db.shape == (d_out,) and not db.any()
     assert binding.linear(x, w, activation=name).shape == (0, d_out)
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=str)
+@pytest.mark.parametrize("size", [(200, 70, 40), (4096, 64, 4096), (40000, 72, 200)], ids=str)
+def test_rows_past_32_bits(size, dt):
+    """x and dy as columns of matrices so wide that their last rows lie past 2^31 numbers."""
+    rows, d_in, d_out = size
+    x, w, b, _, dy = make(*size, dt)
+    ld = (1 << 31) // (rows - 1) + d_in + d_out + 2
+    buffer = torch.empty(rows * ld, dtype=dt, device="cuda").view(rows, ld)
+    X, DY = buffer[:, 1:1 + d_in], buffer[:, 1 + d_in:1 + d_in + d_out]
+    X.copy_(x.cuda())
+    DY.copy_(dy.cuda())
+    assert (rows - 1) * ld >= 1 << 31
+    refs.within(binding.linear(X, w.cuda(), bias=b.cuda()), refs.linear(x, w, b, "none", None)[0], "y")
+    for g, want, what in zip(binding.linear_grad(DY, X, w.cuda()), refs.linear_grad(dy, x, w, "none", None), ("dx", "dw", "db")):
+        refs.within(g, want, what)
