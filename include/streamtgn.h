@@ -292,7 +292,7 @@ int stgn_probe_gather(const float *table, uint64_t n_rows, uint32_t row_bytes, c
                       uint32_t n_groups, uint32_t per_group, float *out, void *hip_stream);
 
 /* ---- Operators on the caller's tensors: the dense product and the attention of the model's layers and heads, with
- * their gradients.  They need no context: a program that learns the parameters of a head or a layer runs them on its own
+ * their gradients, and what stands between the products of a residual block: norm, dropout, operands in 8 bits and their product.  They need no context: a program that learns the parameters of a head or a layer runs them on its own
  * device memory, and what they give forwards is what the layers and heads of a context compute (a head's layers:
  * stgn_set_predictor_mlp).
  *  - Every pointer is a device pointer of the current device, aligned to its element; the stream is one of that device.
@@ -367,6 +367,87 @@ typedef struct {
 int stgn_attention_workspace(const stgn_attention_args *args, size_t *forward_bytes, size_t *grad_bytes);
 int stgn_attention(const stgn_attention_args *args, void *device_workspace, size_t device_bytes, void *hip_stream);
 int stgn_attention_grad(const stgn_attention_args *args, void *device_workspace, size_t device_bytes, void *hip_stream);
+
+/* Root-mean-square norm of rows, with the residual's addition.  Forward: h = x + residual (h = x where residual is NULL), r = 1 / sqrt(mean h^2 + eps),
+ * y = h r gain from the h of 32 bits; h is handed out where its pointer is not NULL (the residual stream; what the gradient reads).
+ * With q, y is written in 8 bits too (or instead: y may be NULL then): scale[row] = max |y| / 127, q = y 127 / max |y| to the nearest whole
+ * number, halves to the even one, y being the fp32 value h r gain.  A row of zeros has scale 0; a row of whose y one is infinite or no number has scale NaN and
+ * zeros in q.  The sum of squares and r are computed in fp64, r is rounded to fp32: q depends on the inputs alone.
+ * Gradient, from dy and h: dx = r gain dy - h r^3 mean(gain dy h) + dh, which is the gradient of x and of the residual; dgain = column sums of dy h r.  dh (what comes
+ * down the residual stream) may be NULL; a gradient whose pointer is NULL is not computed.
+ * x, residual, h, y, dy, dh: [rows x width]; rows lie ld_* elements apart, the numbers of a row side by side; q: int8 [rows x width], scale: fp32 [rows];
+ * gain, dgain: [width]; dx is dense.  rows may be 0 (dgain is then zeros), width lies in 1 .. 2^24, eps is finite and not negative.  Outputs overlap nothing, except
+ * that h and y may each be exactly x or exactly the residual (not both the same); tensors of equal ld_* may be different columns of one matrix. */
+typedef struct {
+  uint32_t dtype, rows, width, reserved;                      /* reserved: 0 */
+  double eps;
+  uint64_t ld_x, ld_residual, ld_h, ld_y, ld_q, ld_dy, ld_dh; /* (ld_q: in bytes) */
+  const void *x, *residual, *gain;                            /* x, residual: forward only */
+  void *h, *y;                                                /* forward: written (nullable); gradient: h is read, y is not */
+  int8_t *q;
+  float *scale;
+  const void *dy, *dh;                                        /* gradient only, as all that follow */
+  void *dx, *dgain;
+} stgn_rms_norm_args;
+
+/* Workspace bytes of the forward call and of the gradient (each nullable; the gradient's depends on whether dgain is NULL). */
+int stgn_rms_norm_workspace(const stgn_rms_norm_args *args, size_t *forward_bytes, size_t *grad_bytes);
+int stgn_rms_norm(const stgn_rms_norm_args *args, void *device_workspace, size_t device_bytes, void *hip_stream);
+int stgn_rms_norm_grad(const stgn_rms_norm_args *args, void *device_workspace, size_t device_bytes, void *hip_stream);
+
+/* A matrix in 8 bits, the operands of stgn_linear_i8.  columns = 0: a scale for each row, q: [rows x width] (activations).  columns = 1: a scale for
+ * each column and q turned over, [width x rows] (a weight [d_in x d_out] becomes [d_out x d_in]).  Scales and numbers as in stgn_rms_norm, from x itself.
+ * x: [rows x width], ld_x elements apart; q's rows lie ld_q bytes apart; scale: fp32 [rows or width].  rows may be 0 (scales of columns are then 0), width lies
+ * in 1 .. 2^24.  Outputs overlap nothing. */
+typedef struct {
+  uint32_t dtype, columns, rows, width;
+  uint64_t ld_x, ld_q;
+  const void *x;
+  int8_t *q;
+  float *scale;
+} stgn_quantize_args;
+
+int stgn_quantize_workspace(const stgn_quantize_args *args, size_t *bytes);
+int stgn_quantize(const stgn_quantize_args *args, void *device_workspace, size_t device_bytes, void *hip_stream);
+
+/* Dense product of operands in 8 bits: y = act(x_scale[row] w_scale[column] sum_k x[row][k] w[column][k] + bias) + residual.  The sums are exact 32-bit integers, all
+ * that follows is fp32; dtype is the type of bias, residual and y.
+ * x: int8 [rows x d_in], w: int8 [d_out x d_in] (k along both operands' rows), ld_x and ld_w bytes apart; x_scale, w_scale: fp32 [rows], [d_out];
+ * bias: [d_out]; residual, y: [rows x d_out], ld_* elements apart.  bias and residual may be NULL.  rows may be 0, d_in lies in 1 .. 131,071 (sums of products of -128 stay
+ * 32-bit numbers), d_out in 1 .. 2^24.  y overlaps nothing, except that it may be exactly the residual; residual and y of equal ld_* may be different columns of one
+ * matrix. */
+typedef struct {
+  uint32_t dtype, activation;
+  uint32_t rows, d_in, d_out;
+  uint32_t reserved;                                          /* 0 */
+  uint64_t ld_x, ld_w, ld_residual, ld_y;
+  const int8_t *x, *w;
+  const float *x_scale, *w_scale;
+  const void *bias, *residual;
+  void *y;
+} stgn_linear_i8_args;
+
+int stgn_linear_i8_workspace(const stgn_linear_i8_args *args, size_t *bytes);
+int stgn_linear_i8(const stgn_linear_i8_args *args, void *device_workspace, size_t device_bytes, void *hip_stream);
+
+/* Dropout with the residual's addition: y = residual + (kept ? x / (1 - p) : 0).  The mask is stored nowhere: number j of row i is kept where the 16 bits that Philox
+ * 4x32-10 gives for it are not below border = round(65536 p), p in effect being border / 65536.  Key: rng[0] (seed); counter words: group, group >> 32 | site << 16,
+ * rng[1] (step), rng[1] >> 32, with group = i ceil(width / 8) + j / 8; number j takes half j % 2 (0: the low one) of result word j % 8 / 2.  The mask depends on seed, step, site, i, j
+ * and width alone: the gradient is the same call on dy without a residual (the residual's is dy), and a captured call draws another mask when the
+ * program writes another step into rng.  What is dropped is 0, whatever it holds.
+ * x, residual, y: [rows x width], ld_* elements apart; rng: uint64 [2] on the device, 8-byte aligned, read when the stream executes the call.  p lies in 0 .. 1 (from 1 - 2^-17 on
+ * all is dropped), site in 0 .. 65535, width in 1 .. 2^24; residual may be NULL, rows may be 0.  y overlaps nothing, except that it may be exactly x or exactly the
+ * residual; tensors of equal ld_* may be different columns of one matrix. */
+typedef struct {
+  uint32_t dtype, rows, width, site;
+  double p;
+  uint64_t ld_x, ld_residual, ld_y;
+  const void *x, *residual;
+  void *y;
+  const uint64_t *rng;
+} stgn_dropout_args;
+
+int stgn_dropout(const stgn_dropout_args *args, void *hip_stream);
 
 /* NULL ctx: message of the thread's last failed call without a context (create, workspace queries, operators), or where none of
  * the thread's has failed, of any thread's last create or query.  Valid until the thread's next call without a context. */

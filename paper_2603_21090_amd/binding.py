@@ -62,9 +62,34 @@ class AttentionArgs(C.Structure):
                [(n, C.c_void_p) for n in ("q_lens", "k_lens", "q", "k", "v", "out", "lse", "dout", "dq", "dk", "dv")]
 
 
-# the same two, packed at once: a call's arguments cost the host a microsecond, not one per field
+class RmsNormArgs(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("dtype", "rows", "width", "reserved")] + [("eps", C.c_double)] + \
+               [(n, C.c_uint64) for n in ("ld_x", "ld_residual", "ld_h", "ld_y", "ld_q", "ld_dy", "ld_dh")] + \
+               [(n, C.c_void_p) for n in ("x", "residual", "gain", "h", "y", "q", "scale", "dy", "dh", "dx", "dgain")]
+
+
+class QuantizeArgs(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("dtype", "columns", "rows", "width")] + [(n, C.c_uint64) for n in ("ld_x", "ld_q")] + \
+               [(n, C.c_void_p) for n in ("x", "q", "scale")]
+
+
+class LinearI8Args(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("dtype", "activation", "rows", "d_in", "d_out", "reserved")] + \
+               [(n, C.c_uint64) for n in ("ld_x", "ld_w", "ld_residual", "ld_y")] + \
+               [(n, C.c_void_p) for n in ("x", "w", "x_scale", "w_scale", "bias", "residual", "y")]
+
+
+class DropoutArgs(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("dtype", "rows", "width", "site")] + [("p", C.c_double)] + \
+               [(n, C.c_uint64) for n in ("ld_x", "ld_residual", "ld_y")] + [(n, C.c_void_p) for n in ("x", "residual", "y", "rng")]
+
+
+# the same, packed at once: a call's arguments cost the host a microsecond, not one per field
 _PACK_LINEAR, _PACK_ATTENTION = struct.Struct("@6I6Q10P"), struct.Struct("@9If15Q11P")
+_PACK_NORM, _PACK_QUANTIZE, _PACK_LINEAR_I8, _PACK_DROPOUT = map(struct.Struct, ("@4Id7Q11P", "@4I2Q3P", "@6I4Q7P", "@4Id3Q4P"))
 assert _PACK_LINEAR.size == C.sizeof(LinearArgs) and _PACK_ATTENTION.size == C.sizeof(AttentionArgs)
+assert _PACK_NORM.size == C.sizeof(RmsNormArgs) and _PACK_QUANTIZE.size == C.sizeof(QuantizeArgs)
+assert _PACK_LINEAR_I8.size == C.sizeof(LinearI8Args) and _PACK_DROPOUT.size == C.sizeof(DropoutArgs)
 
 
 class StgnError(RuntimeError):
@@ -81,7 +106,8 @@ EXPORTS = ("stgn_query_workspace", "stgn_create", "stgn_destroy", "stgn_ingest_b
            "stgn_set_predictor", "stgn_predict_batch", "stgn_predict_batch_static", "stgn_drift_status",
            "stgn_maintain", "stgn_probe_gather", "stgn_linear_workspace", "stgn_linear", "stgn_linear_grad",
            "stgn_attention_workspace", "stgn_attention", "stgn_attention_grad", "stgn_predictor_mlp_workspace",
-           "stgn_set_predictor_mlp")
+           "stgn_set_predictor_mlp", "stgn_rms_norm_workspace", "stgn_rms_norm", "stgn_rms_norm_grad", "stgn_quantize_workspace", "stgn_quantize",
+           "stgn_linear_i8_workspace", "stgn_linear_i8", "stgn_dropout")
 
 
 def load_library():
@@ -117,10 +143,14 @@ def load_library():
     L.stgn_drift_status.argtypes = [vp, C.POINTER(C.c_double), _u32p, vp]
     L.stgn_maintain.argtypes = [vp, C.c_double, C.c_double, C.POINTER(C.c_int), _u32p]
     L.stgn_probe_gather.argtypes = [vp, C.c_uint64, C.c_uint32, vp, C.c_uint32, C.c_uint32, vp, vp]
-    for op in ("linear", "attention"):
+    for op in ("linear", "attention", "rms_norm"):
         getattr(L, f"stgn_{op}_workspace").argtypes = [vp, vp, vp]
         for name in (f"stgn_{op}", f"stgn_{op}_grad"):
             getattr(L, name).argtypes = [vp, vp, C.c_size_t, vp]
+    for op in ("quantize", "linear_i8"):
+        getattr(L, f"stgn_{op}_workspace").argtypes = [vp, vp]
+        getattr(L, f"stgn_{op}").argtypes = [vp, vp, C.c_size_t, vp]
+    L.stgn_dropout.argtypes = [vp, vp]
     L.stgn_last_error.argtypes = [vp]
     L.stgn_last_error.restype = C.c_char_p
     L.stgn_version.restype = C.c_char_p
@@ -200,15 +230,17 @@ def _ld(t):
 
 
 def _run_operator(ask, call, args, grad, device):
-    """Workspace of the call (the caching allocator's, on the current stream), then the call."""
+    """Workspace of the call (the caching allocator's, on the current stream), then the call.  ask: None where the call needs none; grad: None where
+    there is no gradient to ask for."""
     import torch
     if device.type != "cuda":
         raise ValueError(f"tensors must be on the GPU, not on {device}")
     if torch.cuda.current_device() != device.index:
         with torch.cuda.device(device):
             return _run_operator(ask, call, args, grad, device)
-    n = C.c_size_t(0)
-    rc = ask(args, None, C.byref(n)) if grad else ask(args, C.byref(n), None)
+    n, rc = C.c_size_t(0), 0
+    if ask is not None:
+        rc = ask(args, C.byref(n)) if grad is None else ask(args, None, C.byref(n)) if grad else ask(args, C.byref(n), None)
     if rc == 0:
         size, ws = n.value, None
         if size:
@@ -321,6 +353,124 @@ def attention_grad(dout, q, k, v, out, lse, q_lens=None, k_lens=None, causal=Fal
                                 dq.data_ptr(), dk.data_ptr(), dv.data_ptr())
     _run_operator(L.stgn_attention_workspace, L.stgn_attention_grad, args, True, q.device)
     return dq, dk, dv
+
+
+def _rows(name, t, like=None):
+    """The matrix itself, or an error; of `like`'s type, device and shape."""
+    if t.dim() != 2 or t.shape[1] < 1:
+        raise ValueError(f"{name} must be a matrix with one column at least")
+    return _expect(name, t, t if like is None else like, t.shape if like is None else like.shape)
+
+
+def _rms_norm(x, gain, residual, eps, eight, need_y):
+    import torch
+    L = load_library()
+    xp, code, (rows, width) = _rows("x", x), _dtype_code(x), x.shape
+    gp = _expect("gain", gain, x, (width,))
+    rp = _rows("residual", residual, x) if residual is not None else 0
+    h = torch.empty(x.shape, dtype=x.dtype, device=x.device) if residual is not None else None
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_y else None
+    q = torch.empty(x.shape, dtype=torch.int8, device=x.device) if eight else None
+    scale = torch.empty(rows, dtype=torch.float32, device=x.device) if eight else None
+    at = [0 if t is None else t.data_ptr() for t in (h, y, q, scale)]
+    args = _PACK_NORM.pack(code, rows, width, 0, eps, _ld(x), _ld(residual) if residual is not None else 0, width, width, width, 0, 0, xp, rp, gp, *at, 0, 0, 0, 0)
+    _run_operator(None, L.stgn_rms_norm, args, False, x.device)
+    return y, q, scale, h
+
+
+def rms_norm(x, gain, residual=None, eps=1e-6):
+    """y = h gain / sqrt(mean h^2 + eps) of each row, h = x + residual (stgn_rms_norm): x and residual [rows, width], gain [width], of one type
+    (float32, bfloat16, float16).  Returns y, or (y, h) with a residual: h is the residual stream, and what rms_norm_grad reads (x where there is no
+    residual).  No autograd graph: rms_norm_grad computes the gradients."""
+    y, _, _, h = _rms_norm(x, gain, residual, eps, False, True)
+    return y if residual is None else (y, h)
+
+
+def rms_norm_i8(x, gain, residual=None, eps=1e-6, keep_y=False):
+    """The same norm with y in 8 bits, for linear_i8: (q int8 [rows, width], scale float32 [rows]), then h with a residual, then y with keep_y."""
+    y, q, scale, h = _rms_norm(x, gain, residual, eps, True, keep_y)
+    return (q, scale) + (() if residual is None else (h,)) + ((y,) if keep_y else ())
+
+
+def rms_norm_grad(dy, h, gain, dh=None, eps=1e-6, need_x=True, need_gain=True):
+    """Gradients of rms_norm (stgn_rms_norm_grad): (dx, dgain), None for those not asked for.  h: what rms_norm returned beside y, or its x
+    where there was no residual; dh: the gradient that comes down the residual stream, added to dx.  The residual's gradient is dx too."""
+    import torch
+    L = load_library()
+    hp, code, (rows, width) = _rows("h", h), _dtype_code(h), h.shape
+    yp, gp = _rows("dy", dy, h), _expect("gain", gain, h, (width,))
+    dp = _rows("dh", dh, h) if dh is not None else 0
+    dx = torch.empty(h.shape, dtype=h.dtype, device=h.device) if need_x else None
+    dgain = torch.empty(width, dtype=h.dtype, device=h.device) if need_gain else None
+    args = _PACK_NORM.pack(code, rows, width, 0, eps, 0, 0, _ld(h), 0, 0, _ld(dy), _ld(dh) if dh is not None else 0, 0, 0, gp, hp, 0, 0, 0, yp, dp,
+                           dx.data_ptr() if need_x else 0, dgain.data_ptr() if need_gain else 0)
+    _run_operator(L.stgn_rms_norm_workspace, L.stgn_rms_norm_grad, args, True, h.device)
+    return dx, dgain
+
+
+def quantize(x, columns=False):
+    """A matrix in 8 bits, for linear_i8 (stgn_quantize): (q int8, scale float32), x = q times its scale to half a step.  Rows: q [rows, width], scale
+    [rows].  columns=True, for a weight [d_in, d_out]: q [d_out, d_in], scale [d_out]."""
+    import torch
+    L = load_library()
+    xp, code, (rows, width) = _rows("x", x), _dtype_code(x), x.shape
+    q = torch.empty((width, rows) if columns else (rows, width), dtype=torch.int8, device=x.device)
+    scale = torch.empty(q.shape[0], dtype=torch.float32, device=x.device)
+    args = _PACK_QUANTIZE.pack(code, 1 if columns else 0, rows, width, _ld(x), q.shape[1], xp, q.data_ptr(), scale.data_ptr())
+    _run_operator(L.stgn_quantize_workspace if columns else None, L.stgn_quantize, args, None, x.device)
+    return q, scale
+
+
+def linear_i8(x, x_scale, w, w_scale, bias=None, activation="none", residual=None, dtype=None):
+    """y = act(x_scale w_scale sum x w + bias) + residual from operands in 8 bits (stgn_linear_i8): x int8 [rows, d_in], x_scale float32 [rows], w int8 [d_out,
+    d_in], w_scale float32 [d_out], as rms_norm_i8 and quantize give them; bias [d_out] and residual [rows, d_out] of y's type, which is `dtype`,
+    else theirs, else bfloat16.  activation: as in linear."""
+    import torch
+    L = load_library()
+    if x.dim() != 2 or w.dim() != 2:
+        raise ValueError("x and w must be matrices")
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}")
+    for name, t, want in (("x", x, torch.int8), ("x_scale", x_scale, torch.float32), ("w_scale", w_scale, torch.float32)):
+        if t.dtype != want:
+            raise ValueError(f"{name}: {t.dtype}, expected {want}")
+    (rows, d_in), d_out = x.shape, w.shape[0]
+    xp, wp = _expect("x", x, x, x.shape), _expect("w", w, x, (d_out, d_in))
+    if x_scale.device != x.device:
+        raise ValueError(f"x_scale: on {x_scale.device}, expected {x.device}")
+    sp, tp = _expect("x_scale", x_scale, x_scale, (rows,)), _expect("w_scale", w_scale, x_scale, (d_out,))
+    if dtype is None:
+        dtype = bias.dtype if bias is not None else residual.dtype if residual is not None else torch.bfloat16
+    y = torch.empty((rows, d_out), dtype=dtype, device=x.device)
+    bp = _expect("bias", bias, y, (d_out,)) if bias is not None else 0
+    rp = _expect("residual", residual, y, y.shape) if residual is not None else 0
+    args = _PACK_LINEAR_I8.pack(_dtype_code(y), ACTIVATIONS[activation], rows, d_in, d_out, 0, _ld(x), _ld(w), _ld(residual) if rp else 0, d_out,
+                                xp, wp, sp, tp, bp, rp, y.data_ptr())
+    _run_operator(L.stgn_linear_i8_workspace, L.stgn_linear_i8, args, None, x.device)
+    return y
+
+
+def dropout(x, p, rng, site=0, residual=None):
+    """y = residual + (kept ? x / (1 - p) : 0) (stgn_dropout): x and residual [rows, width] of one type.  rng: int64 [2] on the device, seed and step; site:
+    which of a program's dropouts this is (0 .. 65535).  The mask is a function of these and of the place alone: write another step (rng[1] += 1) behind
+    the backward pass, not between it and the forward one.  The residual's gradient is dy, x's is dropout_grad."""
+    import torch
+    L = load_library()
+    xp, code, (rows, width) = _rows("x", x), _dtype_code(x), x.shape
+    if rng.dtype != torch.int64 or rng.device != x.device or rng.shape != (2,) or not rng.is_contiguous():
+        raise ValueError(f"rng: a dense int64 tensor [2] on {x.device} is expected")
+    rp = _rows("residual", residual, x) if residual is not None else 0
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if not 0 <= site <= 65535:
+        raise ValueError("site must lie in 0 .. 65535")
+    args = _PACK_DROPOUT.pack(code, rows, width, site, p, _ld(x), _ld(residual) if residual is not None else 0, width, xp, rp, y.data_ptr(), rng.data_ptr())
+    _run_operator(None, lambda a, ws, size, stream: L.stgn_dropout(a, stream), args, None, x.device)
+    return y
+
+
+def dropout_grad(dy, p, rng, site=0):
+    """Gradient of dropout's x: the same mask and factor on dy, with the seed, step and site of the forward call."""
+    return dropout(dy, p, rng, site)
 
 
 def _marshal_weights(weights: dict, layers: int, has_memory: bool):

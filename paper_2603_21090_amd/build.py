@@ -11,8 +11,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libstreamtgn.so")
 SOURCES = ["api.hip", "ingest_kernels.hip", "memory_kernels.hip", "frontier_kernels.hip", "embed_kernels.hip",
-           "layer_h1.hip", "layer_h2.hip", "layer_h4.hip", "operators_api.hip",
-           *(f"{op}_{t}.hip" for op in ("linear", "attention", "attention_rows") for t in ("f32", "bf16", "f16"))]
+           "layer_h1.hip", "layer_h2.hip", "layer_h4.hip", "operators_api.hip", "dropout.hip",
+           *(f"{op}_{t}.hip" for op in ("linear", "attention", "attention_rows", "norm", "linear_i8") for t in ("f32", "bf16", "f16"))]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-value", "-Wno-unused-result",
          "-Wno-pass-failed",
          # packed fp32 forms are kept out of the generated code on this target

@@ -1,0 +1,6 @@
+// dense products of operands in 8 bits with outputs of one element type
+#include "linear_i8.h"
+
+namespace stgn {
+hipError_t linear_i8_f32(const Linear8Args& a, void* ws, hipStream_t s) { return dense8::forward<float>(a, ws, s); }
+}  // namespace stgn

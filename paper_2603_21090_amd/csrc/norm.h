@@ -1,0 +1,623 @@
+// The root-mean-square norm of rows with the residual's addition, its gradient, and rows or columns in 8 bits with scales.
+//
+//   h = x + residual,  r = 1 / sqrt(mean h^2 + eps),  y = h r g;       scale = max |y| / 127,  q = y 127 / max |y| to the nearest whole number
+//   dx = r (g dy - h r mean(r g dy h)) + dh,                            dg = column sums of dy h r
+//
+// Bytes bound all of it: a row is read once and stays in its lanes' registers between its sums and its outputs.  LANES lanes hold a row in NP
+// pieces of 16 bytes each, as few lanes as hold it: 16 lanes (sixteen rows a workgroup) to 1,024 (one); longer rows are read again.
+// The sum of squares is a sum of 64 bits: r, and with it a number in 8 bits whose value lies next to a border, then does not hang on the
+// order of the sum, and no magnitude of 32 bits overflows it.
+#pragma once
+#include <math.h>
+
+#include "operators.h"
+#include "tile_ops.h"
+
+namespace stgn {
+namespace norm {
+
+template <class T> constexpr int kE = Elem<T>::E;
+
+template <class T>
+__device__ inline void unpack(const u32x4& r, float (&v)[kE<T>]) {
+  const typename Elem<T>::Frag f = __builtin_bit_cast(typename Elem<T>::Frag, r);
+#pragma unroll
+  for (int j = 0; j < kE<T>; ++j) v[j] = (float)f[j];
+}
+template <class T>
+__device__ inline void store_piece(T* row, int c, int width, const float (&v)[kE<T>]) {
+  if constexpr (kE<T> == 4) store4(row, c, width, floatx4{v[0], v[1], v[2], v[3]});
+  else store8(row, c, width, floatx4{v[0], v[1], v[2], v[3]}, floatx4{v[4], v[5], v[6], v[7]});
+}
+// a piece of a row, read so that no other lane's elements are touched (where a row may be written in place while others are still read)
+template <class T>
+__device__ inline u32x4 load_own(const T* row, int c, int width) {
+  return c + kE<T> <= width ? load16<T, kWhole>(row + c, kE<T>) : load16<T, kShort>(row + c, width - c);
+}
+
+template <int E>
+__device__ inline void store_bytes(int8_t* row, int c, int width, const int (&q)[E]) {
+  uint32_t w[E / 4];
+#pragma unroll
+  for (int i = 0; i < E / 4; ++i)
+    w[i] = (q[4 * i] & 255) | (q[4 * i + 1] & 255) << 8 | (q[4 * i + 2] & 255) << 16 | (uint32_t)q[4 * i + 3] << 24;
+  if (c + E <= width) {
+    if constexpr (E == 4) *reinterpret_cast<u32_any*>(row + c) = w[0];
+    else *reinterpret_cast<u32x2_any*>(row + c) = u32x2_any{w[0], w[1]};
+  } else {
+#pragma unroll
+    for (int j = 0; j < E - 1; ++j)
+      if (c + j < width) row[c + j] = (int8_t)q[j];
+  }
+}
+
+// y 127 / top to the nearest whole number, halves to the even one; up = 127 / top in 64 bits.  The product is off by 2^-45 at most.  A quotient of
+// numbers of 24 bits that is no half is 2^-34 or more away from one, so rounding it to multiples of 2^-40 first makes halves exact and
+// moves nothing across one: q is the definition's number for every y and top.
+__device__ inline int to_eight(float y, double up) {
+  constexpr double kSnap = 6144.0, kWhole52 = 6755399441055744.0;        // 1.5 x 2^12, 1.5 x 2^52
+  const double t = ((double)y * up + kSnap) - kSnap;
+  return (int)(uint32_t)__builtin_bit_cast(uint64_t, t + kWhole52);
+}
+// of the bits of a row's largest magnitude; a row with an infinity or a NaN has scale NaN and zeros, so that what is computed from it shows them
+__device__ inline float scale_of(uint32_t top) { return top >= 0x7F800000u ? __builtin_nanf("") : (float)((double)__builtin_bit_cast(float, top) / 127.0); }
+__device__ inline double up_of(uint32_t top) {
+  return top == 0u || top >= 0x7F800000u ? 0.0 : 127.0 / (double)__builtin_bit_cast(float, top);
+}
+__device__ inline int to_eight(float y, double up, uint32_t top) { return top >= 0x7F800000u ? 0 : to_eight(y, up); }
+__device__ inline uint32_t magnitude(float y) { return __builtin_bit_cast(uint32_t, y) & 0x7FFFFFFFu; }
+
+__device__ inline float inverse_root(double sum, int width, double eps) {
+  const double r = 1.0 / sqrt(sum / width + eps);
+  return r > 3.4028234663852886e38 ? 3.4028234663852886e38f : (float)r;          // (rows of zeros with eps = 0 stay zeros)
+}
+
+// h r g in fp32.  (fp16: left to itself, the compiler takes the last product and the rounding to fp16 as one where nothing else needs the fp32 value, and y
+// would have other bits beside 8-bit outputs than without them.)
+template <class T>
+__device__ inline float normed(float h, float r, float g) {
+  float y = h * r * g;
+  if constexpr (std::is_same<T, _Float16>::value) asm("" : "+v"(y));
+  return y;
+}
+
+// value of all LANES lanes that hold a row; `at`: LDS of its own for rows that lie in several waves
+template <int LANES, class V, class F>
+__device__ inline V across(V v, V* at, F f) {
+#pragma unroll
+  for (int d = (LANES < 64 ? LANES : 64) / 2; d > 0; d >>= 1) v = f(v, (V)__shfl_xor(v, d));
+  if constexpr (LANES > 64) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = at[0];
+#pragma unroll
+    for (int w = 1; w < LANES / 64; ++w) v = f(v, at[w]);
+  }
+  return v;
+}
+template <int LANES>
+__device__ inline double sum_across(double v, double* at) { return across<LANES>(v, at, [](double a, double b) { return a + b; }); }
+template <int LANES>
+__device__ inline uint32_t top_across(uint32_t v, uint32_t* at) { return across<LANES>(v, at, [](uint32_t a, uint32_t b) { return a > b ? a : b; }); }
+
+constexpr int block_of(int lanes) { return lanes < 256 ? 256 : lanes; }
+
+enum Kind { kNorm, kNorm8, kRows8 };                          // y; 8 bits of y (and y); 8 bits of x
+
+// Rows whose pieces stay in registers.  All of a row is read before any of it is written: outputs may lie where the inputs do.
+template <class T, int LANES, int NP, Kind KIND>
+__global__ __launch_bounds__(block_of(LANES)) void rows_kernel(NormArgs a) {
+  constexpr int E = kE<T>, PER = block_of(LANES) / LANES;
+  __shared__ double sums[LANES > 64 ? LANES / 64 : 1];
+  __shared__ uint32_t tops[LANES > 64 ? LANES / 64 : 1];
+  const int lane = (int)threadIdx.x % LANES;
+  const RowEnd end = row_end<T>(a.width);
+  for (int64_t row = (int64_t)blockIdx.x * PER + (int)threadIdx.x / LANES; row < a.rows; row += (int64_t)gridDim.x * PER) {
+    const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
+    const T* res = a.residual ? static_cast<const T*>(a.residual) + row * a.ld_res : nullptr;
+    float v[NP][E];
+    by_end(end, [&](auto e) {
+      constexpr RowEnd END = decltype(e)::value;
+      u32x4 rx[NP], rr[NP];
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const int c = (lane + i * LANES) * E;
+        rx[i] = rr[i] = u32x4{0, 0, 0, 0};
+        if (c < a.width) {
+          rx[i] = load16<T, END>(x + c, a.width - c);
+          if (res) rr[i] = load16<T, END>(res + c, a.width - c);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        unpack<T>(rx[i], v[i]);
+        if (res) {
+          float u[E];
+          unpack<T>(rr[i], u);
+#pragma unroll
+          for (int j = 0; j < E; ++j) v[i][j] += u[j];
+        }
+      }
+    });
+    if constexpr (KIND != kRows8) {
+      double sum = 0.0;
+#pragma unroll
+      for (int i = 0; i < NP; ++i)
+#pragma unroll
+        for (int j = 0; j < E; ++j) sum = fma((double)v[i][j], (double)v[i][j], sum);
+      const float r = inverse_root(sum_across<LANES>(sum, sums), a.width, a.eps);
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const int c = (lane + i * LANES) * E;
+        if (c >= a.width) continue;
+        if (a.h) store_piece(static_cast<T*>(a.h) + row * a.ld_h, c, a.width, v[i]);
+        float g[E];
+        unpack<T>(load_own(static_cast<const T*>(a.gain), c, a.width), g);
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[i][j] = normed<T>(v[i][j], r, g[j]);
+        if (KIND == kNorm || a.y) store_piece(static_cast<T*>(a.y) + row * a.ld_y, c, a.width, v[i]);
+      }
+    }
+    if constexpr (KIND != kNorm) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < NP; ++i)
+#pragma unroll
+        for (int j = 0; j < E; ++j) top = max(top, (lane + i * LANES) * E + j < a.width ? magnitude(v[i][j]) : 0u);
+      top = top_across<LANES>(top, tops);
+      const double up = up_of(top);
+      if (lane == 0) a.scale[row] = scale_of(top);
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const int c = (lane + i * LANES) * E;
+        if (c >= a.width) continue;
+        int q[E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) q[j] = to_eight(v[i][j], up, top);
+        store_bytes<E>(a.q + row * a.ld_q, c, a.width, q);
+      }
+    }
+  }
+}
+
+// Rows longer than 1,024 lanes hold: read once a sum and once for the outputs.
+template <class T, Kind KIND>
+__global__ __launch_bounds__(1024) void long_rows_kernel(NormArgs a) {
+  constexpr int E = kE<T>, LANES = 1024;
+  __shared__ double sums[LANES / 64];
+  __shared__ uint32_t tops[LANES / 64];
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
+    const T* res = a.residual ? static_cast<const T*>(a.residual) + row * a.ld_res : nullptr;
+    auto each = [&](auto f) {
+      for (int c = (int)threadIdx.x * E; c < a.width; c += LANES * E) {
+        float v[E], u[E];
+        unpack<T>(load_own(x, c, a.width), v);
+        if (res) {
+          unpack<T>(load_own(res, c, a.width), u);
+#pragma unroll
+          for (int j = 0; j < E; ++j) v[j] += u[j];
+        }
+        f(c, v);
+      }
+    };
+    float r = 1.f;
+    if constexpr (KIND != kRows8) {
+      double sum = 0.0;
+      each([&](int, float (&v)[E]) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) sum = fma((double)v[j], (double)v[j], sum);
+      });
+      r = inverse_root(sum_across<LANES>(sum, sums), a.width, a.eps);
+    }
+    auto norm = [&](int c, float (&v)[E]) {
+      if constexpr (KIND != kRows8) {
+        float g[E];
+        unpack<T>(load_own(static_cast<const T*>(a.gain), c, a.width), g);
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[j] = normed<T>(v[j], r, g[j]);
+      }
+    };
+    uint32_t top = 0;
+    if constexpr (KIND != kNorm) {
+      each([&](int c, float (&v)[E]) {
+        norm(c, v);
+#pragma unroll
+        for (int j = 0; j < E; ++j) top = max(top, c + j < a.width ? magnitude(v[j]) : 0u);
+      });
+      top = top_across<LANES>(top, tops);
+      if (threadIdx.x == 0) a.scale[row] = scale_of(top);
+    }
+    const double up = up_of(top);
+    each([&](int c, float (&v)[E]) {
+      if (a.h) store_piece(static_cast<T*>(a.h) + row * a.ld_h, c, a.width, v);
+      norm(c, v);
+      if (KIND != kRows8 && (KIND == kNorm || a.y)) store_piece(static_cast<T*>(a.y) + row * a.ld_y, c, a.width, v);
+      if constexpr (KIND != kNorm) {
+        int q[E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) q[j] = to_eight(v[j], up, top);
+        store_bytes<E>(a.q + row * a.ld_q, c, a.width, q);
+      }
+    });
+  }
+}
+
+constexpr int64_t kMostBlocks = 1 << 20;                      // of a launch; more rows go round again
+
+// f(lanes, pieces) for the fewest lanes that hold a row, or longer() where none do
+template <class T, class F, class L>
+hipError_t by_width(int width, F f, L longer) {
+  constexpr int E = kE<T>;
+#define STGN_HOLDS(lanes, pieces) \
+  if (width <= lanes * pieces * E) return f(std::integral_constant<int, lanes>(), std::integral_constant<int, pieces>());
+  STGN_HOLDS(16, 1)
+  STGN_HOLDS(64, 1)
+  STGN_HOLDS(64, 2)
+  STGN_HOLDS(64, 4)
+  STGN_HOLDS(256, 2)
+  STGN_HOLDS(256, 4)
+  STGN_HOLDS(1024, 2)
+  STGN_HOLDS(1024, 4)
+#undef STGN_HOLDS
+  return longer();
+}
+
+inline int64_t blocks_for(int64_t rows, int lanes) {
+  const int per = block_of(lanes) / lanes;
+  const int64_t n = (rows + per - 1) / per;
+  return n < kMostBlocks ? n : kMostBlocks;
+}
+
+template <class T, Kind KIND>
+hipError_t rows_of(const NormArgs& a, hipStream_t s) {
+  return by_width<T>(
+      a.width,
+      [&](auto lanes, auto pieces) {
+        constexpr int L = decltype(lanes)::value, N = decltype(pieces)::value;
+        return launch(rows_kernel<T, L, N, KIND>, blocks_for(a.rows, L), block_of(L), s, a);
+      },
+      [&]() { return launch(long_rows_kernel<T, KIND>, a.rows < kMostBlocks ? a.rows : kMostBlocks, 1024, s, a); });
+}
+
+// ---- gradient
+
+// r, and r mean(g dy h): dx = r (g dy - (h r) back), whose factors neither overflow nor vanish where h is large or small
+struct Back { float r, back; };
+__device__ inline Back back_of(double squares, double dots, int width, double eps) {
+  Back b;
+  b.r = inverse_root(squares, width, eps);
+  b.back = (float)((double)b.r * (dots / width));
+  return b;
+}
+
+// A workgroup walks down the rows and keeps the gain's gradient of its rows in registers: one partial sum a column and workgroup.
+template <class T, int LANES, int NP>
+__global__ __launch_bounds__(block_of(LANES)) void grad_kernel(NormGradArgs a, float* part) {
+  constexpr int E = kE<T>, PER = block_of(LANES) / LANES;
+  __shared__ double sums[2][LANES > 64 ? LANES / 64 : 1];
+  __shared__ float fold[PER > 1 ? PER : 1][PER > 1 ? LANES * NP * E : 1];
+  const int lane = (int)threadIdx.x % LANES;
+  const RowEnd end = row_end<T>(a.width);
+  float acc[NP][E];
+#pragma unroll
+  for (int i = 0; i < NP; ++i)
+#pragma unroll
+    for (int j = 0; j < E; ++j) acc[i][j] = 0.f;
+  for (int64_t row = (int64_t)blockIdx.x * PER + (int)threadIdx.x / LANES; row < a.rows; row += (int64_t)gridDim.x * PER) {
+    const T* h = static_cast<const T*>(a.h) + row * a.ld_h;
+    const T* dy = static_cast<const T*>(a.dy) + row * a.ld_dy;
+    const T* dh = a.dh ? static_cast<const T*>(a.dh) + row * a.ld_dh : nullptr;
+    u32x4 rh[NP], ry[NP], rd[NP];
+    by_end(end, [&](auto e) {
+      constexpr RowEnd END = decltype(e)::value;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const int c = (lane + i * LANES) * E;
+        rh[i] = ry[i] = rd[i] = u32x4{0, 0, 0, 0};
+        if (c < a.width) {
+          rh[i] = load16<T, END>(h + c, a.width - c);
+          ry[i] = load16<T, END>(dy + c, a.width - c);
+          if (dh) rd[i] = load16<T, END>(dh + c, a.width - c);
+        }
+      }
+    });
+    double squares = 0.0, dots = 0.0;
+    float t[NP][E];                                           // g dy
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int c = (lane + i * LANES) * E;
+      float hv[E], gv[E];
+      unpack<T>(rh[i], hv);
+      unpack<T>(ry[i], t[i]);
+      unpack<T>(c < a.width ? load_own(static_cast<const T*>(a.gain), c, a.width) : u32x4{0, 0, 0, 0}, gv);
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        t[i][j] *= gv[j];
+        squares = fma((double)hv[j], (double)hv[j], squares);
+        dots = fma((double)t[i][j], (double)hv[j], dots);
+      }
+    }
+    squares = sum_across<LANES>(squares, sums[0]);
+    dots = sum_across<LANES>(dots, sums[1]);
+    const Back b = back_of(squares, dots, a.width, a.eps);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int c = (lane + i * LANES) * E;
+      float hv[E], yv[E], dv[E];
+      unpack<T>(rh[i], hv);
+      unpack<T>(ry[i], yv);
+      unpack<T>(rd[i], dv);
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        const float unit = hv[j] * b.r;
+        acc[i][j] = fmaf(yv[j], unit, acc[i][j]);
+        dv[j] = fmaf(b.r, fmaf(-unit, b.back, t[i][j]), dv[j]);
+      }
+      if (a.dx && c < a.width) store_piece(static_cast<T*>(a.dx) + row * a.ld_dx, c, a.width, dv);
+    }
+  }
+  if (!a.dgain) return;
+  if constexpr (PER > 1) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+#pragma unroll
+      for (int j = 0; j < E; ++j) fold[threadIdx.x / LANES][(lane + i * LANES) * E + j] = acc[i][j];
+    __syncthreads();
+    for (int c = (int)threadIdx.x; c < a.width; c += (int)blockDim.x) {
+      float v = fold[0][c];
+#pragma unroll
+      for (int p = 1; p < PER; ++p) v += fold[p][c];
+      if (gridDim.x > 1) part[(int64_t)blockIdx.x * a.width + c] = v;
+      else static_cast<T*>(a.dgain)[c] = (T)v;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int c = (lane + i * LANES) * E;
+      if (c >= a.width) continue;
+      if (gridDim.x > 1) {
+#pragma unroll
+        for (int j = 0; j < E; j += 4)
+          if (c + j < a.width) store4(part + (int64_t)blockIdx.x * a.width, c + j, a.width, floatx4{acc[i][j], acc[i][j + 1], acc[i][j + 2], acc[i][j + 3]});
+      } else {
+        store_piece(static_cast<T*>(a.dgain), c, a.width, acc[i]);
+      }
+    }
+  }
+}
+
+// Rows longer than the lanes hold: dx, and r of every row for the gain's gradient behind it
+template <class T>
+__global__ __launch_bounds__(1024) void long_grad_kernel(NormGradArgs a, float* r) {
+  constexpr int E = kE<T>, LANES = 1024;
+  __shared__ double sums[2][LANES / 64];
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const T* h = static_cast<const T*>(a.h) + row * a.ld_h;
+    const T* dy = static_cast<const T*>(a.dy) + row * a.ld_dy;
+    const T* dh = a.dh ? static_cast<const T*>(a.dh) + row * a.ld_dh : nullptr;
+    auto each = [&](auto f) {
+      for (int c = (int)threadIdx.x * E; c < a.width; c += LANES * E) {
+        float hv[E], t[E], g[E];
+        unpack<T>(load_own(h, c, a.width), hv);
+        unpack<T>(load_own(dy, c, a.width), t);
+        unpack<T>(load_own(static_cast<const T*>(a.gain), c, a.width), g);
+#pragma unroll
+        for (int j = 0; j < E; ++j) t[j] *= g[j];
+        f(c, hv, t);
+      }
+    };
+    double squares = 0.0, dots = 0.0;
+    each([&](int, float (&hv)[E], float (&t)[E]) {
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        squares = fma((double)hv[j], (double)hv[j], squares);
+        dots = fma((double)t[j], (double)hv[j], dots);
+      }
+    });
+    squares = sum_across<LANES>(squares, sums[0]);
+    dots = sum_across<LANES>(dots, sums[1]);
+    const Back b = back_of(squares, dots, a.width, a.eps);
+    if (a.dgain && threadIdx.x == 0) r[row] = b.r;
+    if (!a.dx) continue;
+    each([&](int c, float (&hv)[E], float (&t)[E]) {
+      float dv[E];
+      unpack<T>(dh ? load_own(dh, c, a.width) : u32x4{0, 0, 0, 0}, dv);
+#pragma unroll
+      for (int j = 0; j < E; ++j) dv[j] = fmaf(b.r, fmaf(-hv[j] * b.r, b.back, t[j]), dv[j]);
+      store_piece(static_cast<T*>(a.dx) + row * a.ld_dx, c, a.width, dv);
+    });
+  }
+}
+// ... the sums of 256 columns over a chunk of rows
+template <class T>
+__global__ __launch_bounds__(256) void long_gain_kernel(NormGradArgs a, const float* r, float* part, int rows_per) {
+  __shared__ floatx4 wsum[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int cols = (a.width + 255) / 256, n = (int)(blockIdx.x % cols) * 256 + lane * 4;
+  const int64_t chunk = blockIdx.x / cols, m1 = min((int64_t)a.rows, (chunk + 1) * rows_per);
+  floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+  if (n < a.width) {
+#pragma unroll 4
+    for (int64_t m = chunk * rows_per + wave; m < m1; m += 4)
+      acc += load4(static_cast<const T*>(a.dy) + m * a.ld_dy, n, a.width) * load4(static_cast<const T*>(a.h) + m * a.ld_h, n, a.width) * r[m];
+  }
+  wsum[wave][lane] = acc;
+  __syncthreads();
+  if (wave == 0 && n < a.width)
+    store4(part + chunk * a.width, n, a.width, (wsum[0][lane] + wsum[1][lane]) + (wsum[2][lane] + wsum[3][lane]));
+}
+
+template <class T>
+__global__ __launch_bounds__(1024) void gain_kernel(const float* part, int parts, int width, T* dgain) {
+  __shared__ float wsum[16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (int)blockIdx.x * 64 + lane;
+  float acc = 0.f;
+  if (c < width) {
+#pragma unroll 8
+    for (int i = wave; i < parts; i += 16) acc += part[(int64_t)i * width + c];
+  }
+  wsum[wave][lane] = acc;
+  __syncthreads();
+  if (wave == 0 && c < width) {
+#pragma unroll
+    for (int w = 1; w < 16; ++w) acc += wsum[w][lane];
+    dgain[c] = (T)acc;
+  }
+}
+
+inline int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+// parts: partial sums a column; of long rows: chunks of rows, and r of every row in front of the sums
+struct GradPlan { int64_t blocks; int parts, rows_per; size_t sums, total; bool is_long; };
+template <class T>
+GradPlan grad_plan(const NormGradArgs& a) {
+  GradPlan p{};
+  by_width<T>(
+      a.width,
+      [&](auto lanes, auto) {
+        p.blocks = blocks_for(a.rows, decltype(lanes)::value);
+        if (a.dgain && p.blocks > 1024) p.blocks = 1024;
+        p.parts = (int)p.blocks;
+        return hipSuccess;
+      },
+      [&]() {
+        p.is_long = true;
+        p.blocks = a.rows < kMostBlocks ? a.rows : kMostBlocks;
+        const int64_t chunks = a.rows < 64 ? 1 : a.rows < 64 * 64 ? a.rows / 64 : 64;
+        p.rows_per = (int)((a.rows + chunks - 1) / chunks);
+        if (p.rows_per < 1) p.rows_per = 1;
+        p.parts = (int)((a.rows + p.rows_per - 1) / p.rows_per);
+        return hipSuccess;
+      });
+  if (a.dgain) {
+    p.sums = p.is_long ? (size_t)up((int64_t)a.rows * sizeof(float), 256) : 0;
+    p.total = p.sums + (p.parts > 1 || p.is_long ? (size_t)p.parts * a.width * sizeof(float) : 0);
+  }
+  return p;
+}
+
+template <class T>
+hipError_t backward(const NormGradArgs& a, void* ws, hipStream_t s) {
+  const GradPlan p = grad_plan<T>(a);
+  float* part = ws ? reinterpret_cast<float*>(static_cast<char*>(ws) + p.sums) : nullptr;
+  hipError_t e = hipSuccess;
+  if (p.blocks > 0)
+    e = by_width<T>(
+        a.width,
+        [&](auto lanes, auto pieces) {
+          constexpr int L = decltype(lanes)::value, N = decltype(pieces)::value;
+          return launch(grad_kernel<T, L, N>, p.blocks, block_of(L), s, a, part);
+        },
+        [&]() {
+          hipError_t f = launch(long_grad_kernel<T>, p.blocks, 1024, s, a, static_cast<float*>(ws));
+          if (f == hipSuccess && a.dgain)
+            f = launch(long_gain_kernel<T>, (int64_t)p.parts * ((a.width + 255) / 256), 256, s, a, (const float*)ws, part, p.rows_per);
+          return f;
+        });
+  if (e == hipSuccess && a.dgain && (p.parts != 1 || p.is_long))
+    e = launch(gain_kernel<T>, (a.width + 63) / 64, 1024, s, (const float*)part, p.parts, a.width, static_cast<T*>(a.dgain));
+  return e;
+}
+
+// ---- columns in 8 bits: largest magnitudes of 256 columns over chunks of rows, then tiles turned over through LDS
+
+template <class T>
+__global__ __launch_bounds__(256) void column_tops_kernel(ColumnsArgs a, uint32_t* tops, int rows_per) {
+  __shared__ uint32_t wtop[4][256];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int cols = (a.width + 255) / 256, n0 = (int)(blockIdx.x % cols) * 256, n = n0 + lane * 4;
+  const int64_t chunk = blockIdx.x / cols, m1 = min((int64_t)a.rows, (chunk + 1) * rows_per);
+  uint32_t top[4] = {0, 0, 0, 0};
+  if (n < a.width) {
+#pragma unroll 8
+    for (int64_t m = chunk * rows_per + wave; m < m1; m += 4) {
+      const floatx4 v = load4(static_cast<const T*>(a.x) + m * a.ld_x, n, a.width);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) top[j] = max(top[j], magnitude(v[j]));
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) wtop[wave][lane * 4 + j] = top[j];
+  __syncthreads();
+  const int c = (int)threadIdx.x;
+  if (n0 + c < a.width) tops[chunk * a.width + n0 + c] = max(max(wtop[0][c], wtop[1][c]), max(wtop[2][c], wtop[3][c]));
+}
+
+constexpr int kTileRows = 128, kTileCols = 64;
+
+template <class T>
+__global__ __launch_bounds__(256) void columns_kernel(ColumnsArgs a, const uint32_t* tops, int chunks) {
+  constexpr int E = kE<T>, STRIDE = kTileRows + 16;
+  __shared__ uint32_t part[4][kTileCols], top[kTileCols];
+  __shared__ __attribute__((aligned(16))) int8_t tile[kTileCols * STRIDE];
+  const int tiles_n = (a.width + kTileCols - 1) / kTileCols;
+  const int n0 = (int)(blockIdx.x % tiles_n) * kTileCols;
+  const int64_t m0 = (int64_t)(blockIdx.x / tiles_n) * kTileRows;
+  {
+    const int c = threadIdx.x & 63, from = threadIdx.x >> 6;
+    uint32_t t = 0;
+    if (n0 + c < a.width)
+      for (int i = from; i < chunks; i += 4) t = max(t, tops[(int64_t)i * a.width + n0 + c]);
+    part[from][c] = t;
+    __syncthreads();
+    if (from == 0) {
+      t = max(max(part[0][c], part[1][c]), max(part[2][c], part[3][c]));
+      top[c] = t;
+      if (m0 == 0 && n0 + c < a.width) a.scale[n0 + c] = scale_of(t);
+    }
+    __syncthreads();
+  }
+  // four rows of a piece: a word of four bytes in each of the piece's columns
+  for (int i = threadIdx.x; i < kTileRows / 4 * (kTileCols / E); i += 256) {
+    const int piece = i % (kTileCols / E), quad = i / (kTileCols / E), c = n0 + piece * E;
+    float v[4][E];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int64_t m = m0 + quad * 4 + u;
+      unpack<T>(m < a.rows && c < a.width ? load_own(static_cast<const T*>(a.x) + m * a.ld_x, c, a.width) : u32x4{0, 0, 0, 0}, v[u]);
+    }
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+      const uint32_t t = top[piece * E + j];
+      const double by = up_of(t);
+      uint32_t w = 0;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) w |= (uint32_t)(to_eight(v[u][j], by, t) & 255) << 8 * u;
+      *reinterpret_cast<uint32_t*>(tile + (piece * E + j) * STRIDE + quad * 4) = w;
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < kTileCols * (kTileRows / 16); i += 256) {
+    const int c = i / (kTileRows / 16), at = i % (kTileRows / 16) * 16;
+    if (n0 + c >= a.width || m0 + at >= a.rows) continue;
+    int8_t* to = a.q + (int64_t)(n0 + c) * a.ld_q + m0 + at;
+    const int8_t* from = tile + c * STRIDE + at;
+    if (m0 + at + 16 <= a.rows) {
+      *reinterpret_cast<u32x4_any*>(to) = *reinterpret_cast<const u32x4*>(from);
+    } else {
+      for (int j = 0; j < a.rows - m0 - at; ++j) to[j] = from[j];
+    }
+  }
+}
+
+inline int column_chunks(int64_t rows, int64_t width) {
+  const int64_t cols = (width + 255) / 256, want = (1024 + cols - 1) / cols, most = rows <= 32 ? 1 : (rows + 31) / 32;
+  return (int)(want < most ? want : most);
+}
+inline size_t columns_bytes(const ColumnsArgs& a) { return (size_t)column_chunks(a.rows, a.width) * a.width * sizeof(uint32_t); }
+
+template <class T>
+hipError_t columns(const ColumnsArgs& a, void* ws, hipStream_t s) {
+  int chunks = column_chunks(a.rows, a.width);
+  const int rows_per = (a.rows + chunks - 1) / chunks > 0 ? (a.rows + chunks - 1) / chunks : 1;
+  uint32_t* tops = static_cast<uint32_t*>(ws);
+  hipError_t e = launch(column_tops_kernel<T>, (int64_t)chunks * ((a.width + 255) / 256), 256, s, a, tops, rows_per);
+  if (e != hipSuccess) return e;
+  const int64_t down = a.rows ? (a.rows + kTileRows - 1) / kTileRows : 1;           // (no rows: the scales)
+  return launch(columns_kernel<T>, down * ((a.width + kTileCols - 1) / kTileCols), 256, s, a, (const uint32_t*)tops, chunks);
+}
+
+}  // namespace norm
+}  // namespace stgn

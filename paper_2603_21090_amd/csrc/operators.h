@@ -36,6 +36,53 @@ struct LinearGradArgs {
   int rows, d_in, d_out, act;
 };
 
+// the norm of rows (with gain), rows in 8 bits (without), both
+struct NormArgs {
+  const void *x, *residual, *gain;
+  void *h, *y;                                                // null: not wanted
+  int8_t* q;
+  float* scale;                                               // [rows]
+  int64_t ld_x, ld_res, ld_h, ld_y, ld_q;
+  int rows, width;
+  double eps;
+};
+
+struct NormGradArgs {
+  const void *dy, *h, *gain, *dh;
+  void *dx, *dgain;                                           // null: not wanted
+  int64_t ld_dy, ld_h, ld_dh, ld_dx;
+  int rows, width;
+  double eps;
+};
+
+// columns in 8 bits: x [rows x width], q [width x rows]
+struct ColumnsArgs {
+  const void* x;
+  int8_t* q;
+  float* scale;                                               // [width]
+  int64_t ld_x, ld_q;
+  int rows, width;
+};
+
+struct DropoutArgs {
+  const void *x, *residual;
+  void* y;
+  const uint64_t* rng;                                        // seed, step
+  int64_t ld_x, ld_res, ld_y;
+  int rows, width;
+  uint32_t border, site;                                      // numbers of 16 bits below the border are dropped
+  float scale;                                                // of what is kept
+};
+
+struct Linear8Args {
+  const int8_t *x, *w;                                        // [rows x d_in], [d_out x d_in]
+  const float *x_scale, *w_scale;
+  const void *bias, *residual;
+  void* y;
+  int64_t ld_x, ld_w, ld_res, ld_y;
+  int rows, d_in, d_out, act;
+};
+
 size_t linear_bytes(const LinearArgs& a, int dtype);
 hipError_t launch_linear(const LinearArgs& a, int dtype, void* ws, hipStream_t s);
 

@@ -3,6 +3,7 @@
 #include <utility>
 
 #include "attention_rows.h"
+#include "linear_i8.h"
 #include "operators.h"
 #include "streamtgn.h"
 
@@ -18,7 +19,15 @@ namespace stgn {
   size_t linear_bytes_##T(const LinearArgs& a);                                           \
   size_t linear_grad_bytes_##T(const LinearGradArgs& a);                                  \
   hipError_t linear_##T(const LinearArgs& a, void* ws, hipStream_t s);                    \
-  hipError_t linear_grad_##T(const LinearGradArgs& a, void* ws, hipStream_t s);
+  hipError_t linear_grad_##T(const LinearGradArgs& a, void* ws, hipStream_t s);           \
+  hipError_t rms_norm_##T(const NormArgs& a, hipStream_t s);                              \
+  size_t rms_norm_grad_bytes_##T(const NormGradArgs& a);                                  \
+  hipError_t rms_norm_grad_##T(const NormGradArgs& a, void* ws, hipStream_t s);           \
+  hipError_t rows_in_8_##T(const NormArgs& a, hipStream_t s);                             \
+  size_t columns_bytes_##T(const ColumnsArgs& a);                                         \
+  hipError_t columns_in_8_##T(const ColumnsArgs& a, void* ws, hipStream_t s);             \
+  hipError_t linear_i8_##T(const Linear8Args& a, void* ws, hipStream_t s);                \
+  hipError_t dropout_##T(const DropoutArgs& a, hipStream_t s);
 STGN_PER_TYPE(f32)
 STGN_PER_TYPE(bf16)
 STGN_PER_TYPE(f16)
@@ -260,6 +269,171 @@ AttnArgs attention_args(const stgn_attention_args* a) {
   return t;
 }
 
+// Matrices [rows x width] that a call reads or writes: one that it writes may be exactly one that it reads, or lie beside it in one wider matrix
+struct Matrix { const void* p; uint64_t ld; };
+bool apart_or_same(const Matrix& out, const Matrix& other, bool same_allowed, uint64_t rows, uint64_t width, size_t es) {
+  if (!out.p || !other.p) return true;
+  if (same_allowed && out.p == other.p && out.ld == other.ld) return true;
+  const Span s = span_of(out.p, rows, width, out.ld, es), t = span_of(other.p, rows, width, other.ld, es);
+  return !meet(s, t) || (out.ld == other.ld && beside(s, width * es, t, width * es, out.ld * es));
+}
+const char* const kFar = "a matrix reaches over more than 2^48 bytes";
+// why a matrix's rows are refused, or NULL
+const char* bad_matrix(const Matrix& m, uint64_t rows, uint64_t width, size_t es) {
+  if (!m.p) return nullptr;
+  if (!aligned(m.p, es)) return "a pointer is not aligned to its element";
+  if (m.ld < width || m.ld > kMaxLd) return "rows lie closer together than their width, or too far apart";
+  return too_far(rows, m.ld, 1, 0, 1, 0, width, es) ? kFar : nullptr;
+}
+
+int check_rms_norm(const stgn_rms_norm_args* a, bool grad, bool sizes_only) {
+  if (!a) return no("NULL arguments");
+  if (a->dtype > STGN_F16) return no("dtype must be STGN_F32, STGN_BF16 or STGN_F16");
+  if (a->reserved) return no("reserved must be 0");
+  if (a->rows > kMaxRows) return no("rows out of range");
+  if (a->width == 0 || a->width > kMaxWidth) return no("width must lie in 1 .. 2^24");
+  if (sizes_only) return STGN_OK;
+  if (!(a->eps >= 0.0) || a->eps - a->eps != 0.0) return no("eps must be finite and not negative");
+  const size_t es = size_of(a->dtype);
+  const uint64_t rows = a->rows, width = a->width;
+  if (!a->gain) return no("NULL gain");
+  if (!aligned(a->gain, es) || !aligned(a->dgain, es) || !aligned(a->dx, es)) return no("a pointer is not aligned to its element");
+  const Span gain = span_of(a->gain, 1, width, 0, es);
+  if (!grad) {
+    if (rows && !a->x) return no("NULL x");
+    if (rows && !a->y && !a->q) return no("NULL y and q");
+    if (rows && a->q && !a->scale) return no("q needs scale");
+    const Matrix x{a->x, a->ld_x}, res{a->residual, a->ld_residual}, h{a->h, a->ld_h}, y{a->y, a->ld_y}, q{a->q, a->ld_q};
+    for (const Matrix& m : {x, res, h, y})
+      if (const char* why = bad_matrix(m, rows, width, es)) return no(why);
+    if (const char* why = bad_matrix(q, rows, width, 1)) return no(why);
+    if (a->q && !aligned(a->scale, 4)) return no("a pointer is not aligned to its element");
+    for (const Matrix& out : {h, y})
+      for (const Matrix& in : {x, res})
+        if (!apart_or_same(out, in, true, rows, width, es)) return no("h and y may each be exactly x or the residual, or overlap neither");
+    if (!apart_or_same(h, y, false, rows, width, es)) return no("two outputs overlap");
+    const Span sq = span_of(a->q, rows, width, a->ld_q, 1), sc = span_of(a->q ? a->scale : nullptr, 1, rows, 0, 4);
+    for (const Matrix& m : {x, res, h, y}) {
+      const Span t = span_of(m.p, rows, width, m.ld, es);
+      if (meet(sq, t) || meet(sc, t)) return no("q or scale overlaps another tensor");
+    }
+    for (const Matrix& m : {h, y})
+      if (meet(gain, span_of(m.p, rows, width, m.ld, es))) return no("an output overlaps the gain");
+    if (meet(sq, gain) || meet(sc, gain) || meet(sq, sc)) return no("q or scale overlaps another tensor");
+    return STGN_OK;
+  }
+  if (rows && (!a->h || !a->dy)) return no("NULL h or dy");
+  const Matrix in[] = {{a->h, a->ld_h}, {a->dy, a->ld_dy}, {a->dh, a->ld_dh}};
+  for (const Matrix& m : in)
+    if (const char* why = bad_matrix(m, rows, width, es)) return no(why);
+  if (a->dx && too_far(rows, width, 1, 0, 1, 0, width, es)) return no(kFar);
+  const Span dx = span_of(a->dx, rows, width, width, es), dg = span_of(a->dgain, 1, width, 0, es);
+  for (const Matrix& m : in) {
+    const Span t = span_of(m.p, rows, width, m.ld, es);
+    if (meet(dx, t) || meet(dg, t)) return no("a gradient overlaps an input");
+  }
+  if (meet(dx, gain) || meet(dg, gain)) return no("a gradient overlaps an input");
+  if (meet(dx, dg)) return no("two gradients overlap");
+  return STGN_OK;
+}
+
+NormArgs norm_args(const stgn_rms_norm_args* a) {
+  NormArgs n{};
+  n.x = a->x; n.residual = a->residual; n.gain = a->gain; n.h = a->h; n.y = a->y; n.q = a->q; n.scale = a->scale;
+  n.ld_x = (int64_t)a->ld_x; n.ld_res = (int64_t)a->ld_residual; n.ld_h = (int64_t)a->ld_h; n.ld_y = (int64_t)a->ld_y; n.ld_q = (int64_t)a->ld_q;
+  n.rows = (int)a->rows; n.width = (int)a->width; n.eps = a->eps;
+  return n;
+}
+
+NormGradArgs norm_grad_args(const stgn_rms_norm_args* a) {
+  NormGradArgs n{};
+  n.dy = a->dy; n.h = a->h; n.gain = a->gain; n.dh = a->dh; n.dx = a->dx; n.dgain = a->dgain;
+  n.ld_dy = (int64_t)a->ld_dy; n.ld_h = (int64_t)a->ld_h; n.ld_dh = (int64_t)a->ld_dh; n.ld_dx = (int64_t)a->width;
+  n.rows = (int)a->rows; n.width = (int)a->width; n.eps = a->eps;
+  return n;
+}
+
+int check_quantize(const stgn_quantize_args* a, bool sizes_only) {
+  if (!a) return no("NULL arguments");
+  if (a->dtype > STGN_F16) return no("dtype must be STGN_F32, STGN_BF16 or STGN_F16");
+  if (a->columns > 1) return no("columns must be 0 or 1");
+  if (a->rows > kMaxRows) return no("rows out of range");
+  if (a->width == 0 || a->width > kMaxWidth) return no("width must lie in 1 .. 2^24");
+  if (a->columns && (((uint64_t)a->rows + 127) / 128) * (((uint64_t)a->width + 63) / 64) > kMaxGroups) return no("the matrix has more tiles than a launch");
+  if (sizes_only) return STGN_OK;
+  const size_t es = size_of(a->dtype);
+  const uint64_t q_rows = a->columns ? a->width : a->rows, q_width = a->columns ? a->rows : a->width;
+  if ((a->rows && (!a->x || !a->q)) || (q_rows && !a->scale)) return no("NULL x, q or scale");
+  if (const char* why = bad_matrix({a->x, a->ld_x}, a->rows, a->width, es)) return no(why);
+  if (const char* why = bad_matrix({a->q, a->ld_q}, q_rows, q_width, 1)) return no(why);
+  if (!aligned(a->scale, 4)) return no("a pointer is not aligned to its element");
+  const Span x = span_of(a->x, a->rows, a->width, a->ld_x, es), q = span_of(a->q, q_rows, q_width, a->ld_q, 1), sc = span_of(a->scale, 1, q_rows, 0, 4);
+  if (meet(x, q) || meet(x, sc) || meet(q, sc)) return no("an output overlaps the input or the other output");
+  return STGN_OK;
+}
+
+ColumnsArgs columns_args(const stgn_quantize_args* a) {
+  ColumnsArgs c{};
+  c.x = a->x; c.q = a->q; c.scale = a->scale; c.ld_x = (int64_t)a->ld_x; c.ld_q = (int64_t)a->ld_q;
+  c.rows = (int)a->rows; c.width = (int)a->width;
+  return c;
+}
+
+int check_linear_i8(const stgn_linear_i8_args* a, bool sizes_only) {
+  if (!a) return no("NULL arguments");
+  if (a->dtype > STGN_F16) return no("dtype must be STGN_F32, STGN_BF16 or STGN_F16");
+  if (a->activation > STGN_ACT_SILU) return no("unknown activation");
+  if (a->reserved) return no("reserved must be 0");
+  if (a->rows > kMaxRows) return no("rows out of range");
+  if (a->d_in == 0 || a->d_in > 131071) return no("d_in must lie in 1 .. 131071");
+  if (a->d_out == 0 || a->d_out > kMaxWidth) return no("d_out must lie in 1 .. 2^24");
+  if ((((uint64_t)a->rows + 63) / 64) * (((uint64_t)a->d_out + 63) / 64) > kMaxGroups - 1024) return no("the product has more tiles than a launch");
+  if (sizes_only) return STGN_OK;
+  const size_t es = size_of(a->dtype);
+  const uint64_t rows = a->rows, n = a->d_out;
+  if (!a->w || !a->w_scale || (rows && (!a->x || !a->x_scale || !a->y))) return no("NULL x, w, a scale or y");
+  if (!aligned(a->x_scale, 4) || !aligned(a->w_scale, 4) || !aligned(a->bias, es)) return no("a pointer is not aligned to its element");
+  const Matrix x{a->x, a->ld_x}, w{a->w, a->ld_w}, y{a->y, a->ld_y}, res{a->residual, a->ld_residual};
+  if (const char* why = bad_matrix(x, rows, a->d_in, 1)) return no(why);
+  if (const char* why = bad_matrix(w, n, a->d_in, 1)) return no(why);
+  for (const Matrix& m : {y, res})
+    if (const char* why = bad_matrix(m, rows, n, es)) return no(why);
+  if (!apart_or_same(y, res, true, rows, n, es)) return no("y overlaps the residual (it may be exactly the residual)");
+  const Span out = span_of(a->y, rows, n, a->ld_y, es);
+  for (const Span& t : {span_of(a->x, rows, a->d_in, a->ld_x, 1), span_of(a->w, n, a->d_in, a->ld_w, 1), span_of(a->x_scale, 1, rows, 0, 4),
+                        span_of(a->w_scale, 1, n, 0, 4), span_of(a->bias, 1, n, 0, es)})
+    if (meet(out, t)) return no("y overlaps an input");
+  return STGN_OK;
+}
+
+Linear8Args linear_i8_args(const stgn_linear_i8_args* a) {
+  Linear8Args l{};
+  l.x = a->x; l.w = a->w; l.x_scale = a->x_scale; l.w_scale = a->w_scale; l.bias = a->bias; l.residual = a->residual; l.y = a->y;
+  l.ld_x = (int64_t)a->ld_x; l.ld_w = (int64_t)a->ld_w; l.ld_res = (int64_t)a->ld_residual; l.ld_y = (int64_t)a->ld_y;
+  l.rows = (int)a->rows; l.d_in = (int)a->d_in; l.d_out = (int)a->d_out; l.act = (int)a->activation;
+  return l;
+}
+
+int check_dropout(const stgn_dropout_args* a) {
+  if (!a) return no("NULL arguments");
+  if (a->dtype > STGN_F16) return no("dtype must be STGN_F32, STGN_BF16 or STGN_F16");
+  if (a->rows > kMaxRows) return no("rows out of range");
+  if (a->width == 0 || a->width > kMaxWidth) return no("width must lie in 1 .. 2^24");
+  if (a->site > 65535) return no("site must lie in 0 .. 65535");
+  if (!(a->p >= 0.0 && a->p <= 1.0)) return no("p must lie in 0 .. 1");
+  const size_t es = size_of(a->dtype);
+  const uint64_t rows = a->rows, width = a->width;
+  if ((rows && (!a->x || !a->y)) || !a->rng) return no("NULL x, y or rng");
+  if (!aligned(a->rng, 8)) return no("a pointer is not aligned to its element");
+  const Matrix x{a->x, a->ld_x}, res{a->residual, a->ld_residual}, y{a->y, a->ld_y};
+  for (const Matrix& m : {x, res, y})
+    if (const char* why = bad_matrix(m, rows, width, es)) return no(why);
+  for (const Matrix& in : {x, res})
+    if (!apart_or_same(y, in, true, rows, width, es)) return no("y may be exactly x or the residual, or overlap neither");
+  if (meet(span_of(a->y, rows, width, a->ld_y, es), span_of(a->rng, 1, 2, 0, 8))) return no("y overlaps rng");
+  return STGN_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -312,6 +486,74 @@ int stgn_attention_grad(const stgn_attention_args* args, void* device_workspace,
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   if (few_rows(a, (int)args->dtype, true)) return finish(STGN_BY_TYPE(args->dtype, attention_rows_grad, a, device_workspace, s));
   return finish(STGN_BY_TYPE(args->dtype, attention_grad, a, device_workspace, s));
+}
+
+int stgn_rms_norm_workspace(const stgn_rms_norm_args* args, size_t* forward_bytes, size_t* grad_bytes) {
+  if (const int rc = check_rms_norm(args, false, true)) return rc;
+  if (forward_bytes) *forward_bytes = 0;
+  if (grad_bytes) *grad_bytes = STGN_BY_TYPE(args->dtype, rms_norm_grad_bytes, norm_grad_args(args));
+  return STGN_OK;
+}
+
+int stgn_rms_norm(const stgn_rms_norm_args* args, void*, size_t, void* hip_stream) {
+  if (const int rc = check_rms_norm(args, false, false)) return rc;
+  if (args->rows == 0) return STGN_OK;
+  return finish(STGN_BY_TYPE(args->dtype, rms_norm, norm_args(args), static_cast<hipStream_t>(hip_stream)));
+}
+
+int stgn_rms_norm_grad(const stgn_rms_norm_args* args, void* device_workspace, size_t device_bytes, void* hip_stream) {
+  if (const int rc = check_rms_norm(args, true, false)) return rc;
+  const NormGradArgs a = norm_grad_args(args);
+  if (const int rc = check_workspace(STGN_BY_TYPE(args->dtype, rms_norm_grad_bytes, a), device_workspace, device_bytes)) return rc;
+  if (!a.dx && !a.dgain) return STGN_OK;
+  return finish(STGN_BY_TYPE(args->dtype, rms_norm_grad, a, device_workspace, static_cast<hipStream_t>(hip_stream)));
+}
+
+int stgn_quantize_workspace(const stgn_quantize_args* args, size_t* bytes) {
+  if (const int rc = check_quantize(args, true)) return rc;
+  if (bytes) *bytes = args->columns ? STGN_BY_TYPE(args->dtype, columns_bytes, columns_args(args)) : 0;
+  return STGN_OK;
+}
+
+int stgn_quantize(const stgn_quantize_args* args, void* device_workspace, size_t device_bytes, void* hip_stream) {
+  if (const int rc = check_quantize(args, false)) return rc;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  if (args->columns) {
+    const ColumnsArgs a = columns_args(args);
+    if (const int rc = check_workspace(STGN_BY_TYPE(args->dtype, columns_bytes, a), device_workspace, device_bytes)) return rc;
+    return finish(STGN_BY_TYPE(args->dtype, columns_in_8, a, device_workspace, s));
+  }
+  if (args->rows == 0) return STGN_OK;
+  NormArgs a{};
+  a.x = args->x; a.q = args->q; a.scale = args->scale; a.ld_x = (int64_t)args->ld_x; a.ld_q = (int64_t)args->ld_q;
+  a.rows = (int)args->rows; a.width = (int)args->width;
+  return finish(STGN_BY_TYPE(args->dtype, rows_in_8, a, s));
+}
+
+int stgn_linear_i8_workspace(const stgn_linear_i8_args* args, size_t* bytes) {
+  if (const int rc = check_linear_i8(args, true)) return rc;
+  if (bytes) *bytes = dense8::part_bytes(linear_i8_args(args));
+  return STGN_OK;
+}
+
+int stgn_linear_i8(const stgn_linear_i8_args* args, void* device_workspace, size_t device_bytes, void* hip_stream) {
+  if (const int rc = check_linear_i8(args, false)) return rc;
+  const Linear8Args a = linear_i8_args(args);
+  if (const int rc = check_workspace(dense8::part_bytes(a), device_workspace, device_bytes)) return rc;
+  if (a.rows == 0) return STGN_OK;
+  return finish(STGN_BY_TYPE(args->dtype, linear_i8, a, device_workspace, static_cast<hipStream_t>(hip_stream)));
+}
+
+int stgn_dropout(const stgn_dropout_args* args, void* hip_stream) {
+  if (const int rc = check_dropout(args)) return rc;
+  if (args->rows == 0) return STGN_OK;
+  DropoutArgs a{};
+  a.x = args->x; a.residual = args->residual; a.y = args->y; a.rng = args->rng;
+  a.ld_x = (int64_t)args->ld_x; a.ld_res = (int64_t)args->ld_residual; a.ld_y = (int64_t)args->ld_y;
+  a.rows = (int)args->rows; a.width = (int)args->width; a.site = args->site;
+  a.border = (uint32_t)nearbyint(args->p * 65536.0);
+  a.scale = a.border < 65536u ? (float)(65536.0 / (65536.0 - a.border)) : 0.f;
+  return finish(STGN_BY_TYPE(args->dtype, dropout, a, static_cast<hipStream_t>(hip_stream)));
 }
 
 }  // extern "C"

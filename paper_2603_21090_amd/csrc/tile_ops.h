@@ -25,9 +25,10 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 // rows of odd widths start anywhere: global memory takes wide accesses at any element's address
-typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(1)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
 typedef uint32_t u32_any __attribute__((aligned(2), may_alias));
 
 template <class T> struct Elem;
@@ -58,6 +59,14 @@ template <> struct Elem<_Float16> {
   static constexpr int E = 8, KF = 32, PB = 2;
   static __device__ inline floatx4 mma(const Frag& a, const Frag& b, floatx4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+  }
+};
+
+template <> struct Elem<int8_t> {                             // sums of 32-bit integers
+  using Frag = i32x4;
+  static constexpr int E = 16, KF = 64;
+  static __device__ inline i32x4 mma(const Frag& a, const Frag& b, i32x4 c) {
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
   }
 };
 
@@ -157,9 +166,12 @@ template <class T>
 __device__ inline u32x4 moved_down(u32x4 v, int bytes) {
   v = bytes & 8 ? u32x4{v[2], v[3], 0u, 0u} : v;
   v = bytes & 4 ? u32x4{v[1], v[2], v[3], 0u} : v;
-  if constexpr (sizeof(T) == 2)
+  if constexpr (sizeof(T) <= 2)
     v = bytes & 2 ? u32x4{__builtin_amdgcn_alignbyte(v[1], v[0], 2), __builtin_amdgcn_alignbyte(v[2], v[1], 2),
                           __builtin_amdgcn_alignbyte(v[3], v[2], 2), v[3] >> 16} : v;
+  if constexpr (sizeof(T) == 1)
+    v = bytes & 1 ? u32x4{__builtin_amdgcn_alignbyte(v[1], v[0], 1), __builtin_amdgcn_alignbyte(v[2], v[1], 1),
+                          __builtin_amdgcn_alignbyte(v[3], v[2], 1), v[3] >> 8} : v;
   return v;
 }
 
