@@ -395,7 +395,7 @@ int stgn_rms_norm_workspace(const stgn_rms_norm_args *args, size_t *forward_byte
 int stgn_rms_norm(const stgn_rms_norm_args *args, void *device_workspace, size_t device_bytes, void *hip_stream);
 int stgn_rms_norm_grad(const stgn_rms_norm_args *args, void *device_workspace, size_t device_bytes, void *hip_stream);
 
-/* A matrix in 8 bits, the operands of stgn_linear_i8.  columns = 0: a scale for each row, q: [rows x width] (activations).  columns = 1: a scale for
+/* A matrix in 8 bits, the operands of stgn_linear_quantized.  columns = 0: a scale for each row, q: [rows x width] (activations).  columns = 1: a scale for
  * each column and q turned over, [width x rows] (a weight [d_in x d_out] becomes [d_out x d_in]).  Scales and numbers as in stgn_rms_norm, from x itself.
  * x: [rows x width], ld_x elements apart; q's rows lie ld_q bytes apart; scale: fp32 [rows or width].  rows may be 0 (scales of columns are then 0), width lies
  * in 1 .. 2^24.  Outputs overlap nothing. */
@@ -425,10 +425,10 @@ typedef struct {
   const float *x_scale, *w_scale;
   const void *bias, *residual;
   void *y;
-} stgn_linear_i8_args;
+} stgn_linear_quantized_args;
 
-int stgn_linear_i8_workspace(const stgn_linear_i8_args *args, size_t *bytes);
-int stgn_linear_i8(const stgn_linear_i8_args *args, void *device_workspace, size_t device_bytes, void *hip_stream);
+int stgn_linear_quantized_workspace(const stgn_linear_quantized_args *args, size_t *bytes);
+int stgn_linear_quantized(const stgn_linear_quantized_args *args, void *device_workspace, size_t device_bytes, void *hip_stream);
 
 /* Dropout with the residual's addition: y = residual + (kept ? x / (1 - p) : 0).  The mask is stored nowhere: number j of row i is kept where the 16 bits that Philox
  * 4x32-10 gives for it are not below border = round(65536 p), p in effect being border / 65536.  Key: rng[0] (seed); counter words: group, group >> 32 | site << 16,

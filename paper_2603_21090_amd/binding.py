@@ -107,7 +107,7 @@ EXPORTS = ("stgn_query_workspace", "stgn_create", "stgn_destroy", "stgn_ingest_b
            "stgn_maintain", "stgn_probe_gather", "stgn_linear_workspace", "stgn_linear", "stgn_linear_grad",
            "stgn_attention_workspace", "stgn_attention", "stgn_attention_grad", "stgn_predictor_mlp_workspace",
            "stgn_set_predictor_mlp", "stgn_rms_norm_workspace", "stgn_rms_norm", "stgn_rms_norm_grad", "stgn_quantize_workspace", "stgn_quantize",
-           "stgn_linear_i8_workspace", "stgn_linear_i8", "stgn_dropout")
+           "stgn_linear_quantized_workspace", "stgn_linear_quantized", "stgn_dropout")
 
 
 def load_library():
@@ -147,7 +147,7 @@ def load_library():
         getattr(L, f"stgn_{op}_workspace").argtypes = [vp, vp, vp]
         for name in (f"stgn_{op}", f"stgn_{op}_grad"):
             getattr(L, name).argtypes = [vp, vp, C.c_size_t, vp]
-    for op in ("quantize", "linear_i8"):
+    for op in ("quantize", "linear_quantized"):
         getattr(L, f"stgn_{op}_workspace").argtypes = [vp, vp]
         getattr(L, f"stgn_{op}").argtypes = [vp, vp, C.c_size_t, vp]
     L.stgn_dropout.argtypes = [vp, vp]
@@ -422,7 +422,7 @@ def quantize(x, columns=False):
 
 
 def linear_i8(x, x_scale, w, w_scale, bias=None, activation="none", residual=None, dtype=None):
-    """y = act(x_scale w_scale sum x w + bias) + residual from operands in 8 bits (stgn_linear_i8): x int8 [rows, d_in], x_scale float32 [rows], w int8 [d_out,
+    """y = act(x_scale w_scale sum x w + bias) + residual from operands in 8 bits (stgn_linear_quantized): x int8 [rows, d_in], x_scale float32 [rows], w int8 [d_out,
     d_in], w_scale float32 [d_out], as rms_norm_i8 and quantize give them; bias [d_out] and residual [rows, d_out] of y's type, which is `dtype`,
     else theirs, else bfloat16.  activation: as in linear."""
     import torch
@@ -446,7 +446,7 @@ def linear_i8(x, x_scale, w, w_scale, bias=None, activation="none", residual=Non
     rp = _expect("residual", residual, y, y.shape) if residual is not None else 0
     args = _PACK_LINEAR_I8.pack(_dtype_code(y), ACTIVATIONS[activation], rows, d_in, d_out, 0, _ld(x), _ld(w), _ld(residual) if rp else 0, d_out,
                                 xp, wp, sp, tp, bp, rp, y.data_ptr())
-    _run_operator(L.stgn_linear_i8_workspace, L.stgn_linear_i8, args, None, x.device)
+    _run_operator(L.stgn_linear_quantized_workspace, L.stgn_linear_quantized, args, None, x.device)
     return y
 
 

@@ -379,7 +379,7 @@ ColumnsArgs columns_args(const stgn_quantize_args* a) {
   return c;
 }
 
-int check_linear_i8(const stgn_linear_i8_args* a, bool sizes_only) {
+int check_linear_i8(const stgn_linear_quantized_args* a, bool sizes_only) {
   if (!a) return no("NULL arguments");
   if (a->dtype > STGN_F16) return no("dtype must be STGN_F32, STGN_BF16 or STGN_F16");
   if (a->activation > STGN_ACT_SILU) return no("unknown activation");
@@ -406,7 +406,7 @@ int check_linear_i8(const stgn_linear_i8_args* a, bool sizes_only) {
   return STGN_OK;
 }
 
-Linear8Args linear_i8_args(const stgn_linear_i8_args* a) {
+Linear8Args linear_i8_args(const stgn_linear_quantized_args* a) {
   Linear8Args l{};
   l.x = a->x; l.w = a->w; l.x_scale = a->x_scale; l.w_scale = a->w_scale; l.bias = a->bias; l.residual = a->residual; l.y = a->y;
   l.ld_x = (int64_t)a->ld_x; l.ld_w = (int64_t)a->ld_w; l.ld_res = (int64_t)a->ld_residual; l.ld_y = (int64_t)a->ld_y;
@@ -530,13 +530,13 @@ int stgn_quantize(const stgn_quantize_args* args, void* device_workspace, size_t
   return finish(STGN_BY_TYPE(args->dtype, rows_in_8, a, s));
 }
 
-int stgn_linear_i8_workspace(const stgn_linear_i8_args* args, size_t* bytes) {
+int stgn_linear_quantized_workspace(const stgn_linear_quantized_args* args, size_t* bytes) {
   if (const int rc = check_linear_i8(args, true)) return rc;
   if (bytes) *bytes = dense8::part_bytes(linear_i8_args(args));
   return STGN_OK;
 }
 
-int stgn_linear_i8(const stgn_linear_i8_args* args, void* device_workspace, size_t device_bytes, void* hip_stream) {
+int stgn_linear_quantized(const stgn_linear_quantized_args* args, void* device_workspace, size_t device_bytes, void* hip_stream) {
   if (const int rc = check_linear_i8(args, false)) return rc;
   const Linear8Args a = linear_i8_args(args);
   if (const int rc = check_workspace(dense8::part_bytes(a), device_workspace, device_bytes)) return rc;

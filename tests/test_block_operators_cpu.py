@@ -85,7 +85,7 @@ def test_quantize_refuses(lib, bad):
                                  dict(x_scale=(3 << 20) + 2), dict(w_scale=(4 << 20) + 1), dict(y=1 << 20), dict(y=2 << 20), dict(y=3 << 20), dict(y=4 << 20),
                                  dict(y=5 << 20), dict(y=(6 << 20) + 2), dict(y=6 << 20, ld_y=33), dict(rows=1 << 24, ld_x=FAR), dict(rows=1 << 24, ld_y=FAR)], ids=str)
 def test_linear_i8_refuses(lib, bad):
-    assert lib.stgn_linear_i8(C.byref(product_args(**bad)), None, 0, None) == INVALID
+    assert lib.stgn_linear_quantized(C.byref(product_args(**bad)), None, 0, None) == INVALID
     assert lib.stgn_last_error(None)
 
 
@@ -101,10 +101,10 @@ def test_dropout_refuses(lib, bad):
 def test_null_arguments_and_workspaces(lib):
     n, m = C.c_size_t(0), C.c_size_t(1)
     assert lib.stgn_dropout(None, None) == INVALID
-    for op in ("rms_norm", "rms_norm_grad", "quantize", "linear_i8"):
+    for op in ("rms_norm", "rms_norm_grad", "quantize", "linear_quantized"):
         assert getattr(lib, f"stgn_{op}")(None, None, 0, None) == INVALID
     assert lib.stgn_rms_norm_workspace(None, C.byref(n), C.byref(n)) == INVALID
-    assert lib.stgn_quantize_workspace(None, C.byref(n)) == INVALID and lib.stgn_linear_i8_workspace(None, C.byref(n)) == INVALID
+    assert lib.stgn_quantize_workspace(None, C.byref(n)) == INVALID and lib.stgn_linear_quantized_workspace(None, C.byref(n)) == INVALID
     args = norm_args()
     assert lib.stgn_rms_norm_workspace(C.byref(args), None, None) == 0
     assert lib.stgn_rms_norm_workspace(C.byref(args), C.byref(m), C.byref(n)) == 0 and n.value > 0 and m.value == 0

@@ -85,9 +85,9 @@ def test_y_in_the_residuals_place(size, dt):
     a = binding.LinearI8Args(dtype=TYPES.index(dt), activation=1, rows=rows, d_in=d_in, d_out=d_out, ld_x=d_in, ld_w=d_in, ld_residual=d_out + 4, ld_y=d_out + 4,
                              x=X.data_ptr(), w=W.data_ptr(), x_scale=XS.data_ptr(), w_scale=WS.data_ptr(), bias=B.data_ptr(), residual=p, y=p)
     lib, n = binding.load_library(), C.c_size_t(0)
-    assert lib.stgn_linear_i8_workspace(C.byref(a), C.byref(n)) == 0
+    assert lib.stgn_linear_quantized_workspace(C.byref(a), C.byref(n)) == 0
     space = torch.empty(n.value, dtype=torch.uint8, device="cuda")
-    assert lib.stgn_linear_i8(C.byref(a), space.data_ptr() if n.value else None, n.value, torch.cuda.current_stream().cuda_stream) == 0, lib.stgn_last_error(None)
+    assert lib.stgn_linear_quantized(C.byref(a), space.data_ptr() if n.value else None, n.value, torch.cuda.current_stream().cuda_stream) == 0, lib.stgn_last_error(None)
     within(m[:, 1:1 + d_out], refs.linear_i8(x, xs, w, ws, b, "relu", r, dt), "y")
     for c in (0, d_out + 1, d_out + 2, d_out + 3):
         assert (m[:, c] == 7).all()
