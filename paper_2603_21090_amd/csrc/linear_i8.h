@@ -337,9 +337,9 @@ struct DirectMove {
   }
 };
 
-// eight neighbouring outputs of row m
+// Eight neighbouring outputs of row m; `residual`: theirs, where all eight are there and the type has 16 bits
 template <class T>
-__device__ inline void finish8(const Product& a, int64_t m, int n, float rs, const i32x4& s, const i32x4& t) {
+__device__ inline void finish8(const Product& a, int64_t m, int n, float rs, const i32x4& s, const i32x4& t, const u32x4& residual) {
   const bool both = n + 4 < a.n;
   floatx4 u = scaled(s, rs, load4(a.l_scale, n, a.n)), v = {0.f, 0.f, 0.f, 0.f};
   if (both) v = scaled(t, rs, load4(a.l_scale, n + 4, a.n));
@@ -354,7 +354,17 @@ __device__ inline void finish8(const Product& a, int64_t m, int n, float rs, con
   if (a.bias) add(static_cast<const T*>(a.bias));
   activate<T>(a.act, u);
   activate<T>(a.act, v);
-  if (a.residual) add(static_cast<const T*>(a.residual) + m * a.ld_res);
+  if (a.residual) {
+    if (sizeof(T) == 2 && n + 8 <= a.n) {
+      if constexpr (sizeof(T) == 2) {
+        const typename Elem<T>::Frag f = __builtin_bit_cast(typename Elem<T>::Frag, residual);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { u[j] += (float)f[j]; v[j] += (float)f[j + 4]; }
+      }
+    } else {
+      add(static_cast<const T*>(a.residual) + m * a.ld_res);
+    }
+  }
   T* out = static_cast<T*>(a.out) + m * a.ld_out;
   if constexpr (sizeof(T) == 2) {
     store8(out, n, a.n, u, v);
@@ -364,26 +374,38 @@ __device__ inline void finish8(const Product& a, int64_t m, int n, float rs, con
   }
 }
 
-// a wave's blocks from output (m0, n0), columns in pairs of blocks
+// A wave's blocks from output (m0, n0), columns in pairs of blocks.  The residual of sixteen rows is on its way while the sixteen rows before are finished.
 template <class T, int NB, int MB>
 __device__ __forceinline__ void finish_pairs(const Product& a, int split, int m0, int n0, i32x4 (&acc)[NB][MB]) {
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, first = n0 + 8 * (lane >> 4);
+  u32x4 ahead[2][NB / 2];
+  auto ask = [&](int y) {
+    const int64_t m = m0 + y * 16 + (lane & 15);
+#pragma unroll
+    for (int x = 0; x < NB / 2; ++x) {
+      ahead[y & 1][x] = u32x4{0, 0, 0, 0};
+      if (sizeof(T) == 2 && a.residual && a.splits == 1 && m < a.m && first + x * 32 + 8 <= a.n)
+        ahead[y & 1][x] = *reinterpret_cast<const u32x4_any*>(static_cast<const T*>(a.residual) + m * a.ld_res + first + x * 32);
+    }
+  };
+  ask(0);
 #pragma unroll
   for (int y = 0; y < MB; ++y) {
+    if (y + 1 < MB) ask(y + 1);
     __builtin_amdgcn_sched_barrier(0);
     const int64_t m = m0 + y * 16 + (lane & 15);
     if (m >= a.m) continue;
     const float rs = a.r_scale[m];
 #pragma unroll
     for (int x = 0; x < NB; x += 2) {
-      const int n = n0 + x * 16 + 8 * (lane >> 4);
+      const int n = first + x * 16;
       if (n >= a.n) continue;
       if (a.splits > 1) {
         int* row = a.part + (split * (int64_t)a.m + m) * a.n;
         store_sums(row, n, a.n, acc[x][y]);
         if (n + 4 < a.n) store_sums(row, n + 4, a.n, acc[x + 1][y]);
       } else {
-        finish8<T>(a, m, n, rs, acc[x][y], acc[x + 1][y]);
+        finish8<T>(a, m, n, rs, acc[x][y], acc[x + 1][y], ahead[y & 1][x / 2]);
       }
     }
   }
