@@ -3,8 +3,9 @@
 //   h = x + residual,  r = 1 / sqrt(mean h^2 + eps),  y = h r g;       scale = max |y| / 127,  q = y 127 / max |y| to the nearest whole number
 //   dx = r (g dy - h r mean(r g dy h)) + dh,                            dg = column sums of dy h r
 //
-// Bytes bound all of it: a row is read once and stays in its lanes' registers between its sums and its outputs.  LANES lanes hold a row in NP
-// pieces of 16 bytes each, as few lanes as hold it: 16 lanes (sixteen rows a workgroup) to 1,024 (one); longer rows are read again.
+// Bytes bound all of it: a row is read once and stays in its lanes' registers between its sums and its outputs.  LANES lanes hold a row, up to 16
+// numbers each, as few lanes as hold it: 16 lanes (sixteen rows a workgroup, whose sums take four steps within a wave) to 1,024 (one row); longer rows are
+// read again.
 // The sum of squares is a sum of 64 bits: r, and with it a number in 8 bits whose value lies next to a border, then does not hang on the
 // order of the sum, and no magnitude of 32 bits overflows it.
 #pragma once
@@ -81,13 +82,32 @@ __device__ inline float normed(float h, float r, float g) {
   return y;
 }
 
-// value of all LANES lanes that hold a row; `at`: LDS of its own for rows that lie in several waves
+// every lane's value from N lanes further on within its sixteen, round about
+template <int N, class V>
+__device__ inline V rotated(V v) {
+  if constexpr (sizeof(V) == 4) {
+    return __builtin_bit_cast(V, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x120 + N, 0xF, 0xF, true));
+  } else {
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    i32x2 w = __builtin_bit_cast(i32x2, v);
+    w[0] = __builtin_amdgcn_mov_dpp(w[0], 0x120 + N, 0xF, 0xF, true);
+    w[1] = __builtin_amdgcn_mov_dpp(w[1], 0x120 + N, 0xF, 0xF, true);
+    return __builtin_bit_cast(V, w);
+  }
+}
+// Value of all LANES lanes that hold a row, the same bits in each; `at`: LDS for rows that lie in several waves, which nobody else uses between one barrier of
+// the workgroup and the next
 template <int LANES, class V, class F>
 __device__ inline V across(V v, V* at, F f) {
-#pragma unroll
-  for (int d = (LANES < 64 ? LANES : 64) / 2; d > 0; d >>= 1) v = f(v, (V)__shfl_xor(v, d));
+  v = f(v, rotated<8>(v));
+  v = f(v, rotated<4>(v));
+  v = f(v, rotated<2>(v));
+  v = f(v, rotated<1>(v));
+  if constexpr (LANES >= 64) {
+    v = f(v, (V)__shfl_xor(v, 16));
+    v = f(v, (V)__shfl_xor(v, 32));
+  }
   if constexpr (LANES > 64) {
-    __syncthreads();
     if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = v;
     __syncthreads();
     v = at[0];
@@ -178,6 +198,7 @@ __global__ __launch_bounds__(block_of(LANES)) void rows_kernel(NormArgs a) {
         store_bytes<E>(a.q + row * a.ld_q, c, a.width, q);
       }
     }
+    if constexpr (LANES > 64) __syncthreads();                // (the sums' LDS, where the workgroup has another row)
   }
 }
 
@@ -241,25 +262,32 @@ __global__ __launch_bounds__(1024) void long_rows_kernel(NormArgs a) {
         store_bytes<E>(a.q + row * a.ld_q, c, a.width, q);
       }
     });
+    __syncthreads();
   }
 }
 
 constexpr int64_t kMostBlocks = 1 << 20;                      // of a launch; more rows go round again
 
-// f(lanes, pieces) for the fewest lanes that hold a row, or longer() where none do
-template <class T, class F, class L>
+// f(lanes, pieces) for the fewest lanes that hold a row, or longer() where none do.  16 numbers a lane keep four waves and more on a SIMD; twice that for
+// the widest rows only.  GRAD: 512 lanes at most there, whose registers hold what the gradient keeps of 32 numbers (1,024 lanes of 16, half the registers
+// each, spill: 4,096 x 16,384 in bf16 192 us, 118 so).
+template <class T, bool GRAD, class F, class L>
 hipError_t by_width(int width, F f, L longer) {
-  constexpr int E = kE<T>;
-#define STGN_HOLDS(lanes, pieces) \
-  if (width <= lanes * pieces * E) return f(std::integral_constant<int, lanes>(), std::integral_constant<int, pieces>());
-  STGN_HOLDS(16, 1)
-  STGN_HOLDS(64, 1)
-  STGN_HOLDS(64, 2)
-  STGN_HOLDS(64, 4)
-  STGN_HOLDS(256, 2)
-  STGN_HOLDS(256, 4)
-  STGN_HOLDS(1024, 2)
-  STGN_HOLDS(1024, 4)
+#define STGN_HOLDS(lanes, numbers) \
+  if (width <= lanes * numbers) return f(std::integral_constant<int, lanes>(), std::integral_constant<int, numbers / kE<T>>());
+  STGN_HOLDS(16, 8)
+  STGN_HOLDS(16, 16)
+  STGN_HOLDS(64, 8)
+  STGN_HOLDS(64, 16)
+  STGN_HOLDS(256, 8)
+  STGN_HOLDS(256, 16)
+  STGN_HOLDS(512, 16)
+  if constexpr (GRAD) {
+    STGN_HOLDS(512, 32)
+  } else {
+    STGN_HOLDS(1024, 16)
+    if constexpr (kE<T> == 8) STGN_HOLDS(1024, 32)
+  }
 #undef STGN_HOLDS
   return longer();
 }
@@ -272,7 +300,7 @@ inline int64_t blocks_for(int64_t rows, int lanes) {
 
 template <class T, Kind KIND>
 hipError_t rows_of(const NormArgs& a, hipStream_t s) {
-  return by_width<T>(
+  return by_width<T, false>(
       a.width,
       [&](auto lanes, auto pieces) {
         constexpr int L = decltype(lanes)::value, N = decltype(pieces)::value;
@@ -301,10 +329,14 @@ __global__ __launch_bounds__(block_of(LANES)) void grad_kernel(NormGradArgs a, f
   const int lane = (int)threadIdx.x % LANES;
   const RowEnd end = row_end<T>(a.width);
   float acc[NP][E];
+  u32x4 rg[NP];
 #pragma unroll
-  for (int i = 0; i < NP; ++i)
+  for (int i = 0; i < NP; ++i) {
+    const int c = (lane + i * LANES) * E;
+    rg[i] = c < a.width ? load_own(static_cast<const T*>(a.gain), c, a.width) : u32x4{0, 0, 0, 0};
 #pragma unroll
     for (int j = 0; j < E; ++j) acc[i][j] = 0.f;
+  }
   for (int64_t row = (int64_t)blockIdx.x * PER + (int)threadIdx.x / LANES; row < a.rows; row += (int64_t)gridDim.x * PER) {
     const T* h = static_cast<const T*>(a.h) + row * a.ld_h;
     const T* dy = static_cast<const T*>(a.dy) + row * a.ld_dy;
@@ -315,48 +347,55 @@ __global__ __launch_bounds__(block_of(LANES)) void grad_kernel(NormGradArgs a, f
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
         const int c = (lane + i * LANES) * E;
-        rh[i] = ry[i] = rd[i] = u32x4{0, 0, 0, 0};
+        rh[i] = ry[i] = u32x4{0, 0, 0, 0};
         if (c < a.width) {
           rh[i] = load16<T, END>(h + c, a.width - c);
           ry[i] = load16<T, END>(dy + c, a.width - c);
-          if (dh) rd[i] = load16<T, END>(dh + c, a.width - c);
         }
       }
     });
     double squares = 0.0, dots = 0.0;
-    float t[NP][E];                                           // g dy
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const int c = (lane + i * LANES) * E;
-      float hv[E], gv[E];
+      float hv[E], yv[E], gv[E];
       unpack<T>(rh[i], hv);
-      unpack<T>(ry[i], t[i]);
-      unpack<T>(c < a.width ? load_own(static_cast<const T*>(a.gain), c, a.width) : u32x4{0, 0, 0, 0}, gv);
+      unpack<T>(ry[i], yv);
+      unpack<T>(rg[i], gv);
 #pragma unroll
       for (int j = 0; j < E; ++j) {
-        t[i][j] *= gv[j];
         squares = fma((double)hv[j], (double)hv[j], squares);
-        dots = fma((double)t[i][j], (double)hv[j], dots);
+        dots = fma((double)(yv[j] * gv[j]), (double)hv[j], dots);
       }
     }
+    __builtin_amdgcn_sched_barrier(0);                        // (dh is asked for when the sums' registers are free, and arrives while they go across)
+    by_end(end, [&](auto e) {
+      constexpr RowEnd END = decltype(e)::value;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const int c = (lane + i * LANES) * E;
+        rd[i] = dh && c < a.width ? load16<T, END>(dh + c, a.width - c) : u32x4{0, 0, 0, 0};
+      }
+    });
     squares = sum_across<LANES>(squares, sums[0]);
     dots = sum_across<LANES>(dots, sums[1]);
     const Back b = back_of(squares, dots, a.width, a.eps);
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int c = (lane + i * LANES) * E;
-      float hv[E], yv[E], dv[E];
+      float hv[E], yv[E], gv[E], dv[E];
       unpack<T>(rh[i], hv);
       unpack<T>(ry[i], yv);
+      unpack<T>(rg[i], gv);
       unpack<T>(rd[i], dv);
 #pragma unroll
       for (int j = 0; j < E; ++j) {
         const float unit = hv[j] * b.r;
         acc[i][j] = fmaf(yv[j], unit, acc[i][j]);
-        dv[j] = fmaf(b.r, fmaf(-unit, b.back, t[i][j]), dv[j]);
+        dv[j] = fmaf(b.r, fmaf(-unit, b.back, yv[j] * gv[j]), dv[j]);
       }
       if (a.dx && c < a.width) store_piece(static_cast<T*>(a.dx) + row * a.ld_dx, c, a.width, dv);
     }
+    if constexpr (LANES > 64) __syncthreads();
   }
   if (!a.dgain) return;
   if constexpr (PER > 1) {
@@ -420,6 +459,7 @@ __global__ __launch_bounds__(1024) void long_grad_kernel(NormGradArgs a, float* 
     dots = sum_across<LANES>(dots, sums[1]);
     const Back b = back_of(squares, dots, a.width, a.eps);
     if (a.dgain && threadIdx.x == 0) r[row] = b.r;
+    __syncthreads();                                          // (the sums' LDS)
     if (!a.dx) continue;
     each([&](int c, float (&hv)[E], float (&t)[E]) {
       float dv[E];
@@ -449,21 +489,26 @@ __global__ __launch_bounds__(256) void long_gain_kernel(NormGradArgs a, const fl
     store4(part + chunk * a.width, n, a.width, (wsum[0][lane] + wsum[1][lane]) + (wsum[2][lane] + wsum[3][lane]));
 }
 
+// The partial sums of sixteen columns a workgroup, in their order but for 64 runs that are added at the end (in 64 bits: as many as the partial sums are, their
+// order then costs no bit)
 template <class T>
 __global__ __launch_bounds__(1024) void gain_kernel(const float* part, int parts, int width, T* dgain) {
-  __shared__ float wsum[16][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (int)blockIdx.x * 64 + lane;
-  float acc = 0.f;
+  __shared__ double wsum[16][16];
+  const int column = threadIdx.x & 15, c = (int)blockIdx.x * 16 + column;
+  double acc = 0.0;
   if (c < width) {
 #pragma unroll 8
-    for (int i = wave; i < parts; i += 16) acc += part[(int64_t)i * width + c];
+    for (int i = (int)threadIdx.x >> 4; i < parts; i += 64) acc += (double)part[(int64_t)i * width + c];
   }
-  wsum[wave][lane] = acc;
+  acc += __shfl_xor(acc, 16);
+  acc += __shfl_xor(acc, 32);
+  if ((threadIdx.x & 63) < 16) wsum[threadIdx.x >> 6][column] = acc;
   __syncthreads();
-  if (wave == 0 && c < width) {
+  if (threadIdx.x < 16 && c < width) {
+    acc = wsum[0][column];
 #pragma unroll
-    for (int w = 1; w < 16; ++w) acc += wsum[w][lane];
-    dgain[c] = (T)acc;
+    for (int w = 1; w < 16; ++w) acc += wsum[w][column];
+    dgain[c] = (T)(float)acc;
   }
 }
 
@@ -474,11 +519,13 @@ struct GradPlan { int64_t blocks; int parts, rows_per; size_t sums, total; bool 
 template <class T>
 GradPlan grad_plan(const NormGradArgs& a) {
   GradPlan p{};
-  by_width<T>(
+  by_width<T, true>(
       a.width,
       [&](auto lanes, auto) {
-        p.blocks = blocks_for(a.rows, decltype(lanes)::value);
-        if (a.dgain && p.blocks > 1024) p.blocks = 1024;
+        constexpr int L = decltype(lanes)::value;
+        p.blocks = blocks_for(a.rows, L);
+        // two workgroups a CU, or a large one: each has its partial sums (16,384 x 4,096 in bf16: 512 workgroups 102 us, 768 107, 1,024 122, 256 136)
+        if (a.dgain) p.blocks = p.blocks < (L <= 256 ? 512 : 256) ? p.blocks : (L <= 256 ? 512 : 256);
         p.parts = (int)p.blocks;
         return hipSuccess;
       },
@@ -504,7 +551,7 @@ hipError_t backward(const NormGradArgs& a, void* ws, hipStream_t s) {
   float* part = ws ? reinterpret_cast<float*>(static_cast<char*>(ws) + p.sums) : nullptr;
   hipError_t e = hipSuccess;
   if (p.blocks > 0)
-    e = by_width<T>(
+    e = by_width<T, true>(
         a.width,
         [&](auto lanes, auto pieces) {
           constexpr int L = decltype(lanes)::value, N = decltype(pieces)::value;
@@ -517,49 +564,70 @@ hipError_t backward(const NormGradArgs& a, void* ws, hipStream_t s) {
           return f;
         });
   if (e == hipSuccess && a.dgain && (p.parts != 1 || p.is_long))
-    e = launch(gain_kernel<T>, (a.width + 63) / 64, 1024, s, (const float*)part, p.parts, a.width, static_cast<T*>(a.dgain));
+    e = launch(gain_kernel<T>, (a.width + 15) / 16, 1024, s, (const float*)part, p.parts, a.width, static_cast<T*>(a.dgain));
   return e;
 }
 
-// ---- columns in 8 bits: largest magnitudes of 256 columns over chunks of rows, then tiles turned over through LDS
+// ---- columns in 8 bits: largest magnitudes of a piece's columns a lane over chunks of rows, then tiles turned over through LDS
 
 template <class T>
-__global__ __launch_bounds__(256) void column_tops_kernel(ColumnsArgs a, uint32_t* tops, int rows_per) {
-  __shared__ uint32_t wtop[4][256];
+__global__ __launch_bounds__(1024) void column_tops_kernel(ColumnsArgs a, uint32_t* tops, int rows_per) {
+  constexpr int E = kE<T>, WIDE = 64 * E;                     // columns a workgroup, a piece a lane
+  __shared__ uint32_t wtop[16][WIDE];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int cols = (a.width + 255) / 256, n0 = (int)(blockIdx.x % cols) * 256, n = n0 + lane * 4;
+  const int cols = (a.width + WIDE - 1) / WIDE, n0 = (int)(blockIdx.x % cols) * WIDE, n = n0 + lane * E;
   const int64_t chunk = blockIdx.x / cols, m1 = min((int64_t)a.rows, (chunk + 1) * rows_per);
-  uint32_t top[4] = {0, 0, 0, 0};
+  uint32_t top[E];
+#pragma unroll
+  for (int j = 0; j < E; ++j) top[j] = 0;
   if (n < a.width) {
 #pragma unroll 8
-    for (int64_t m = chunk * rows_per + wave; m < m1; m += 4) {
-      const floatx4 v = load4(static_cast<const T*>(a.x) + m * a.ld_x, n, a.width);
+    for (int64_t m = chunk * rows_per + wave; m < m1; m += 16) {
+      float v[E];
+      unpack<T>(load_own(static_cast<const T*>(a.x) + m * a.ld_x, n, a.width), v);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) top[j] = max(top[j], magnitude(v[j]));
+      for (int j = 0; j < E; ++j) top[j] = max(top[j], magnitude(v[j]));
     }
   }
 #pragma unroll
-  for (int j = 0; j < 4; ++j) wtop[wave][lane * 4 + j] = top[j];
+  for (int j = 0; j < E; ++j) wtop[wave][lane * E + j] = top[j];
   __syncthreads();
   const int c = (int)threadIdx.x;
-  if (n0 + c < a.width) tops[chunk * a.width + n0 + c] = max(max(wtop[0][c], wtop[1][c]), max(wtop[2][c], wtop[3][c]));
+  if (c < WIDE && n0 + c < a.width) {
+    uint32_t t = wtop[0][c];
+#pragma unroll
+    for (int w = 1; w < 16; ++w) t = max(t, wtop[w][c]);
+    tops[chunk * a.width + n0 + c] = t;
+  }
 }
 
 constexpr int kTileRows = 128, kTileCols = 64;
 
 template <class T>
 __global__ __launch_bounds__(256) void columns_kernel(ColumnsArgs a, const uint32_t* tops, int chunks) {
-  constexpr int E = kE<T>, STRIDE = kTileRows + 16;
+  constexpr int E = kE<T>, STRIDE = kTileRows + 16, ACROSS = kTileCols / E, ITEMS = kTileRows / 4 * ACROSS / 256;
   __shared__ uint32_t part[4][kTileCols], top[kTileCols];
   __shared__ __attribute__((aligned(16))) int8_t tile[kTileCols * STRIDE];
   const int tiles_n = (a.width + kTileCols - 1) / kTileCols;
   const int n0 = (int)(blockIdx.x % tiles_n) * kTileCols;
   const int64_t m0 = (int64_t)(blockIdx.x / tiles_n) * kTileRows;
+  u32x4 raw[ITEMS][4];                                        // four rows of a piece; on their way while the columns' maxima are found
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i) {
+    const int at = i * 256 + (int)threadIdx.x, c = n0 + at % ACROSS * E;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int64_t m = m0 + at / ACROSS * 4 + u;
+      raw[i][u] = m < a.rows && c < a.width ? load_own(static_cast<const T*>(a.x) + m * a.ld_x, c, a.width) : u32x4{0, 0, 0, 0};
+    }
+  }
   {
     const int c = threadIdx.x & 63, from = threadIdx.x >> 6;
     uint32_t t = 0;
-    if (n0 + c < a.width)
+    if (n0 + c < a.width) {
+#pragma unroll 8
       for (int i = from; i < chunks; i += 4) t = max(t, tops[(int64_t)i * a.width + n0 + c]);
+    }
     part[from][c] = t;
     __syncthreads();
     if (from == 0) {
@@ -569,15 +637,13 @@ __global__ __launch_bounds__(256) void columns_kernel(ColumnsArgs a, const uint3
     }
     __syncthreads();
   }
-  // four rows of a piece: a word of four bytes in each of the piece's columns
-  for (int i = threadIdx.x; i < kTileRows / 4 * (kTileCols / E); i += 256) {
-    const int piece = i % (kTileCols / E), quad = i / (kTileCols / E), c = n0 + piece * E;
+  // a word of four rows' bytes in each of the piece's columns
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i) {
+    const int at = i * 256 + (int)threadIdx.x, piece = at % ACROSS, quad = at / ACROSS;
     float v[4][E];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int64_t m = m0 + quad * 4 + u;
-      unpack<T>(m < a.rows && c < a.width ? load_own(static_cast<const T*>(a.x) + m * a.ld_x, c, a.width) : u32x4{0, 0, 0, 0}, v[u]);
-    }
+    for (int u = 0; u < 4; ++u) unpack<T>(raw[i][u], v[u]);
 #pragma unroll
     for (int j = 0; j < E; ++j) {
       const uint32_t t = top[piece * E + j];
@@ -602,18 +668,20 @@ __global__ __launch_bounds__(256) void columns_kernel(ColumnsArgs a, const uint3
   }
 }
 
-inline int column_chunks(int64_t rows, int64_t width) {
-  const int64_t cols = (width + 255) / 256, want = (1024 + cols - 1) / cols, most = rows <= 32 ? 1 : (rows + 31) / 32;
+template <class T>
+inline int column_chunks(int64_t rows, int64_t width) {       // of 128 rows and more, a workgroup for every CU
+  const int64_t cols = (width + 64 * kE<T> - 1) / (64 * kE<T>), want = (256 + cols - 1) / cols, most = rows <= 128 ? 1 : (rows + 127) / 128;
   return (int)(want < most ? want : most);
 }
-inline size_t columns_bytes(const ColumnsArgs& a) { return (size_t)column_chunks(a.rows, a.width) * a.width * sizeof(uint32_t); }
+template <class T>
+size_t columns_bytes(const ColumnsArgs& a) { return (size_t)column_chunks<T>(a.rows, a.width) * a.width * sizeof(uint32_t); }
 
 template <class T>
 hipError_t columns(const ColumnsArgs& a, void* ws, hipStream_t s) {
-  int chunks = column_chunks(a.rows, a.width);
+  const int chunks = column_chunks<T>(a.rows, a.width);
   const int rows_per = (a.rows + chunks - 1) / chunks > 0 ? (a.rows + chunks - 1) / chunks : 1;
   uint32_t* tops = static_cast<uint32_t*>(ws);
-  hipError_t e = launch(column_tops_kernel<T>, (int64_t)chunks * ((a.width + 255) / 256), 256, s, a, tops, rows_per);
+  hipError_t e = launch(column_tops_kernel<T>, (int64_t)chunks * ((a.width + 64 * kE<T> - 1) / (64 * kE<T>)), 1024, s, a, tops, rows_per);
   if (e != hipSuccess) return e;
   const int64_t down = a.rows ? (a.rows + kTileRows - 1) / kTileRows : 1;           // (no rows: the scales)
   return launch(columns_kernel<T>, down * ((a.width + kTileCols - 1) / kTileCols), 256, s, a, (const uint32_t*)tops, chunks);

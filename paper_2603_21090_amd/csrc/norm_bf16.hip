@@ -7,5 +7,5 @@ size_t rms_norm_grad_bytes_bf16(const NormGradArgs& a) { return norm::grad_plan<
 hipError_t rms_norm_grad_bf16(const NormGradArgs& a, void* ws, hipStream_t s) { return norm::backward<__bf16>(a, ws, s); }
 hipError_t rows_in_8_bf16(const NormArgs& a, hipStream_t s) { return norm::rows_of<__bf16, norm::kRows8>(a, s); }
 hipError_t columns_in_8_bf16(const ColumnsArgs& a, void* ws, hipStream_t s) { return norm::columns<__bf16>(a, ws, s); }
-size_t columns_bytes_bf16(const ColumnsArgs& a) { return norm::columns_bytes(a); }
+size_t columns_bytes_bf16(const ColumnsArgs& a) { return norm::columns_bytes<__bf16>(a); }
 }  // namespace stgn
