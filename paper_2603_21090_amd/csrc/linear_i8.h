@@ -4,11 +4,14 @@
 //
 // Both operands have k along their rows, so every fragment is 16 neighbouring bytes.  Accumulators hold the transposed tile, four neighbouring columns
 // of one output row a lane.  Four kernels:
-//   few rows   weights go from memory into the matrix instructions without LDS, waves share k and add up at the end: one launch, bound by the weight's bytes
+//   fragments  operands go from memory into the matrix instructions without LDS, eight waves share k and add up at the end: for few rows or small outputs,
+//              where what counts is one latency instead of one for each tile of k
 //   64 x 64    tiles through registers into LDS, any alignment, k split where tiles are few
 //   128 x 128  the same, and as a variant whose tiles go from memory into LDS directly, for operands in whole pieces of 16 bytes
 //   256 x 256  directly too, two groups of four waves in turn, one multiplying while the other reads
 #pragma once
+#include <utility>
+
 #include "linear.h"
 
 namespace stgn {
@@ -76,7 +79,7 @@ __device__ inline i32x4 load_sums(const int* row, int n, int cols) {
   return v;
 }
 
-// ---- few rows
+// ---- fragments straight from memory
 
 // The last `count` of a piece's 16 bytes, zeros in front (0 and less: none; 16 and more: all)
 __device__ inline i32x4 last_bytes(const i32x4& v, int count) {
@@ -95,19 +98,22 @@ __device__ inline i32x4 piece_at(const int8_t* row, int k, int total) {
   return __builtin_bit_cast(i32x4, *reinterpret_cast<const u32x4_any*>(row + min(k, total - 16)));
 }
 
-// 16 MB rows and 16 NB columns a workgroup; eight waves take 128 bytes of k each in turn, four of their turns are on their way at once.
-// (4 x 4,096 x 4,096: 5.8 us, 2.9 TB/s of weights with the launch; four splits of 64 x 64 tiles and their joining 10.9)
+// 16 MB rows and 16 NB columns a workgroup; eight waves take 128 bytes of k each in turn, four of their turns are on their way at once (4 x 4,096 x 4,096: 5.9
+// us, 2.9 TB/s of weights with the launch, and 11 in tiles of 64 x 64 with 8 splits and their joining; 1,024 x 1,024 x 1,024: 8.3 and 12)
 template <class T, int MB, int NB>
-__global__ __launch_bounds__(512) void few_rows_kernel(Product a) {
-  constexpr int WAVES = 8, DEPTH = MB > 2 ? 2 : 4;
+__global__ __launch_bounds__(512) void fragments_kernel(Product a) {
+  constexpr int WAVES = 8, DEPTH = MB + NB > 6 ? 2 : 4;
   __shared__ i32x4 part[WAVES][MB * NB][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i16 = lane & 15, g = lane >> 4;
-  const int n0 = (int)blockIdx.x * 16 * NB;
+  const unsigned tm = (unsigned)(a.m + 16 * MB - 1) / (16 * MB), tn = (unsigned)(a.n + 16 * NB - 1) / (16 * NB);
+  int row, col;
+  dense::tile_of(blockIdx.x, tm, tn, row, col);
+  const int m0 = row * 16 * MB, n0 = col * 16 * NB;
   const int8_t *l[NB], *r[MB];
 #pragma unroll
   for (int x = 0; x < NB; ++x) l[x] = a.l + (int64_t)min(n0 + x * 16 + i16, a.n - 1) * a.ld_l;
 #pragma unroll
-  for (int y = 0; y < MB; ++y) r[y] = a.r + (int64_t)min(y * 16 + i16, a.m - 1) * a.ld_r;
+  for (int y = 0; y < MB; ++y) r[y] = a.r + (int64_t)min(m0 + y * 16 + i16, a.m - 1) * a.ld_r;
   i32x4 lf[DEPTH][2][NB], rf[DEPTH][2][MB], acc[NB][MB];
 #pragma unroll
   for (int x = 0; x < NB; ++x)
@@ -161,7 +167,7 @@ __global__ __launch_bounds__(512) void few_rows_kernel(Product a) {
     i32x4 sum = part[0][b][lane];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) sum += part[w][b][lane];
-    const int m = b % MB * 16 + i16, n = n0 + b / MB * 16 + 4 * g;
+    const int m = m0 + b % MB * 16 + i16, n = n0 + b / MB * 16 + 4 * g;
     if (m < a.m && n < a.n) finish4<T>(a, m, n, sum);
   }
 }
@@ -546,8 +552,8 @@ __global__ __launch_bounds__(256) void join_kernel(Product a) {
   }
 }
 
-enum Kind { kFewRows, kSmall, kMiddle, kDirect, kLarge };
-struct Plan { Kind kind; int splits, k_per; };
+enum Kind { kFragments, kSmall, kMiddle, kDirect, kLarge };
+struct Plan { Kind kind; int splits, k_per, mb, nb; };         // mb, nb: blocks of 16 rows and columns (fragments)
 
 // Operands in whole pieces of 16 bytes, whose tiles' offsets are 32-bit numbers
 inline bool whole_pieces(const Linear8Args& f) {
@@ -556,18 +562,28 @@ inline bool whole_pieces(const Linear8Args& f) {
 }
 
 // Which kernel, by the number of tiles and the length of their sums (us, bf16 outputs with the full epilogue; each pair is the two sides of a rule):
-//   few rows   up to 64 rows: 64 x 4,096 x 4,096 12.1, tiles with the best split 12.2; 16 rows 6.7 and 9.2
-//   256 x 256  whole tiles of 64 of k, long sums, and tiles that fill the 256 CUs' rounds to nine tenths: 8,192 x 4,096 x 4,096 137, in 128 x 128 146; 3,000 x
-//              5,000 x 2,000 58 and 66; but 5,000 x 4,096 x 4,096 (320 tiles) 142 and 115, 4,096 x 8,192 x 256 65 and 61
-//   128 x 128  from 2^32 multiplications on (padded) where tiles go into LDS directly: 512 x 4,096 x 4,096 24.2, in 64 x 64 31.4; 16,384 x 256 x 1,024 16.7 and
-//              18.2; but 512 x 4,096 x 1,024 15.3 and 11.8; k split to make a workgroup for every CU (200 x 4,096 x 4,096 in one 26.5, in four 18.6)
-//              from 2^34 on through registers: 1,024 x 4,096 x 4,096 42 and 47; but 4,000 x 1,000 x 1,000 26 and 19
+//   fragments  the smallest tile that makes 256 workgroups at most (500 x 500 x 500: 32 x 32 4.0, 32 x 16 4.1, 32 x 64 4.5; 16 x 11,008 x 4,096: 32 x 64 13.3, 16 x 16 14.6) and
+//              reads 400 KB of operands a workgroup at most (256 x 2,048 x 4,096, 393 KB: 14.5, in 128 x 128 16.6; 128 x 4,096 x 8,192, 786 KB: 25.5 and
+//              20.4), with up to 16 rows 1 MB; rows that no 16 bytes align cost it three times that: 64 KB (100 x 1,000 x 999, 48 KB: 5.8, in 64 x 64 8.4;
+//              1,000 x 257 x 1,999, 192 KB: 15.9 and 13.5)
+//   256 x 256  whole tiles of 64 of k, long sums, and tiles that fill the 256 CUs' rounds to nine tenths: 8,192 x 4,096 x 4,096 153, in 128 x 128 182;
+//              2,048 x 8,192 x 4,096 95 and 104; but 5,000 x 4,096 x 4,096 (320 tiles) 141 and 130
+//   128 x 128  from 2^32 multiplications on (padded) where tiles go into LDS directly: 512 x 4,096 x 4,096 24.1, in 64 x 64 31.5; 16,384 x 256 x 1,024 17.7 and
+//              19.3; but 512 x 4,096 x 1,024 16.8 and 14.2; k split to make a workgroup for every CU (200 x 4,096 x 4,096 in one 26.5, in four 18.6)
+//              from 2^34 on through registers: 1,024 x 4,096 x 4,096 42 and 47; but 4,000 x 1,000 x 1,000 28 and 20
 //   64 x 64    everything smaller, k split while there are fewer than 1,024 workgroups, eight tiles of k a split at least, four where there are few workgroups
 //              (70 x 64 x 8,192 in 8 splits 12.6, in 16 9.1)
 inline Plan plan_of(int64_t m, int64_t n, int64_t k, bool whole) {
   const auto tiles_of = [&](int64_t b) { return ((m + b - 1) / b) * ((n + b - 1) / b); };
-  Plan p{kFewRows, 1, (int)up(k, kBK)};
-  if (m <= 64) return p;
+  Plan p{kFragments, 1, (int)up(k, kBK), 0, 0};
+  const int64_t most = !whole ? 64 << 10 : m <= 16 ? 1 << 20 : 400 << 10;
+  for (const auto& b : {std::pair<int, int>{1, 1}, {2, 1}, {2, 2}, {2, 4}, {4, 4}}) {
+    p.mb = b.first;
+    p.nb = b.second;
+    if (((m + 16 * p.mb - 1) / (16 * p.mb)) * ((n + 16 * p.nb - 1) / (16 * p.nb)) > 256) continue;
+    if (16 * (p.mb + p.nb) * k <= most) return p;
+    break;
+  }
   const auto split = [&](int64_t tiles, int64_t workgroups, int64_t least) {
     int64_t splits = workgroups / tiles;
     if (splits > k / (least * kBK)) splits = k / (least * kBK);
@@ -605,10 +621,14 @@ hipError_t run(Product a, const Plan& p, void* ws, hipStream_t s) {
   const auto grid = [&](int64_t b) { return ((a.m + b - 1) / b) * ((a.n + b - 1) / b) * p.splits; };
   hipError_t e = hipErrorInvalidValue;
   switch (p.kind) {
-    case kFewRows:
-      if (a.m <= 16) return launch(few_rows_kernel<T, 1, 1>, (a.n + 15) / 16, 512, s, a);
-      if (a.m <= 32) return launch(few_rows_kernel<T, 2, 1>, (a.n + 15) / 16, 512, s, a);
-      return launch(few_rows_kernel<T, 4, 1>, (a.n + 15) / 16, 512, s, a);
+    case kFragments: {
+      const int64_t n = ((a.m + 16 * p.mb - 1) / (16 * p.mb)) * (int64_t)((a.n + 16 * p.nb - 1) / (16 * p.nb));
+      if (p.mb == 1) return launch(fragments_kernel<T, 1, 1>, n, 512, s, a);
+      if (p.mb == 4) return launch(fragments_kernel<T, 4, 4>, n, 512, s, a);
+      if (p.nb == 1) return launch(fragments_kernel<T, 2, 1>, n, 512, s, a);
+      if (p.nb == 2) return launch(fragments_kernel<T, 2, 2>, n, 512, s, a);
+      return launch(fragments_kernel<T, 2, 4>, n, 512, s, a);
+    }
     case kSmall: e = launch(product_kernel<T, 64, 64, 2, 2, 3>, grid(64), 256, s, a); break;
     case kMiddle: e = launch(product_kernel<T, 128, 128, 2, 2, 1>, grid(128), 256, s, a); break;
     case kDirect: e = launch(direct_kernel<T>, grid(128), 256, s, a); break;
