@@ -356,10 +356,21 @@ def attention_grad(dout, q, k, v, out, lse, q_lens=None, k_lens=None, causal=Fal
 
 
 def _rows(name, t, like=None):
-    """The matrix itself, or an error; of `like`'s type, device and shape."""
-    if t.dim() != 2 or t.shape[1] < 1:
+    """Address of a matrix and elements between its rows, or an error; of `like`'s type, device and shape."""
+    shape = t.shape
+    if like is not None and (t.dtype != like.dtype or t.device != like.device or shape != like.shape):
+        raise ValueError(f"{name}: {t.dtype} {tuple(shape)} on {t.device}, expected {like.dtype} {tuple(like.shape)} on {like.device}")
+    if len(shape) != 2 or shape[1] < 1:
         raise ValueError(f"{name} must be a matrix with one column at least")
-    return _expect(name, t, t if like is None else like, t.shape if like is None else like.shape)
+    rows, width = shape
+    ld, apart = t.stride()
+    if apart != 1 and width > 1 and rows:
+        raise ValueError(f"{name}: the numbers of a row must lie side by side (last stride {apart})")
+    if ld < width:
+        if rows > 1:
+            raise ValueError(f"{name}: rows of {width} numbers lie {ld} apart")
+        ld = width
+    return t.data_ptr(), ld
 
 
 def _dense_like(x, dtype=None):
@@ -371,12 +382,12 @@ def _dense_like(x, dtype=None):
 def _rms_norm(x, gain, residual, eps, eight, need_y):
     import torch
     L = load_library()
-    xp, code, (rows, width) = _rows("x", x), _dtype_code(x), x.shape
+    (xp, ld_x), code, (rows, width) = _rows("x", x), _dtype_code(x), x.shape
     gp = _expect("gain", gain, x, (width,))
     rp = ld_res = hp = yp = qp = sp = 0
     y = q = scale = h = None
     if residual is not None:
-        rp, ld_res, h = _rows("residual", residual, x), _ld(residual), _dense_like(x)
+        (rp, ld_res), h = _rows("residual", residual, x), _dense_like(x)
         hp = h.data_ptr()
     if need_y:
         y = _dense_like(x)
@@ -384,7 +395,7 @@ def _rms_norm(x, gain, residual, eps, eight, need_y):
     if eight:
         q, scale = _dense_like(x, torch.int8), x.new_empty((rows,), dtype=torch.float32)
         qp, sp = q.data_ptr(), scale.data_ptr()
-    args = _PACK_NORM.pack(code, rows, width, 0, eps, _ld(x), ld_res, width, width, width, 0, 0, xp, rp, gp, hp, yp, qp, sp, 0, 0, 0, 0)
+    args = _PACK_NORM.pack(code, rows, width, 0, eps, ld_x, ld_res, width, width, width, 0, 0, xp, rp, gp, hp, yp, qp, sp, 0, 0, 0, 0)
     _run_operator(None, L.stgn_rms_norm, args, False, x.device)
     return y, q, scale, h
 
@@ -407,12 +418,12 @@ def rms_norm_grad(dy, h, gain, dh=None, eps=1e-6, need_x=True, need_gain=True):
     """Gradients of rms_norm (stgn_rms_norm_grad): (dx, dgain), None for those not asked for.  h: what rms_norm returned beside y, or its x
     where there was no residual; dh: the gradient that comes down the residual stream, added to dx.  The residual's gradient is dx too."""
     L = load_library()
-    hp, code, (rows, width) = _rows("h", h), _dtype_code(h), h.shape
-    yp, gp = _rows("dy", dy, h), _expect("gain", gain, h, (width,))
-    dp = _rows("dh", dh, h) if dh is not None else 0
+    (hp, ld_h), code, (rows, width) = _rows("h", h), _dtype_code(h), h.shape
+    (yp, ld_dy), gp = _rows("dy", dy, h), _expect("gain", gain, h, (width,))
+    dp, ld_dh = _rows("dh", dh, h) if dh is not None else (0, 0)
     dx = _dense_like(h) if need_x else None
     dgain = _dense_like(gain) if need_gain else None
-    args = _PACK_NORM.pack(code, rows, width, 0, eps, 0, 0, _ld(h), 0, 0, _ld(dy), _ld(dh) if dh is not None else 0, 0, 0, gp, hp, 0, 0, 0, yp, dp,
+    args = _PACK_NORM.pack(code, rows, width, 0, eps, 0, 0, ld_h, 0, 0, ld_dy, ld_dh, 0, 0, gp, hp, 0, 0, 0, yp, dp,
                            dx.data_ptr() if need_x else 0, dgain.data_ptr() if need_gain else 0)
     _run_operator(L.stgn_rms_norm_workspace, L.stgn_rms_norm_grad, args, True, h.device)
     return dx, dgain
@@ -423,10 +434,10 @@ def quantize(x, columns=False):
     [rows].  columns=True, for a weight [d_in, d_out]: q [d_out, d_in], scale [d_out]."""
     import torch
     L = load_library()
-    xp, code, (rows, width) = _rows("x", x), _dtype_code(x), x.shape
+    (xp, ld_x), code, (rows, width) = _rows("x", x), _dtype_code(x), x.shape
     q = x.new_empty((width, rows), dtype=torch.int8) if columns else _dense_like(x, torch.int8)
     scale = x.new_empty((width if columns else rows,), dtype=torch.float32)
-    args = _PACK_QUANTIZE.pack(code, 1 if columns else 0, rows, width, _ld(x), q.shape[1], xp, q.data_ptr(), scale.data_ptr())
+    args = _PACK_QUANTIZE.pack(code, 1 if columns else 0, rows, width, ld_x, rows if columns else width, xp, q.data_ptr(), scale.data_ptr())
     _run_operator(L.stgn_quantize_workspace if columns else None, L.stgn_quantize, args, None, x.device)
     return q, scale
 
@@ -437,25 +448,22 @@ def linear_i8(x, x_scale, w, w_scale, bias=None, activation="none", residual=Non
     else theirs, else bfloat16.  activation: as in linear."""
     import torch
     L = load_library()
-    if x.dim() != 2 or w.dim() != 2:
-        raise ValueError("x and w must be matrices")
     if activation not in ACTIVATIONS:
         raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}")
-    for name, t, want in (("x", x, torch.int8), ("x_scale", x_scale, torch.float32), ("w_scale", w_scale, torch.float32)):
-        if t.dtype != want:
-            raise ValueError(f"{name}: {t.dtype}, expected {want}")
-    (rows, d_in), d_out = x.shape, w.shape[0]
-    xp, wp = _expect("x", x, x, x.shape), _expect("w", w, x, (d_out, d_in))
-    if x_scale.device != x.device:
-        raise ValueError(f"x_scale: on {x_scale.device}, expected {x.device}")
-    sp, tp = _expect("x_scale", x_scale, x_scale, (rows,)), _expect("w_scale", w_scale, x_scale, (d_out,))
+    (xp, ld_x), (wp, ld_w) = _rows("x", x), _rows("w", w)
+    (rows, d_in), (d_out, k), device = x.shape, w.shape, x.device
+    if x.dtype != torch.int8 or w.dtype != torch.int8 or w.device != device or k != d_in:
+        raise ValueError(f"x and w must be int8 matrices of the same d_in on one device, not {x.dtype} {tuple(x.shape)} on {device} and {w.dtype} {tuple(w.shape)} on {w.device}")
+    for name, t, n in (("x_scale", x_scale, rows), ("w_scale", w_scale, d_out)):
+        if t.dtype != torch.float32 or t.device != device or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
+            raise ValueError(f"{name}: a dense float32 tensor [{n}] on {device} is expected")
     if dtype is None:
         dtype = bias.dtype if bias is not None else residual.dtype if residual is not None else torch.bfloat16
     y = x.new_empty((rows, d_out), dtype=dtype)
     bp = _expect("bias", bias, y, (d_out,)) if bias is not None else 0
-    rp = _expect("residual", residual, y, y.shape) if residual is not None else 0
-    args = _PACK_LINEAR_I8.pack(_dtype_code(y), ACTIVATIONS[activation], rows, d_in, d_out, 0, _ld(x), _ld(w), _ld(residual) if rp else 0, d_out,
-                                xp, wp, sp, tp, bp, rp, y.data_ptr())
+    rp, ld_res = _rows("residual", residual, y) if residual is not None else (0, 0)
+    args = _PACK_LINEAR_I8.pack(_dtype_code(y), ACTIVATIONS[activation], rows, d_in, d_out, 0, ld_x, ld_w, ld_res, d_out,
+                                xp, wp, x_scale.data_ptr(), w_scale.data_ptr(), bp, rp, y.data_ptr())
     _run_operator(L.stgn_linear_quantized_workspace, L.stgn_linear_quantized, args, None, x.device)
     return y
 
@@ -466,14 +474,14 @@ def dropout(x, p, rng, site=0, residual=None):
     the backward pass, not between it and the forward one.  The residual's gradient is dy, x's is dropout_grad."""
     import torch
     L = load_library()
-    xp, code, (rows, width) = _rows("x", x), _dtype_code(x), x.shape
+    (xp, ld_x), code, (rows, width) = _rows("x", x), _dtype_code(x), x.shape
     if rng.dtype != torch.int64 or rng.device != x.device or rng.shape != (2,) or not rng.is_contiguous():
         raise ValueError(f"rng: a dense int64 tensor [2] on {x.device} is expected")
-    rp = _rows("residual", residual, x) if residual is not None else 0
+    rp, ld_res = _rows("residual", residual, x) if residual is not None else (0, 0)
     y = _dense_like(x)
     if not 0 <= site <= 65535:
         raise ValueError("site must lie in 0 .. 65535")
-    args = _PACK_DROPOUT.pack(code, rows, width, site, p, _ld(x), _ld(residual) if residual is not None else 0, width, xp, rp, y.data_ptr(), rng.data_ptr())
+    args = _PACK_DROPOUT.pack(code, rows, width, site, p, ld_x, ld_res, width, xp, rp, y.data_ptr(), rng.data_ptr())
     _run_operator(None, lambda a, ws, size, stream: L.stgn_dropout(a, stream), args, None, x.device)
     return y
 

@@ -290,14 +290,19 @@ __device__ inline void meet_here() {
 }
 __device__ inline uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
 
-// LDS rows hold BK bytes of k unpadded; piece p of row r lies at p ^ turn(r), so that the sixteen rows that one read touches lie in different places of
-// 256 bytes.  The column side's fragments come in pairs: of 32 columns the first holds 8 q + 0 .. 3 (q = 0 .. 3) and the second 8 q + 4 .. 7, so that
-// a lane's two accumulators are eight neighbouring outputs.
+// LDS rows hold BK bytes of k unpadded; piece p of row r lies at p ^ turn(r).  LDS gives 256 bytes a cycle to sixteen lanes of a 16-byte read, and those are lanes 0 .. 3 and
+// 12 .. 15 of one lane group with 4 .. 11 of the next: rows i of 0 .. 3 and 12 .. 15 at piece p and of 4 .. 11 at p ^ 1.  With these turns they lie in
+// sixteen different places of 256 bytes (counted: no conflicts; with the row's number as its turn every read of 64-byte rows took two cycles).  The column side's
+// fragments come in pairs: of 32 columns the first holds 8 q + 0 .. 3 (q = 0 .. 3) and the second 8 q + 4 .. 7, so that a lane's two accumulators are
+// eight neighbouring outputs.
 template <int BK, bool PAIRS>
 struct Direct {
   static constexpr int PIECES = BK / 16;
   static __device__ inline int turn(int r) {
-    if (BK == 64) return PAIRS ? (r >> 3) & 3 : (r >> 2) & 3;
+    if (BK == 64) {
+      const int q = PAIRS ? r >> 3 : r >> 2;
+      return ((q ^ q >> 1) & 1) << 1 | (q >> 1 & 1);
+    }
     return PAIRS ? ((r >> 2) & 6) | ((r >> 1) & 1) : (r >> 1) & 7;
   }
   // offset of this lane's piece of the wave's load number i from the tile's first row on, and which piece of the tile's k it is
