@@ -3,12 +3,12 @@
 //   y = act(x_scale[m] w_scale[n] sum_k x[m][k] w[n][k] + bias[n]) + residual
 //
 // Both operands have k along their rows, so every fragment is 16 neighbouring bytes.  Accumulators hold the transposed tile, four neighbouring columns
-// of one output row a lane.  Four kernels:
+// of one output row a lane.  Kernels:
 //   fragments  operands go from memory into the matrix instructions without LDS, eight waves share k and add up at the end: for few rows or small outputs,
 //              where what counts is one latency instead of one for each tile of k
 //   64 x 64    tiles through registers into LDS, any alignment, k split where tiles are few
 //   128 x 128  the same, and as a variant whose tiles go from memory into LDS directly, for operands in whole pieces of 16 bytes
-//   256 x 256  directly too, two groups of four waves in turn, one multiplying while the other reads
+//   in turns   256 x 256 and 128 x 128, directly too: two groups of four waves, one multiplying while the other reads
 #pragma once
 #include <utility>
 
@@ -479,33 +479,45 @@ __global__ __launch_bounds__(256, 2) void direct_kernel(Product a) {
   finish_pairs<T, NB, MB>(a, split, m0 + wm, n0 + wn, acc);
 }
 
-// 256 x 256 outputs a workgroup of eight waves, each 64 rows x 128 columns, four tiles of 64 bytes of k in LDS.  Two groups of four waves, one of each on
-// every SIMD, half a step apart: while one group multiplies, the other reads its next fragments and asks for the tile three steps on, so that the
-// matrix pipe has work all the time.
+// until `tiles` of this wave's latest tiles of LOADS loads are on their way at most
+template <int LOADS, int MOST>
+__device__ inline void wait_tiles(int tiles) {
+  if constexpr (MOST == 0) {
+    wait_loads<0>();
+  } else {
+    if (tiles >= MOST) wait_loads<LOADS * MOST>();
+    else wait_tiles<LOADS, MOST - 1>(tiles);
+  }
+}
+
+// BM x BN outputs a workgroup of eight waves, BUFS tiles of 64 bytes of k in LDS.  Two groups of four waves, one of each on every SIMD, half a step
+// apart: while one group multiplies, the other reads its next fragments and asks for a tile BUFS - 1 steps on, so that the matrix pipe has work all the
+// time.
 //  - A tile is read by either group after the barrier behind which both have waited for their own loads of it: the wait for tile t + 1 is in
 //    front of the barrier that ends a group's reading of tile t.
-//  - A buffer is written again (the loads of tile t + 3) after the barrier behind which both groups have their fragments of tile t - 1 in registers.
+//  - A buffer is written again (the loads of tile t + BUFS - 1) after the barrier behind which both groups have their fragments of tile t - 1 in registers.
 // Group 1 waits once more in front of the loop, group 0 behind it: both pass the same number of barriers.  k is whole tiles (a last tile that k may end in
 // cost 6 us of 146 at 8,192 x 4,096 x 4,096).
-template <class T>
-__global__ __launch_bounds__(512) void large_kernel(Product a) {
-  constexpr int BK = 64, MB = 4, NB = 8, TILE = 256 * BK, BUFS = 4, LOADS = 4;
-  __shared__ __attribute__((aligned(16))) int8_t lds[BUFS * 2 * TILE];
-  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wm = (wave & 3) * 64, wn = (wave >> 2) * 128;
-  const unsigned tm = (unsigned)(a.m + 255) / 256, tn = (unsigned)(a.n + 255) / 256;
+template <class T, int BM, int BN, int WM, int WN, int BUFS>
+__global__ __launch_bounds__(512) void turns_kernel(Product a) {
+  constexpr int BK = 64, MB = BM / WM / 16, NB = BN / WN / 16, LT = BN * BK, TILE = (BM + BN) * BK, LOADS = TILE / 1024 / 8;
+  static_assert(WM * WN == 8, "eight waves");
+  __shared__ __attribute__((aligned(16))) int8_t lds[BUFS * TILE];        // the columns' tile | the rows' tile, BUFS times
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wm = wave % WM * MB * 16, wn = wave / WM * NB * 16;
+  const unsigned tm = (unsigned)(a.m + BM - 1) / BM, tn = (unsigned)(a.n + BN - 1) / BN;
+  const int split = (int)(blockIdx.x / (tm * tn));
   int row, col;
-  dense::tile_of(blockIdx.x, tm, tn, row, col);
-  const int m0 = row * 256, n0 = col * 256, tiles = a.k / BK;
-  DirectMove<BK, true, 256, 8, false> ml;
-  DirectMove<BK, false, 256, 8, false> mr;
+  dense::tile_of(blockIdx.x % (tm * tn), tm, tn, row, col);
+  const int m0 = row * BM, n0 = col * BN, kb = split * a.k_per, tiles = (min(a.k, kb + a.k_per) - kb) / BK;
+  DirectMove<BK, true, BN, 8, false> ml;
+  DirectMove<BK, false, BM, 8, false> mr;
   static_assert(decltype(ml)::LOADS + decltype(mr)::LOADS == LOADS, "loads of a tile and wave");
-  ml.start(a.l, a.ld_l, n0, a.n, 0, wave);
-  mr.start(a.r, a.ld_r, m0, a.m, 0, wave);
+  ml.start(a.l, a.ld_l, n0, a.n, kb, wave);
+  mr.start(a.r, a.ld_r, m0, a.m, kb, wave);
   const uint32_t to = lds_address(lds);
-  auto issue = [&](int t) {
-    const uint32_t at = to + (t & (BUFS - 1)) * 2 * TILE;
-    ml.issue(at, wave, a.k - t * BK);
-    mr.issue(at + TILE, wave, a.k - t * BK);
+  auto issue = [&](int buf) {
+    ml.issue(to + buf * TILE, wave, BK);
+    mr.issue(to + buf * TILE + LT, wave, BK);
   };
   i32x4 acc[NB][MB];
 #pragma unroll
@@ -513,22 +525,22 @@ __global__ __launch_bounds__(512) void large_kernel(Product a) {
 #pragma unroll
     for (int y = 0; y < MB; ++y) acc[x][y] = i32x4{0, 0, 0, 0};
   for (int t = 0; t < BUFS - 1 && t < tiles; ++t) issue(t);
-  if (tiles >= BUFS - 1) wait_loads<LOADS*(BUFS - 2)>();
-  else wait_loads<0>();
+  wait_tiles<LOADS, BUFS - 2>(tiles - 1);
   meet_here();
   if (wave >= 4) meet_here();
+  int buf = 0;
   for (int t = 0; t < tiles; ++t) {
-    const int8_t *l = lds + (t & (BUFS - 1)) * 2 * TILE, *r = l + TILE;
+    const int8_t *l = lds + buf * TILE, *r = l + LT;
     i32x4 lf[NB], rf[MB];
 #pragma unroll
     for (int y = 0; y < MB; ++y) rf[y] = Direct<BK, false>::frag(r, wm + y * 16, 0);
 #pragma unroll
     for (int x = 0; x < NB; ++x) lf[x] = Direct<BK, true>::frag(l, wn + x * 16, 0);
     if (t + BUFS - 1 < tiles) {
-      issue(t + BUFS - 1);
+      issue(buf == 0 ? BUFS - 1 : buf - 1);
       wait_loads<LOADS*(BUFS - 2)>();
     } else {
-      wait_loads<0>();
+      wait_tiles<LOADS, BUFS - 2>(tiles - 2 - t);
     }
     wait_lds();
     meet_here();
@@ -537,9 +549,10 @@ __global__ __launch_bounds__(512) void large_kernel(Product a) {
 #pragma unroll
       for (int y = 0; y < MB; ++y) acc[x][y] = Elem<int8_t>::mma(lf[x], rf[y], acc[x][y]);
     meet_here();
+    buf = buf == BUFS - 1 ? 0 : buf + 1;
   }
   if (wave < 4) meet_here();
-  finish_pairs<T, NB, MB>(a, 0, m0 + wm, n0 + wn, acc);
+  finish_pairs<T, NB, MB>(a, split, m0 + wm, n0 + wn, acc);
 }
 
 // Sums of the splits and the epilogue, four outputs a thread
@@ -557,7 +570,7 @@ __global__ __launch_bounds__(256) void join_kernel(Product a) {
   }
 }
 
-enum Kind { kFragments, kSmall, kMiddle, kDirect, kLarge };
+enum Kind { kFragments, kSmall, kMiddle, kDirect, kTurns, kLarge };
 struct Plan { Kind kind; int splits, k_per, mb, nb; };         // mb, nb: blocks of 16 rows and columns (fragments)
 
 // Operands in whole pieces of 16 bytes, whose tiles' offsets are 32-bit numbers
@@ -574,7 +587,9 @@ inline bool whole_pieces(const Linear8Args& f) {
 //   256 x 256  whole tiles of 64 of k, long sums, and tiles that fill the 256 CUs' rounds to nine tenths: 8,192 x 4,096 x 4,096 153, in 128 x 128 182;
 //              2,048 x 8,192 x 4,096 95 and 104; but 5,000 x 4,096 x 4,096 (320 tiles) 141 and 130
 //   128 x 128  from 2^32 multiplications on (padded) where tiles go into LDS directly: 512 x 4,096 x 4,096 24.1, in 64 x 64 31.5; 16,384 x 256 x 1,024 17.7 and
-//              19.3; but 512 x 4,096 x 1,024 16.8 and 14.2; k split to make a workgroup for every CU (200 x 4,096 x 4,096 in one 26.5, in four 18.6)
+//              19.3; but 512 x 4,096 x 1,024 16.8 and 14.2; k split to make a workgroup for every CU (200 x 4,096 x 4,096 in one 26.5, in four 18.6);
+//              by eight waves in turns where a CU has one workgroup at most or little to sum (2,048 x 2,048 x 2,048 20.1, by four waves 22.1; 4,096 x 8,192 x 256
+//              66 and 70; but 16,384 x 1,024 x 1,024 50 and 47)
 //              from 2^34 on through registers: 1,024 x 4,096 x 4,096 42 and 47; but 4,000 x 1,000 x 1,000 28 and 20
 //   64 x 64    everything smaller, k split while there are fewer than 1,024 workgroups, eight tiles of k a split at least, four where there are few workgroups
 //              (70 x 64 x 8,192 in 8 splits 12.6, in 16 9.1)
@@ -602,6 +617,7 @@ inline Plan plan_of(int64_t m, int64_t n, int64_t k, bool whole) {
   } else if (whole && middle * k >= 1 << 18) {
     p.kind = kDirect;
     split(middle, 256, 8);
+    if (k % 64 == 0 && p.splits == 1 && (middle <= 256 || k <= 512)) p.kind = kTurns;
   } else if (middle * k >= 1 << 20 && middle >= 256) {
     p.kind = kMiddle;
   } else {
@@ -637,7 +653,8 @@ hipError_t run(Product a, const Plan& p, void* ws, hipStream_t s) {
     case kSmall: e = launch(product_kernel<T, 64, 64, 2, 2, 3>, grid(64), 256, s, a); break;
     case kMiddle: e = launch(product_kernel<T, 128, 128, 2, 2, 1>, grid(128), 256, s, a); break;
     case kDirect: e = launch(direct_kernel<T>, grid(128), 256, s, a); break;
-    case kLarge: return launch(large_kernel<T>, grid(256), 512, s, a);
+    case kTurns: return launch(turns_kernel<T, 128, 128, 2, 4, 5>, grid(128), 512, s, a);
+    case kLarge: return launch(turns_kernel<T, 256, 256, 4, 2, 4>, grid(256), 512, s, a);
   }
   if (e != hipSuccess || p.splits == 1) return e;
   const int64_t blocks = ((int64_t)a.m * ((a.n + 3) / 4) + 255) / 256;

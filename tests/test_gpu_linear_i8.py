@@ -148,3 +148,32 @@ def test_rows_past_32_bits(size):
         return buffer[:, 1:1 + t.shape[1]]
     got = binding.linear_i8(far(x), xs.cuda(), far(w), ws.cuda(), bias=b.cuda(), residual=far(r))
     within(got, refs.linear_i8(x, xs, w, ws, b, "none", r, dt), "y")
+
+
+# one size and more for each kernel and its edges: fragments of every shape; tiles of 64 x 64 in one sum and in several; 128 x 128 through registers (rows that no
+# 16 bytes align), directly with k that ends inside a tile, in one sum and in several; in turns with few and with many tiles; 256 x 256, whole and cut
+KINDS = [(16, 512, 4000), (33, 512, 2000), (100, 640, 1250), (60, 1500, 8100), (1000, 272, 1000), (500, 1027, 900), (300, 3001, 200), (2100, 4001, 2050), (2100, 1040, 2050),
+         (200, 4112, 4096), (1500, 2048, 1530), (2000, 512, 4090), (3900, 1088, 4090), (4096, 1024, 4096)]
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=str)
+@pytest.mark.parametrize("size", KINDS, ids=str)
+def test_every_kernel(size, dt):
+    x, xs, w, ws, b, r = (t.cuda() for t in make(*size, dt))
+    cpu = lambda t: tuple(v.cpu() for v in t)  # noqa: E731
+    within(binding.linear_i8(x, xs, w, ws, bias=b, activation="gelu", residual=r), cpu(refs.linear_i8(x, xs, w, ws, b, "gelu", r, dt)), "y")
+    within(binding.linear_i8(x, xs, w, ws, dtype=dt), cpu(refs.linear_i8(x, xs, w, ws, None, "none", None, dt)), "no epilogue")
+
+
+@pytest.mark.parametrize("size", [(260, 32784, 260), (1500, 2048, 1500)], ids=str)
+def test_rows_in_whole_pieces_that_lie_far_apart(size):
+    """Rows 2^23 - 16 bytes apart: a tile's last row lies 2^30 bytes and more from its first."""
+    x, xs, w, ws, b, _ = (t.cuda() for t in make(*size, torch.float32))
+    ld = (1 << 23) - 16
+    X = torch.empty(size[0] * ld, dtype=torch.int8, device="cuda").view(size[0], ld)[:, :size[1]]
+    X.copy_(x)
+    W = torch.empty(260 * ld if size[2] == 260 else w.numel(), dtype=torch.int8, device="cuda").view(size[2], -1)[:, :size[1]]
+    W.copy_(w)
+    got = binding.linear_i8(X, xs, W, ws, bias=b)
+    within(got, tuple(v.cpu() for v in refs.linear_i8(x, xs, w, ws, b, "none", None, torch.float32)), "y")
+    assert torch.equal(got, binding.linear_i8(x, xs, w, ws, bias=b))
