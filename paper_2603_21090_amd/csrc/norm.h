@@ -36,6 +36,21 @@ __device__ inline u32x4 load_own(const T* row, int c, int width) {
   return c + kE<T> <= width ? load16<T, kWhole>(row + c, kE<T>) : load16<T, kShort>(row + c, width - c);
 }
 
+// The piece at column c as it is asked for, and as it is used: a row that ends with a part of a piece is read from its last 16 bytes, which are moved down when they
+// are used (behind the load, the move would wait for it: 20,000 x 2,100 in bf16 181 us of gradient, TODO so)
+template <class T>
+__device__ inline u32x4 ask_piece(const T* row, int c, int width, RowEnd end) {
+  if (c >= width) return u32x4{0, 0, 0, 0};
+  if (end == kShort) return load16<T, kShort>(row + c, width - c);
+  return *reinterpret_cast<const u32x4_any*>(row + c - max(c + kE<T> - width, 0));
+}
+template <class T>
+__device__ inline u32x4 settle(const u32x4& v, int c, int width, RowEnd end) {
+  const int early = c + kE<T> - width;
+  if (end == kWide && early > 0 && early < kE<T>) return moved_down<T>(v, early * (int)sizeof(T));
+  return v;
+}
+
 template <int E>
 __device__ inline void store_bytes(int8_t* row, int c, int width, const int (&q)[E]) {
   uint32_t w[E / 4];
@@ -125,7 +140,8 @@ constexpr int block_of(int lanes) { return lanes < 256 ? 256 : lanes; }
 
 enum Kind { kNorm, kNorm8, kRows8 };                          // y; 8 bits of y (and y); 8 bits of x
 
-// Rows whose pieces stay in registers.  All of a row is read before any of it is written: outputs may lie where the inputs do.
+// Rows whose pieces stay in registers.  All of a row is read before any of it is written: outputs may lie where the inputs do.  A workgroup walks down the rows: the
+// gain is read once, and the next row is on its way while one is summed and written (in bf16 16,384 x 4,096 57 -> 50 us, 30,000 x 2,000 57 -> 47).
 template <class T, int LANES, int NP, Kind KIND>
 __global__ __launch_bounds__(block_of(LANES)) void rows_kernel(NormArgs a) {
   constexpr int E = kE<T>, PER = block_of(LANES) / LANES;
@@ -133,39 +149,51 @@ __global__ __launch_bounds__(block_of(LANES)) void rows_kernel(NormArgs a) {
   __shared__ uint32_t tops[LANES > 64 ? LANES / 64 : 1];
   const int lane = (int)threadIdx.x % LANES;
   const RowEnd end = row_end<T>(a.width);
-  for (int64_t row = (int64_t)blockIdx.x * PER + (int)threadIdx.x / LANES; row < a.rows; row += (int64_t)gridDim.x * PER) {
+  constexpr bool AHEAD = LANES < 1024 || NP * E <= 16;        // (32 numbers a lane of 1,024 leave no registers for another row)
+  u32x4 rx[NP], rr[NP], rg[NP];
+  auto ask = [&](int64_t row) {
     const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
     const T* res = a.residual ? static_cast<const T*>(a.residual) + row * a.ld_res : nullptr;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) rx[i] = ask_piece(x, (lane + i * LANES) * E, a.width, end);
+    if (res) {
+#pragma unroll
+      for (int i = 0; i < NP; ++i) rr[i] = ask_piece(res, (lane + i * LANES) * E, a.width, end);
+    }
+  };
+  const int64_t step = (int64_t)gridDim.x * PER;
+  int64_t row = (int64_t)blockIdx.x * PER + (int)threadIdx.x / LANES;
+  if (AHEAD && row < a.rows) ask(row);
+  if constexpr (KIND != kRows8) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int c = (lane + i * LANES) * E;
+      rg[i] = c < a.width ? load_own(static_cast<const T*>(a.gain), c, a.width) : u32x4{0, 0, 0, 0};
+    }
+  }
+  for (; row < a.rows; row += step) {
+    if (!AHEAD) ask(row);
     float v[NP][E];
-    by_end(end, [&](auto e) {
-      constexpr RowEnd END = decltype(e)::value;
-      u32x4 rx[NP], rr[NP];
 #pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        const int c = (lane + i * LANES) * E;
-        rx[i] = rr[i] = u32x4{0, 0, 0, 0};
-        if (c < a.width) {
-          rx[i] = load16<T, END>(x + c, a.width - c);
-          if (res) rr[i] = load16<T, END>(res + c, a.width - c);
-        }
+    for (int i = 0; i < NP; ++i) {
+      const int c = (lane + i * LANES) * E;
+      unpack<T>(settle<T>(rx[i], c, a.width, end), v[i]);
+      if (a.residual) {
+        float u[E];
+        unpack<T>(settle<T>(rr[i], c, a.width, end), u);
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[i][j] += u[j];
       }
-#pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        unpack<T>(rx[i], v[i]);
-        if (res) {
-          float u[E];
-          unpack<T>(rr[i], u);
-#pragma unroll
-          for (int j = 0; j < E; ++j) v[i][j] += u[j];
-        }
-      }
-    });
+    }
+    if (AHEAD && row + step < a.rows) ask(row + step);
     if constexpr (KIND != kRows8) {
       double sum = 0.0;
 #pragma unroll
-      for (int i = 0; i < NP; ++i)
+      for (int i = 0; i < NP; ++i) {
+        if ((lane + i * LANES) * E >= a.width) continue;      // (a wave without the piece is past it at once)
 #pragma unroll
         for (int j = 0; j < E; ++j) sum = fma((double)v[i][j], (double)v[i][j], sum);
+      }
       const float r = inverse_root(sum_across<LANES>(sum, sums), a.width, a.eps);
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
@@ -173,7 +201,7 @@ __global__ __launch_bounds__(block_of(LANES)) void rows_kernel(NormArgs a) {
         if (c >= a.width) continue;
         if (a.h) store_piece(static_cast<T*>(a.h) + row * a.ld_h, c, a.width, v[i]);
         float g[E];
-        unpack<T>(load_own(static_cast<const T*>(a.gain), c, a.width), g);
+        unpack<T>(rg[i], g);
 #pragma unroll
         for (int j = 0; j < E; ++j) v[i][j] = normed<T>(v[i][j], r, g[j]);
         if (KIND == kNorm || a.y) store_piece(static_cast<T*>(a.y) + row * a.ld_y, c, a.width, v[i]);
@@ -279,14 +307,20 @@ hipError_t by_width(int width, F f, L longer) {
   STGN_HOLDS(16, 16)
   STGN_HOLDS(64, 8)
   STGN_HOLDS(64, 16)
-  STGN_HOLDS(256, 8)
+  if constexpr (kE<T> == 8) {
+    STGN_HOLDS(64, 32)
+  } else {
+    STGN_HOLDS(256, 8)
+  }
   STGN_HOLDS(256, 16)
   STGN_HOLDS(512, 16)
   if constexpr (GRAD) {
     STGN_HOLDS(512, 32)
   } else {
     STGN_HOLDS(1024, 16)
-    if constexpr (kE<T> == 8) STGN_HOLDS(1024, 32)
+    if constexpr (kE<T> == 8) {
+      STGN_HOLDS(1024, 32)
+    }
   }
 #undef STGN_HOLDS
   return longer();
@@ -304,7 +338,12 @@ hipError_t rows_of(const NormArgs& a, hipStream_t s) {
       a.width,
       [&](auto lanes, auto pieces) {
         constexpr int L = decltype(lanes)::value, N = decltype(pieces)::value;
-        return launch(rows_kernel<T, L, N, KIND>, blocks_for(a.rows, L), block_of(L), s, a);
+        int64_t blocks = blocks_for(a.rows, L);
+        // four workgroups a CU, two of 512 lanes, one of 1,024 walk down the rows (16,384 x 4,096 in bf16: 50 us, a workgroup a row 52; in 8 bits 52 and 68).  With a
+        // residual, whose four streams keep memory busy anyhow, a workgroup a row (92 us, 101 walking).
+        const int64_t most = L <= 256 ? 1024 : L == 512 ? 512 : 256;
+        if (!(KIND == kNorm && a.residual) && blocks > most) blocks = most;
+        return launch(rows_kernel<T, L, N, KIND>, blocks, block_of(L), s, a);
       },
       [&]() { return launch(long_rows_kernel<T, KIND>, a.rows < kMostBlocks ? a.rows : kMostBlocks, 1024, s, a); });
 }
@@ -337,26 +376,41 @@ __global__ __launch_bounds__(block_of(LANES)) void grad_kernel(NormGradArgs a, f
 #pragma unroll
     for (int j = 0; j < E; ++j) acc[i][j] = 0.f;
   }
-  for (int64_t row = (int64_t)blockIdx.x * PER + (int)threadIdx.x / LANES; row < a.rows; row += (int64_t)gridDim.x * PER) {
-    const T* h = static_cast<const T*>(a.h) + row * a.ld_h;
-    const T* dy = static_cast<const T*>(a.dy) + row * a.ld_dy;
-    const T* dh = a.dh ? static_cast<const T*>(a.dh) + row * a.ld_dh : nullptr;
-    u32x4 rh[NP], ry[NP], rd[NP];
-    by_end(end, [&](auto e) {
-      constexpr RowEnd END = decltype(e)::value;
+  constexpr bool AHEAD = NP < 8;                              // (32 numbers of fp32 a lane leave no registers for another row)
+  u32x4 rh[NP], ry[NP], rd[NP], next_h[NP], next_y[NP];
+  auto ask = [&](u32x4(&to)[NP], const void* matrix, int64_t ld, int64_t row) {
+    const T* p = static_cast<const T*>(matrix) + row * ld;
 #pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        const int c = (lane + i * LANES) * E;
-        rh[i] = ry[i] = u32x4{0, 0, 0, 0};
-        if (c < a.width) {
-          rh[i] = load16<T, END>(h + c, a.width - c);
-          ry[i] = load16<T, END>(dy + c, a.width - c);
-        }
-      }
-    });
+    for (int i = 0; i < NP; ++i) to[i] = ask_piece(p, (lane + i * LANES) * E, a.width, end);
+  };
+#pragma unroll
+  for (int i = 0; i < NP; ++i) rd[i] = u32x4{0, 0, 0, 0};
+  const int64_t step = (int64_t)gridDim.x * PER;
+  int64_t row = (int64_t)blockIdx.x * PER + (int)threadIdx.x / LANES;
+  if (AHEAD && row < a.rows) {
+    ask(next_h, a.h, a.ld_h, row);
+    ask(next_y, a.dy, a.ld_dy, row);
+  }
+  for (; row < a.rows; row += step) {
+    if (!AHEAD) {
+      ask(next_h, a.h, a.ld_h, row);
+      ask(next_y, a.dy, a.ld_dy, row);
+    }
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int c = (lane + i * LANES) * E;
+      rh[i] = settle<T>(next_h[i], c, a.width, end);
+      ry[i] = settle<T>(next_y[i], c, a.width, end);
+    }
+    if (a.dh) ask(rd, a.dh, a.ld_dh, row);
+    if (AHEAD && row + step < a.rows) {
+      ask(next_h, a.h, a.ld_h, row + step);
+      ask(next_y, a.dy, a.ld_dy, row + step);
+    }
     double squares = 0.0, dots = 0.0;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
+      if ((lane + i * LANES) * E >= a.width) continue;        // (a wave without the piece is past it at once)
       float hv[E], yv[E], gv[E];
       unpack<T>(rh[i], hv);
       unpack<T>(ry[i], yv);
@@ -367,33 +421,25 @@ __global__ __launch_bounds__(block_of(LANES)) void grad_kernel(NormGradArgs a, f
         dots = fma((double)(yv[j] * gv[j]), (double)hv[j], dots);
       }
     }
-    __builtin_amdgcn_sched_barrier(0);                        // (dh is asked for when the sums' registers are free, and arrives while they go across)
-    by_end(end, [&](auto e) {
-      constexpr RowEnd END = decltype(e)::value;
-#pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        const int c = (lane + i * LANES) * E;
-        rd[i] = dh && c < a.width ? load16<T, END>(dh + c, a.width - c) : u32x4{0, 0, 0, 0};
-      }
-    });
     squares = sum_across<LANES>(squares, sums[0]);
     dots = sum_across<LANES>(dots, sums[1]);
     const Back b = back_of(squares, dots, a.width, a.eps);
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int c = (lane + i * LANES) * E;
+      if (c >= a.width) continue;
       float hv[E], yv[E], gv[E], dv[E];
       unpack<T>(rh[i], hv);
       unpack<T>(ry[i], yv);
       unpack<T>(rg[i], gv);
-      unpack<T>(rd[i], dv);
+      unpack<T>(settle<T>(rd[i], c, a.width, end), dv);
 #pragma unroll
       for (int j = 0; j < E; ++j) {
         const float unit = hv[j] * b.r;
         acc[i][j] = fmaf(yv[j], unit, acc[i][j]);
         dv[j] = fmaf(b.r, fmaf(-unit, b.back, yv[j] * gv[j]), dv[j]);
       }
-      if (a.dx && c < a.width) store_piece(static_cast<T*>(a.dx) + row * a.ld_dx, c, a.width, dv);
+      if (a.dx) store_piece(static_cast<T*>(a.dx) + row * a.ld_dx, c, a.width, dv);
     }
     if constexpr (LANES > 64) __syncthreads();
   }
@@ -521,11 +567,15 @@ GradPlan grad_plan(const NormGradArgs& a) {
   GradPlan p{};
   by_width<T, true>(
       a.width,
-      [&](auto lanes, auto) {
+      [&](auto lanes, auto pieces) {
         constexpr int L = decltype(lanes)::value;
         p.blocks = blocks_for(a.rows, L);
-        // two workgroups a CU, or a large one: each has its partial sums (16,384 x 4,096 in bf16: 512 workgroups 102 us, 768 107, 1,024 122, 256 136)
-        if (a.dgain) p.blocks = p.blocks < (L <= 256 ? 512 : 256) ? p.blocks : (L <= 256 ? 512 : 256);
+        // As many workgroups as the CUs hold at once, each of which has its partial sums (16 numbers a lane in fp32, 32, and full rows of 256 lanes: two a CU;
+        // us, bf16: 51,480 x 777 with 512 workgroups 80, 768 72, 1,024 92; 78,125 x 512 72, 64, 65; 9,765 x 4,096 65, 68, 80)
+        constexpr int NUMBERS = decltype(pieces)::value * kE<T>;
+        const bool two = NUMBERS > 16 || (NUMBERS == 16 && (sizeof(T) == 4 || (L == 256 && a.width * 4 >= L * NUMBERS * 3)));
+        const int64_t most = L > 256 ? 256 : two ? 512 : NUMBERS == 16 ? 768 : 1024;
+        if (a.dgain && p.blocks > most) p.blocks = most;
         p.parts = (int)p.blocks;
         return hipSuccess;
       },
