@@ -51,12 +51,15 @@ __device__ inline u32x4 settle(const u32x4& v, int c, int width, RowEnd end) {
   return v;
 }
 
+// the low bytes of four numbers
+__device__ inline uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __builtin_amdgcn_perm(b, a, 0x0C0C0400u) | __builtin_amdgcn_perm(d, c, 0x04000C0Cu);
+}
 template <int E>
-__device__ inline void store_bytes(int8_t* row, int c, int width, const int (&q)[E]) {
+__device__ inline void store_bytes(int8_t* row, int c, int width, const uint32_t (&q)[E]) {
   uint32_t w[E / 4];
 #pragma unroll
-  for (int i = 0; i < E / 4; ++i)
-    w[i] = (q[4 * i] & 255) | (q[4 * i + 1] & 255) << 8 | (q[4 * i + 2] & 255) << 16 | (uint32_t)q[4 * i + 3] << 24;
+  for (int i = 0; i < E / 4; ++i) w[i] = low_bytes(q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]);
   if (c + E <= width) {
     if constexpr (E == 4) *reinterpret_cast<u32_any*>(row + c) = w[0];
     else *reinterpret_cast<u32x2_any*>(row + c) = u32x2_any{w[0], w[1]};
@@ -70,17 +73,18 @@ __device__ inline void store_bytes(int8_t* row, int c, int width, const int (&q)
 // y 127 / top to the nearest whole number, halves to the even one; up = 127 / top in 64 bits.  The product is off by 2^-45 at most.  A quotient of
 // numbers of 24 bits that is no half is 2^-34 or more away from one, so rounding it to multiples of 2^-40 first makes halves exact and
 // moves nothing across one: q is the definition's number for every y and top.
-__device__ inline int to_eight(float y, double up) {
+// The number is the low byte.  up = 0 in rows with an infinity or a NaN: all their numbers are 0, a NaN's low byte being 0 too (fp32 has 23 bits of its payload,
+// the high ones in fp64).
+__device__ inline uint32_t to_eight(float y, double up) {
   constexpr double kSnap = 6144.0, kWhole52 = 6755399441055744.0;        // 1.5 x 2^12, 1.5 x 2^52
   const double t = ((double)y * up + kSnap) - kSnap;
-  return (int)(uint32_t)__builtin_bit_cast(uint64_t, t + kWhole52);
+  return (uint32_t)__builtin_bit_cast(uint64_t, t + kWhole52);
 }
 // of the bits of a row's largest magnitude; a row with an infinity or a NaN has scale NaN and zeros, so that what is computed from it shows them
 __device__ inline float scale_of(uint32_t top) { return top >= 0x7F800000u ? __builtin_nanf("") : (float)((double)__builtin_bit_cast(float, top) / 127.0); }
 __device__ inline double up_of(uint32_t top) {
   return top == 0u || top >= 0x7F800000u ? 0.0 : 127.0 / (double)__builtin_bit_cast(float, top);
 }
-__device__ inline int to_eight(float y, double up, uint32_t top) { return top >= 0x7F800000u ? 0 : to_eight(y, up); }
 __device__ inline uint32_t magnitude(float y) { return __builtin_bit_cast(uint32_t, y) & 0x7FFFFFFFu; }
 
 __device__ inline float inverse_root(double sum, int width, double eps) {
@@ -212,7 +216,7 @@ __global__ __launch_bounds__(block_of(LANES)) void rows_kernel(NormArgs a) {
 #pragma unroll
       for (int i = 0; i < NP; ++i)
 #pragma unroll
-        for (int j = 0; j < E; ++j) top = max(top, (lane + i * LANES) * E + j < a.width ? magnitude(v[i][j]) : 0u);
+        for (int j = 0; j < E; ++j) top = max(top, magnitude(v[i][j]));          // (past the row: zeros)
       top = top_across<LANES>(top, tops);
       const double up = up_of(top);
       if (lane == 0) a.scale[row] = scale_of(top);
@@ -220,9 +224,9 @@ __global__ __launch_bounds__(block_of(LANES)) void rows_kernel(NormArgs a) {
       for (int i = 0; i < NP; ++i) {
         const int c = (lane + i * LANES) * E;
         if (c >= a.width) continue;
-        int q[E];
+        uint32_t q[E];
 #pragma unroll
-        for (int j = 0; j < E; ++j) q[j] = to_eight(v[i][j], up, top);
+        for (int j = 0; j < E; ++j) q[j] = to_eight(v[i][j], up);
         store_bytes<E>(a.q + row * a.ld_q, c, a.width, q);
       }
     }
@@ -284,9 +288,9 @@ __global__ __launch_bounds__(1024) void long_rows_kernel(NormArgs a) {
       norm(c, v);
       if (KIND != kRows8 && (KIND == kNorm || a.y)) store_piece(static_cast<T*>(a.y) + row * a.ld_y, c, a.width, v);
       if constexpr (KIND != kNorm) {
-        int q[E];
+        uint32_t q[E];
 #pragma unroll
-        for (int j = 0; j < E; ++j) q[j] = to_eight(v[j], up, top);
+        for (int j = 0; j < E; ++j) q[j] = to_eight(v[j], up);
         store_bytes<E>(a.q + row * a.ld_q, c, a.width, q);
       }
     });
@@ -696,12 +700,9 @@ __global__ __launch_bounds__(256) void columns_kernel(ColumnsArgs a, const uint3
     for (int u = 0; u < 4; ++u) unpack<T>(raw[i][u], v[u]);
 #pragma unroll
     for (int j = 0; j < E; ++j) {
-      const uint32_t t = top[piece * E + j];
-      const double by = up_of(t);
-      uint32_t w = 0;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) w |= (uint32_t)(to_eight(v[u][j], by, t) & 255) << 8 * u;
-      *reinterpret_cast<uint32_t*>(tile + (piece * E + j) * STRIDE + quad * 4) = w;
+      const double by = up_of(top[piece * E + j]);
+      *reinterpret_cast<uint32_t*>(tile + (piece * E + j) * STRIDE + quad * 4) =
+          low_bytes(to_eight(v[0][j], by), to_eight(v[1][j], by), to_eight(v[2][j], by), to_eight(v[3][j], by));
     }
   }
   __syncthreads();

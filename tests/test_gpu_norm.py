@@ -165,6 +165,16 @@ def test_rows_of_zeros_infinities_and_nan(width, dt):
     assert y[3].isnan().all() and y[2, 7].isnan() and y[4, 0].isnan()
 
 
+@pytest.mark.parametrize("bits", [0x7F800001, 0x7FBFFFFF, 0x7FFFFFFF, -0x3FFFF9, -1, 0x7F800000, -0x800000], ids=hex)
+def test_every_kind_of_nan_gives_zeros(bits):
+    """NaN of any payload, quiet and signalling, and the infinities: the row's or column's numbers are zeros, its scale NaN."""
+    x = torch.ones(3, 300)
+    x.view(torch.int32)[1, 37] = bits
+    assert not x[1, 37].isfinite()
+    for q, scale in (binding.quantize(x.cuda()), binding.rms_norm_i8(x.cuda(), torch.ones(300, device="cuda")), binding.quantize(x.t().contiguous().cuda(), columns=True)):
+        assert not q[1].any() and scale[1].isnan() and (q[[0, 2]] == 127).all()
+
+
 def test_large_and_small_numbers():
     """Squares that fp32 could not hold."""
     _, h, gain, dy, _ = make(4, 300, torch.float32)
