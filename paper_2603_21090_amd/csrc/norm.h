@@ -37,7 +37,7 @@ __device__ inline u32x4 load_own(const T* row, int c, int width) {
 }
 
 // The piece at column c as it is asked for, and as it is used: a row that ends with a part of a piece is read from its last 16 bytes, which are moved down when they
-// are used (behind the load, the move would wait for it: 20,000 x 2,100 in bf16 181 us of gradient, TODO so)
+// are used (behind the load, the move would wait for it: 20,000 x 2,100 in bf16 181 us of gradient, 81 so)
 template <class T>
 __device__ inline u32x4 ask_piece(const T* row, int c, int width, RowEnd end) {
   if (c >= width) return u32x4{0, 0, 0, 0};
@@ -55,6 +55,14 @@ __device__ inline u32x4 settle(const u32x4& v, int c, int width, RowEnd end) {
 __device__ inline uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   return __builtin_amdgcn_perm(b, a, 0x0C0C0400u) | __builtin_amdgcn_perm(d, c, 0x04000C0Cu);
 }
+// Whether none of the wave's lanes has piece i of its row (of 16 lanes a row, every wave has every piece)
+template <int LANES, int E>
+__device__ inline bool without(int i, int width) {
+  if (LANES < 64) return false;
+  const int first = LANES > 64 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x & (LANES - 1)) : 0;
+  return (first + i * LANES) * E >= width;
+}
+
 template <int E>
 __device__ inline void store_bytes(int8_t* row, int c, int width, const uint32_t (&q)[E]) {
   uint32_t w[E / 4];
@@ -147,7 +155,7 @@ enum Kind { kNorm, kNorm8, kRows8 };                          // y; 8 bits of y 
 // Rows whose pieces stay in registers.  All of a row is read before any of it is written: outputs may lie where the inputs do.  A workgroup walks down the rows: the
 // gain is read once, and the next row is on its way while one is summed and written (in bf16 16,384 x 4,096 57 -> 50 us, 30,000 x 2,000 57 -> 47).
 template <class T, int LANES, int NP, Kind KIND>
-__global__ __launch_bounds__(block_of(LANES)) void rows_kernel(NormArgs a) {
+__global__ __launch_bounds__(block_of(LANES), LANES == 512 ? 4 : 1) void rows_kernel(NormArgs a) {
   constexpr int E = kE<T>, PER = block_of(LANES) / LANES;
   __shared__ double sums[LANES > 64 ? LANES / 64 : 1];
   __shared__ uint32_t tops[LANES > 64 ? LANES / 64 : 1];
@@ -194,7 +202,7 @@ __global__ __launch_bounds__(block_of(LANES)) void rows_kernel(NormArgs a) {
       double sum = 0.0;
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
-        if ((lane + i * LANES) * E >= a.width) continue;      // (a wave without the piece is past it at once)
+        if (without<LANES, E>(i, a.width)) continue;
 #pragma unroll
         for (int j = 0; j < E; ++j) sum = fma((double)v[i][j], (double)v[i][j], sum);
       }
@@ -414,7 +422,7 @@ __global__ __launch_bounds__(block_of(LANES)) void grad_kernel(NormGradArgs a, f
     double squares = 0.0, dots = 0.0;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      if ((lane + i * LANES) * E >= a.width) continue;        // (a wave without the piece is past it at once)
+      if (without<LANES, E>(i, a.width)) continue;
       float hv[E], yv[E], gv[E];
       unpack<T>(rh[i], hv);
       unpack<T>(ry[i], yv);
@@ -431,7 +439,7 @@ __global__ __launch_bounds__(block_of(LANES)) void grad_kernel(NormGradArgs a, f
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int c = (lane + i * LANES) * E;
-      if (c >= a.width) continue;
+      if (without<LANES, E>(i, a.width)) continue;
       float hv[E], yv[E], gv[E], dv[E];
       unpack<T>(rh[i], hv);
       unpack<T>(ry[i], yv);
@@ -443,7 +451,7 @@ __global__ __launch_bounds__(block_of(LANES)) void grad_kernel(NormGradArgs a, f
         acc[i][j] = fmaf(yv[j], unit, acc[i][j]);
         dv[j] = fmaf(b.r, fmaf(-unit, b.back, yv[j] * gv[j]), dv[j]);
       }
-      if (a.dx) store_piece(static_cast<T*>(a.dx) + row * a.ld_dx, c, a.width, dv);
+      if (a.dx && c < a.width) store_piece(static_cast<T*>(a.dx) + row * a.ld_dx, c, a.width, dv);
     }
     if constexpr (LANES > 64) __syncthreads();
   }
@@ -574,10 +582,10 @@ GradPlan grad_plan(const NormGradArgs& a) {
       [&](auto lanes, auto pieces) {
         constexpr int L = decltype(lanes)::value;
         p.blocks = blocks_for(a.rows, L);
-        // As many workgroups as the CUs hold at once, each of which has its partial sums (16 numbers a lane in fp32, 32, and full rows of 256 lanes: two a CU;
+        // As many workgroups as the CUs hold at once, each of which has its partial sums (16 numbers a lane in fp32, 32, rows of 16 lanes and full ones of 256: two a CU;
         // us, bf16: 51,480 x 777 with 512 workgroups 80, 768 72, 1,024 92; 78,125 x 512 72, 64, 65; 9,765 x 4,096 65, 68, 80)
         constexpr int NUMBERS = decltype(pieces)::value * kE<T>;
-        const bool two = NUMBERS > 16 || (NUMBERS == 16 && (sizeof(T) == 4 || (L == 256 && a.width * 4 >= L * NUMBERS * 3)));
+        const bool two = NUMBERS > 16 || (NUMBERS == 16 && (sizeof(T) == 4 || L == 16 || (L == 256 && a.width * 4 >= L * NUMBERS * 3)));
         const int64_t most = L > 256 ? 256 : two ? 512 : NUMBERS == 16 ? 768 : 1024;
         if (a.dgain && p.blocks > most) p.blocks = most;
         p.parts = (int)p.blocks;
