@@ -29,7 +29,28 @@ __device__ inline Words philox(uint64_t group, uint32_t site, uint64_t seed, uin
   return {{a, b, c, d}};
 }
 
-// eight neighbouring numbers a thread; a row's last ones are read by themselves, as y may lie where x or the residual does
+// eight neighbouring numbers of a row from column c on, those that it has; nothing beside them is touched, as y may lie where x or the residual does
+template <class T>
+__device__ inline void load8(const T* row, int c, int width, floatx4& u, floatx4& v) {
+  if constexpr (sizeof(T) == 2) {
+    u = v = floatx4{0.f, 0.f, 0.f, 0.f};
+    add8(row, c, width, u, v);
+  } else {
+    u = load4(row, c, width);
+    v = c + 4 < width ? load4(row, c + 4, width) : floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+}
+template <class T>
+__device__ inline void save8(T* row, int c, int width, const floatx4& u, const floatx4& v) {
+  if constexpr (sizeof(T) == 2) {
+    store8(row, c, width, u, v);
+  } else {
+    store4(row, c, width, u);
+    if (c + 4 < width) store4(row, c + 4, width, v);
+  }
+}
+
+// a group a thread, the generator while the group is on its way
 template <class T>
 __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a) {
   const uint64_t seed = a.rng[0], step = a.rng[1];
@@ -39,24 +60,21 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a) {
   for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (uint64_t)gridDim.x * 256) {
     const int64_t row = small ? (uint32_t)i / groups : i / groups;
     const int c = (int)(uint32_t)(i - row * groups) * 8;
+    floatx4 u, v, s = {0.f, 0.f, 0.f, 0.f}, t = s;
+    load8(static_cast<const T*>(a.x) + row * a.ld_x, c, a.width, u, v);
+    if (a.residual) load8(static_cast<const T*>(a.residual) + row * a.ld_res, c, a.width, s, t);
+    __builtin_amdgcn_sched_barrier(0);
     const Words r = philox(i, a.site, seed, step);
-    floatx4 u = {0.f, 0.f, 0.f, 0.f}, v = u;
-    const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
-    u = load4(x, c, a.width);
-    if (c + 4 < a.width) v = load4(x, c + 4, a.width);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       u[j] = (r.w[j / 2] >> j % 2 * 16 & 0xFFFFu) >= a.border ? u[j] * a.scale : 0.f;
       v[j] = (r.w[2 + j / 2] >> j % 2 * 16 & 0xFFFFu) >= a.border ? v[j] * a.scale : 0.f;
     }
     if (a.residual) {
-      const T* res = static_cast<const T*>(a.residual) + row * a.ld_res;
-      u += load4(res, c, a.width);
-      if (c + 4 < a.width) v += load4(res, c + 4, a.width);
+      u += s;
+      v += t;
     }
-    T* y = static_cast<T*>(a.y) + row * a.ld_y;
-    store4(y, c, a.width, u);
-    if (c + 4 < a.width) store4(y, c + 4, a.width, v);
+    save8(static_cast<T*>(a.y) + row * a.ld_y, c, a.width, u, v);
   }
 }
 
