@@ -372,7 +372,8 @@ int stgn_attention_grad(const stgn_attention_args *args, void *device_workspace,
  * y = h r gain from the h of 32 bits; h is handed out where its pointer is not NULL (the residual stream; what the gradient reads).
  * With q, y is written in 8 bits too (or instead: y may be NULL then): scale[row] = max |y| / 127, q = y 127 / max |y| to the nearest whole
  * number, halves to the even one, y being the fp32 value h r gain.  A row of zeros has scale 0; a row of whose y one is infinite or no number has scale NaN and
- * zeros in q.  The sum of squares and r are computed in fp64, r is rounded to fp32: q depends on the inputs alone.
+ * zeros in q.  The sum of squares and r are computed in fp64, r is rounded to fp32 (3.4e38 at most: with eps = 0 a row of zeros stays zeros, and has no finite
+ * gradient): q depends on the inputs alone.
  * Gradient, from dy and h: dx = r gain dy - h r^3 mean(gain dy h) + dh, which is the gradient of x and of the residual; dgain = column sums of dy h r.  dh (what comes
  * down the residual stream) may be NULL; a gradient whose pointer is NULL is not computed.
  * x, residual, h, y, dy, dh: [rows x width]; rows lie ld_* elements apart, the numbers of a row side by side; q: int8 [rows x width], scale: fp32 [rows];
@@ -411,7 +412,8 @@ int stgn_quantize_workspace(const stgn_quantize_args *args, size_t *bytes);
 int stgn_quantize(const stgn_quantize_args *args, void *device_workspace, size_t device_bytes, void *hip_stream);
 
 /* Dense product of operands in 8 bits: y = act(x_scale[row] w_scale[column] sum_k x[row][k] w[column][k] + bias) + residual.  The sums are exact 32-bit integers, all
- * that follows is fp32; dtype is the type of bias, residual and y.
+ * that follows is fp32, the sum times x_scale first (infinite from x_scale = 1.6e29 on, where the sum is large, whatever w_scale is); dtype is the type of bias,
+ * residual and y.
  * x: int8 [rows x d_in], w: int8 [d_out x d_in] (k along both operands' rows), ld_x and ld_w bytes apart; x_scale, w_scale: fp32 [rows], [d_out];
  * bias: [d_out]; residual, y: [rows x d_out], ld_* elements apart.  bias and residual may be NULL.  rows may be 0, d_in lies in 1 .. 131,071 (sums of products of -128 stay
  * 32-bit numbers), d_out in 1 .. 2^24.  y overlaps nothing, except that it may be exactly the residual; residual and y of equal ld_* may be different columns of one

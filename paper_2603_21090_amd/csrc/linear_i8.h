@@ -628,6 +628,7 @@ inline Plan plan_of(int64_t m, int64_t n, int64_t k, bool whole) {
 }
 
 inline size_t part_bytes(const Linear8Args& f) {
+  if (f.rows == 0) return 0;                                  // (a plan has a tile at least)
   // (the pointers' alignment is not known where the workspace is asked for: enough for either)
   const Plan p = plan_of(f.rows, f.d_out, f.d_in, true), q = plan_of(f.rows, f.d_out, f.d_in, false);
   const int splits = p.splits > q.splits ? p.splits : q.splits;

@@ -98,6 +98,26 @@ def test_dropout_refuses(lib, bad):
     assert lib.stgn_last_error(None)
 
 
+@pytest.mark.parametrize("wide", [1, 20, 2048, 2049, 4096, 40001, 131071])
+def test_no_rows(lib, wide):
+    """Nothing is enqueued for a product, a norm or dropout of no rows, at any width."""
+    n = C.c_size_t(7)
+    args = product_args(rows=0, d_in=wide, ld_x=wide, ld_w=wide, d_out=wide, ld_y=wide, ld_residual=wide)
+    assert lib.stgn_linear_quantized_workspace(C.byref(args), C.byref(n)) == 0 and n.value == 0
+    assert lib.stgn_linear_quantized(C.byref(args), None, 0, None) == 0
+    args = norm_args(rows=0, width=wide, **{f"ld_{m}": wide for m in ("x", "residual", "h", "y", "q", "dy", "dh")})
+    assert lib.stgn_rms_norm_workspace(C.byref(args), C.byref(n), C.byref(n)) == 0
+    assert lib.stgn_rms_norm(C.byref(args), None, 0, None) == 0
+    args.dx = args.dgain = None
+    assert lib.stgn_rms_norm_grad(C.byref(args), 1 << 30, n.value, None) == 0
+    for columns in (0, 1):
+        args = quantize_args(rows=0, columns=columns, width=wide, ld_x=wide, ld_q=wide)
+        assert lib.stgn_quantize_workspace(C.byref(args), C.byref(n)) == 0 and (n.value > 0) == (columns == 1)
+    args = quantize_args(rows=0, width=wide, ld_x=wide, ld_q=wide)
+    assert lib.stgn_quantize(C.byref(args), None, 0, None) == 0
+    assert lib.stgn_dropout(C.byref(dropout_args(rows=0, width=wide, ld_x=wide, ld_y=wide, ld_residual=wide)), None) == 0
+
+
 def test_null_arguments_and_workspaces(lib):
     n, m = C.c_size_t(0), C.c_size_t(1)
     assert lib.stgn_dropout(None, None) == INVALID
