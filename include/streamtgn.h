@@ -417,7 +417,8 @@ int stgn_quantize(const stgn_quantize_args *args, void *device_workspace, size_t
  * x: int8 [rows x d_in], w: int8 [d_out x d_in] (k along both operands' rows), ld_x and ld_w bytes apart; x_scale, w_scale: fp32 [rows], [d_out];
  * bias: [d_out]; residual, y: [rows x d_out], ld_* elements apart.  bias and residual may be NULL.  rows may be 0, d_in lies in 1 .. 131,071 (sums of products of -128 stay
  * 32-bit numbers), d_out in 1 .. 2^24.  y overlaps nothing, except that it may be exactly the residual; residual and y of equal ld_* may be different columns of one
- * matrix. */
+ * matrix.  Large products take least time where x and w start at a multiple of 16 bytes and d_in, ld_x and ld_w are multiples of 64: others are laid out again in the
+ * workspace, or take a slower kernel. */
 typedef struct {
   uint32_t dtype, activation;
   uint32_t rows, d_in, d_out;

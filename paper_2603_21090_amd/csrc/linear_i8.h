@@ -7,8 +7,8 @@
 //   fragments  operands go from memory into the matrix instructions without LDS, eight waves share k and add up at the end: for few rows or small outputs,
 //              where what counts is one latency instead of one for each tile of k
 //   64 x 64    tiles through registers into LDS, any alignment, k split where tiles are few
-//   128 x 128  the same, and as a variant whose tiles go from memory into LDS directly, for operands in whole pieces of 16 bytes
-//   in turns   256 x 256 and 128 x 128, directly too: two groups of four waves, one multiplying while the other reads
+//   128 x 128  tiles from memory into LDS directly, for operands in whole pieces of 16 bytes, or laid out so first
+//   256 x 256  directly too, in turns: two groups of four waves, one multiplying while the other reads
 #pragma once
 #include <utility>
 
@@ -51,15 +51,43 @@ __device__ inline void activate(int act, floatx4& v) {
   }
 }
 
-// scales, bias, activation, residual: four neighbouring outputs of row m
+// Four neighbouring numbers of a row as they lie in memory, those that it has
 template <class T>
-__device__ inline void finish4(const Product& a, int64_t m, int n, const i32x4& sum) {
-  floatx4 v = scaled(sum, a.r_scale[m], load4(a.l_scale, n, a.n));
-  if (a.bias) v += load4(static_cast<const T*>(a.bias), n, a.n);
-  activate<T>(a.act, v);
-  if (a.residual) v += load4(static_cast<const T*>(a.residual) + m * a.ld_res, n, a.n);
-  store4(static_cast<T*>(a.out) + m * a.ld_out, n, a.n, v);
+__device__ inline typename Elem<T>::Four ask4(const T* row, int n, int cols) {
+  using Bits = std::conditional_t<sizeof(T) == 4, u32x4_any, u32x2_any>;
+  if (n + 4 <= cols) return __builtin_bit_cast(typename Elem<T>::Four, *reinterpret_cast<const Bits*>(row + n));
+  typename Elem<T>::Four f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) f[j] = n + j < cols ? row[n + j] : (T)0.f;
+  return f;
 }
+// What four neighbouring outputs of row m take beside their sums: scales, bias, activation, residual.  Asked for in front of the sums, so that their latency and
+// that of the operands are one.
+template <class T>
+struct Ends {
+  typename Elem<T>::Four bias, residual;
+  floatx4 ls;
+  float rs;
+  __device__ inline void ask(const Product& a, int64_t m, int n) {
+    rs = a.r_scale[m];
+    ls = __builtin_bit_cast(floatx4, ask4(a.l_scale, n, a.n));
+    if (a.bias) bias = ask4(static_cast<const T*>(a.bias), n, a.n);
+    if (a.residual) residual = ask4(static_cast<const T*>(a.residual) + m * a.ld_res, n, a.n);
+  }
+  __device__ inline void finish(const Product& a, int64_t m, int n, const i32x4& sum) const {
+    floatx4 v = scaled(sum, rs, ls);
+    if (a.bias) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] += (float)bias[j];
+    }
+    activate<T>(a.act, v);
+    if (a.residual) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] += (float)residual[j];
+    }
+    store4(static_cast<T*>(a.out) + m * a.ld_out, n, a.n, v);
+  }
+};
 
 __device__ inline void store_sums(int* row, int n, int cols, const i32x4& v) {
   if (n + 4 <= cols) {
@@ -140,7 +168,23 @@ __global__ __launch_bounds__(512) void fragments_kernel(Product a) {
       }
     }
   };
-  constexpr int STEP = WAVES * kBK;
+  constexpr int STEP = WAVES * kBK, MINE = (MB * NB + WAVES - 1) / WAVES;
+  Ends<T> ends[MINE];                                         // of this wave's blocks of the joined sums
+  auto place = [&](int i, int& m, int& n) {
+    const int b = wave + i * WAVES;
+    m = m0 + b % MB * 16 + i16;
+    n = n0 + b / MB * 16 + 4 * g;
+    return b < MB * NB && m < a.m && n < a.n;
+  };
+  auto ask = [&] {
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) {
+      int m, n;
+      if (place(i, m, n)) ends[i].ask(a, m, n);
+    }
+  };
+  constexpr bool EARLY = (MB + NB) * DEPTH < 24;              // (registers)
+  if (EARLY) ask();
 #pragma unroll
   for (int d = 0; d < DEPTH; ++d)
     if (wave * kBK + d * STEP < a.k) fetch(d, wave * kBK + d * STEP);
@@ -158,30 +202,34 @@ __global__ __launch_bounds__(512) void fragments_kernel(Product a) {
       if (k + DEPTH * STEP < a.k) fetch(d, k + DEPTH * STEP);
     }
   }
+  if (!EARLY) ask();
 #pragma unroll
   for (int x = 0; x < NB; ++x)
 #pragma unroll
     for (int y = 0; y < MB; ++y) part[wave][x * MB + y][lane] = acc[x][y];
   __syncthreads();
-  for (int b = wave; b < MB * NB; b += WAVES) {
+#pragma unroll
+  for (int i = 0; i < MINE; ++i) {
+    const int b = wave + i * WAVES;
+    int m, n;
+    if (!place(i, m, n)) continue;
     i32x4 sum = part[0][b][lane];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) sum += part[w][b][lane];
-    const int m = m0 + b % MB * 16 + i16, n = n0 + b / MB * 16 + 4 * g;
-    if (m < a.m && n < a.n) finish4<T>(a, m, n, sum);
+    ends[i].finish(a, m, n, sum);
   }
 }
 
 // ---- tiles through registers
 
-// DEPTH tiles of k are on their way in registers while one is multiplied; with one, two are in LDS and a barrier a tile is enough (as in the kernel of
-// other types: where tiles are small and few, what a tile takes is the wait for memory).
-template <class T, int BM, int BN, int WM, int WN, int DEPTH>
-__global__ __launch_bounds__(WM * WN * 64, BM * BN <= 64 * 64 ? 4 : 2) void product_kernel(Product a) {
+// 64 x 64 outputs a workgroup of four waves, any alignment.  Three tiles of k are on their way in registers while one is multiplied: where tiles are small and
+// few, what a tile takes is the wait for memory.
+template <class T>
+__global__ __launch_bounds__(256, 4) void product_kernel(Product a) {
   using El = Elem<int8_t>;
-  constexpr int THREADS = WM * WN * 64, MB = BM / WM / 16, NB = BN / WN / 16, S = lds_stride<int8_t>(kBK), BUFS = DEPTH == 1 ? 2 : 1;
-  __shared__ __attribute__((aligned(16))) int8_t ls[BUFS][BN * S], rs[BUFS][BM * S];
-  const int wave = threadIdx.x >> 6, wm = wave % WM * MB * 16, wn = wave / WM * NB * 16;
+  constexpr int BM = 64, BN = 64, THREADS = 256, MB = 2, NB = 2, DEPTH = 3, S = lds_stride<int8_t>(kBK);
+  __shared__ __attribute__((aligned(16))) int8_t ls[BN * S], rs[BM * S];
+  const int wave = threadIdx.x >> 6, wm = wave % 2 * MB * 16, wn = wave / 2 * NB * 16;
   const unsigned tm = (unsigned)(a.m + BM - 1) / BM, tn = (unsigned)(a.n + BN - 1) / BN;
   const int split = (int)(blockIdx.x / (tm * tn));
   int row, col;
@@ -205,68 +253,59 @@ __global__ __launch_bounds__(WM * WN * 64, BM * BN <= 64 * 64 ? 4 : 2) void prod
     ml.fetch(rl[d], k);
     mr.fetch(rr[d], k);
   };
-  auto multiply = [&](const int8_t* l, const int8_t* r) {
+  auto multiply = [&] {
 #pragma unroll
     for (int s = 0; s < kBK; s += El::KF) {
       i32x4 lf[NB], rf[MB];
 #pragma unroll
-      for (int x = 0; x < NB; ++x) lf[x] = frag_rows(l, S, wn + x * 16, s);
+      for (int x = 0; x < NB; ++x) lf[x] = frag_rows(ls, S, wn + x * 16, s);
 #pragma unroll
-      for (int y = 0; y < MB; ++y) rf[y] = frag_rows(r, S, wm + y * 16, s);
+      for (int y = 0; y < MB; ++y) rf[y] = frag_rows(rs, S, wm + y * 16, s);
 #pragma unroll
       for (int x = 0; x < NB; ++x)
 #pragma unroll
         for (int y = 0; y < MB; ++y) acc[x][y] = El::mma(lf[x], rf[y], acc[x][y]);
     }
   };
-  if constexpr (DEPTH == 1) {
-    if (kb < ke) {
-      fetch(0, kb);
-      ml.store(ls[0], rl[0]);
-      mr.store(rs[0], rr[0]);
-    }
-    int buf = 0;
-    for (int k = kb; k < ke; k += kBK, buf ^= 1) {
+#pragma unroll
+  for (int d = 0; d < DEPTH; ++d)
+    if (kb + d * kBK < ke) fetch(d, kb + d * kBK);
+  for (int kt = kb; kt < ke; kt += DEPTH * kBK) {
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {
+      const int k = kt + d * kBK;
+      if (k >= ke) break;
       __syncthreads();
-      const bool more = k + kBK < ke;
-      if (more) fetch(0, k + kBK);
-      multiply(ls[buf], rs[buf]);
-      if (more) {
-        ml.store(ls[buf ^ 1], rl[0]);
-        mr.store(rs[buf ^ 1], rr[0]);
-      }
-    }
-  } else {
-#pragma unroll
-    for (int d = 0; d < DEPTH; ++d)
-      if (kb + d * kBK < ke) fetch(d, kb + d * kBK);
-    for (int kt = kb; kt < ke; kt += DEPTH * kBK) {
-#pragma unroll
-      for (int d = 0; d < DEPTH; ++d) {
-        const int k = kt + d * kBK;
-        if (k >= ke) break;
-        __syncthreads();
-        ml.store(ls[0], rl[d]);
-        mr.store(rs[0], rr[d]);
-        __syncthreads();
-        if (k + DEPTH * kBK < ke) fetch(d, k + DEPTH * kBK);
-        multiply(ls[0], rs[0]);
-      }
+      ml.store(ls, rl[d]);
+      mr.store(rs, rr[d]);
+      __syncthreads();
+      if (k + DEPTH * kBK < ke) fetch(d, k + DEPTH * kBK);
+      multiply();
     }
   }
-  const int lane = threadIdx.x & 63, nb = n0 + wn + 4 * (lane >> 4);
+  const int lane = threadIdx.x & 63, m = m0 + wm + (lane & 15), n = n0 + wn + 4 * (lane >> 4);
+  if (a.splits > 1) {
+#pragma unroll
+    for (int y = 0; y < MB; ++y)
+#pragma unroll
+      for (int x = 0; x < NB; ++x)
+        if (m + y * 16 < a.m && n + x * 16 < a.n) store_sums(a.part + (split * (int64_t)a.m + m + y * 16) * a.n, n + x * 16, a.n, acc[x][y]);
+    return;
+  }
+  Ends<T> ends[2][NB];                                        // of sixteen rows and the next sixteen
+  auto ask = [&](int y) {
+#pragma unroll
+    for (int x = 0; x < NB; ++x)
+      if (m + y * 16 < a.m && n + x * 16 < a.n) ends[y & 1][x].ask(a, m + y * 16, n + x * 16);
+  };
+  ask(0);
 #pragma unroll
   for (int y = 0; y < MB; ++y) {
+    if (y + 1 < MB) ask(y + 1);
     __builtin_amdgcn_sched_barrier(0);
-    const int64_t m = m0 + wm + y * 16 + (lane & 15);
-    if (m >= a.m) continue;
 #pragma unroll
-    for (int x = 0; x < NB; ++x) {
-      const int n = nb + x * 16;
-      if (n >= a.n) continue;
-      if (a.splits > 1) store_sums(a.part + (split * (int64_t)a.m + m) * a.n, n, a.n, acc[x][y]);
-      else finish4<T>(a, m, n, acc[x][y]);
-    }
+    for (int x = 0; x < NB; ++x)
+      if (m + y * 16 < a.m && n + x * 16 < a.n) ends[y & 1][x].finish(a, m + y * 16, n + x * 16, acc[x][y]);
   }
 }
 
@@ -348,75 +387,119 @@ struct DirectMove {
   }
 };
 
-// Eight neighbouring outputs of row m; `residual`: theirs, where all eight are there and the type has 16 bits
+// eight neighbouring outputs as they lie in memory
 template <class T>
-__device__ inline void finish8(const Product& a, int64_t m, int n, float rs, const i32x4& s, const i32x4& t, const u32x4& residual) {
-  const bool both = n + 4 < a.n;
-  floatx4 u = scaled(s, rs, load4(a.l_scale, n, a.n)), v = {0.f, 0.f, 0.f, 0.f};
-  if (both) v = scaled(t, rs, load4(a.l_scale, n + 4, a.n));
-  auto add = [&](const T* row) {
+struct Eight {
+  u32x4 p[sizeof(T) / 2];
+  __device__ inline Eight() {}
+  __device__ inline Eight(const floatx4& u, const floatx4& v) {
     if constexpr (sizeof(T) == 2) {
-      add8(row, n, a.n, u, v);
-    } else {
-      u += load4(row, n, a.n);
-      if (both) v += load4(row, n + 4, a.n);
-    }
-  };
-  if (a.bias) add(static_cast<const T*>(a.bias));
-  activate<T>(a.act, u);
-  activate<T>(a.act, v);
-  if (a.residual) {
-    if (sizeof(T) == 2 && n + 8 <= a.n) {
-      if constexpr (sizeof(T) == 2) {
-        const typename Elem<T>::Frag f = __builtin_bit_cast(typename Elem<T>::Frag, residual);
+      typename Elem<T>::Frag f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) { u[j] += (float)f[j]; v[j] += (float)f[j + 4]; }
-      }
+      for (int j = 0; j < 4; ++j) { f[j] = (T)u[j]; f[j + 4] = (T)v[j]; }
+      p[0] = __builtin_bit_cast(u32x4, f);
     } else {
-      add(static_cast<const T*>(a.residual) + m * a.ld_res);
+      p[0] = __builtin_bit_cast(u32x4, u);
+      p[1] = __builtin_bit_cast(u32x4, v);
     }
   }
-  T* out = static_cast<T*>(a.out) + m * a.ld_out;
-  if constexpr (sizeof(T) == 2) {
-    store8(out, n, a.n, u, v);
-  } else {
-    store4(out, n, a.n, u);
-    if (both) store4(out, n + 4, a.n, v);
+  __device__ inline void load(const T* from) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) p[i] = reinterpret_cast<const u32x4_any*>(from)[i];
+  }
+  __device__ inline void store(T* to) const {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<u32x4_any*>(to)[i] = p[i];
+  }
+  __device__ inline void add(floatx4& u, floatx4& v) const {
+    if constexpr (sizeof(T) == 2) {
+      const typename Elem<T>::Frag f = __builtin_bit_cast(typename Elem<T>::Frag, p[0]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) { u[j] += (float)f[j]; v[j] += (float)f[j + 4]; }
+    } else {
+      u += __builtin_bit_cast(floatx4, p[0]);
+      v += __builtin_bit_cast(floatx4, p[1]);
+    }
+  }
+};
+
+// The epilogue of a wave's blocks from output (m0, n0), columns in pairs of blocks, for outputs of eight columns and more; of the eights that the output has
+// in part nothing is stored.  What the columns' side takes is asked for once, and the residual of sixteen rows is on its way while the sixteen rows before are
+// finished: a wait for a load is also one for the stores in front of it (eights that each waited for their own loads: 8,192 x 4,096 x 4,096 with gelu
+// and residual 174, so 157; 16,384 x 1,024 x 1,024 47 and 37).  Rows and columns past the output's are computed from its last ones.
+template <class T, int ACT, bool WHOLE, int NB, int MB>
+__device__ __forceinline__ void finish_eights(const Product& a, int m0, int n0, i32x4 (&acc)[NB][MB]) {
+  constexpr int XS = sizeof(T) == 4 && NB == 8 ? 1 : NB / 2;  // eights at a time (registers)
+  const int lane = threadIdx.x & 63, m = m0 + (lane & 15), first = n0 + 8 * (lane >> 4);
+#pragma unroll
+  for (int x0 = 0; x0 < NB / 2; x0 += XS) {
+    Eight<T> res[2][XS], bias[XS];
+    floatx4 ls[XS][2];
+    float rs[MB];
+    auto column = [&](int x) { return WHOLE ? first + (x0 + x) * 32 : min(first + (x0 + x) * 32, a.n - 8); };
+    auto row = [&](int y) { return (int64_t)(WHOLE ? m + y * 16 : min(m + y * 16, a.m - 1)); };
+    auto ask = [&](int y) {
+#pragma unroll
+      for (int x = 0; x < XS; ++x) res[y & 1][x].load(static_cast<const T*>(a.residual) + row(y) * a.ld_res + column(x));
+    };
+    if (a.residual) ask(0);
+#pragma unroll
+    for (int x = 0; x < XS; ++x) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) ls[x][h] = __builtin_bit_cast(floatx4, *reinterpret_cast<const u32x4_any*>(a.l_scale + column(x) + h * 4));
+      if (a.bias) bias[x].load(static_cast<const T*>(a.bias) + column(x));
+    }
+#pragma unroll
+    for (int y = 0; y < MB; ++y) rs[y] = a.r_scale[row(y)];
+#pragma unroll
+    for (int y = 0; y < MB; ++y) {
+      if (a.residual && y + 1 < MB) ask(y + 1);
+#pragma unroll
+      for (int x = 0; x < XS; ++x) {
+        __builtin_amdgcn_sched_barrier(0);
+        floatx4 u = scaled(acc[2 * (x0 + x)][y], rs[y], ls[x][0]), v = scaled(acc[2 * (x0 + x) + 1][y], rs[y], ls[x][1]);
+        if (a.bias) bias[x].add(u, v);
+        dense::activate<T, ACT>(u);
+        dense::activate<T, ACT>(v);
+        if (a.residual) res[y & 1][x].add(u, v);
+        const int n = first + (x0 + x) * 32;
+        if (WHOLE || (m + y * 16 < a.m && n + 8 <= a.n)) Eight<T>(u, v).store(static_cast<T*>(a.out) + (m + y * 16) * a.ld_out + n);
+      }
+    }
   }
 }
 
-// A wave's blocks from output (m0, n0), columns in pairs of blocks.  The residual of sixteen rows is on its way while the sixteen rows before are finished.
+// ... of any width, or a split's sums
 template <class T, int NB, int MB>
 __device__ __forceinline__ void finish_pairs(const Product& a, int split, int m0, int n0, i32x4 (&acc)[NB][MB]) {
-  const int lane = threadIdx.x & 63, first = n0 + 8 * (lane >> 4);
-  u32x4 ahead[2][NB / 2];
-  auto ask = [&](int y) {
-    const int64_t m = m0 + y * 16 + (lane & 15);
-#pragma unroll
-    for (int x = 0; x < NB / 2; ++x) {
-      ahead[y & 1][x] = u32x4{0, 0, 0, 0};
-      if (sizeof(T) == 2 && a.residual && a.splits == 1 && m < a.m && first + x * 32 + 8 <= a.n)
-        ahead[y & 1][x] = *reinterpret_cast<const u32x4_any*>(static_cast<const T*>(a.residual) + m * a.ld_res + first + x * 32);
+  auto eights = [&](auto whole) {
+    constexpr bool WHOLE = decltype(whole)::value;
+    switch (a.act) {
+      case dense::ACT_RELU: finish_eights<T, dense::ACT_RELU, WHOLE>(a, m0, n0, acc); break;
+      case dense::ACT_GELU: finish_eights<T, dense::ACT_GELU, WHOLE>(a, m0, n0, acc); break;
+      case dense::ACT_SILU: finish_eights<T, dense::ACT_SILU, WHOLE>(a, m0, n0, acc); break;
+      default: finish_eights<T, dense::ACT_NONE, WHOLE>(a, m0, n0, acc); break;
     }
   };
-  ask(0);
+  if (a.splits == 1 && m0 + MB * 16 <= a.m && n0 + NB * 16 <= a.n) return eights(std::true_type());
+  if (a.splits == 1 && a.n >= 8) {
+    eights(std::false_type());
+    if (n0 + NB * 16 <= a.n || a.n % 8 == 0) return;
+  }
+  const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int y = 0; y < MB; ++y) {
-    if (y + 1 < MB) ask(y + 1);
-    __builtin_amdgcn_sched_barrier(0);
     const int64_t m = m0 + y * 16 + (lane & 15);
     if (m >= a.m) continue;
-    const float rs = a.r_scale[m];
 #pragma unroll
-    for (int x = 0; x < NB; x += 2) {
-      const int n = first + x * 16;
-      if (n >= a.n) continue;
+    for (int x = 0; x < NB; ++x) {
+      const int n = n0 + x / 2 * 32 + 8 * (lane >> 4) + x % 2 * 4;
       if (a.splits > 1) {
-        int* row = a.part + (split * (int64_t)a.m + m) * a.n;
-        store_sums(row, n, a.n, acc[x][y]);
-        if (n + 4 < a.n) store_sums(row, n + 4, a.n, acc[x + 1][y]);
-      } else {
-        finish8<T>(a, m, n, rs, acc[x][y], acc[x + 1][y], ahead[y & 1][x / 2]);
+        if (n < a.n) store_sums(a.part + (split * (int64_t)a.m + m) * a.n, n, a.n, acc[x][y]);
+      } else if (n < a.n && n >= a.n / 8 * 8) {               // (of an eight that the output has in part)
+        Ends<T> ends;
+        ends.ask(a, m, n);
+        ends.finish(a, m, n, acc[x][y]);
       }
     }
   }
@@ -490,18 +573,17 @@ __device__ inline void wait_tiles(int tiles) {
   }
 }
 
-// BM x BN outputs a workgroup of eight waves, BUFS tiles of 64 bytes of k in LDS.  Two groups of four waves, one of each on every SIMD, half a step
-// apart: while one group multiplies, the other reads its next fragments and asks for a tile BUFS - 1 steps on, so that the matrix pipe has work all the
+// 256 x 256 outputs a workgroup of eight waves, four tiles of 64 bytes of k in LDS.  Two groups of four waves, one of each on every SIMD, half a step
+// apart: while one group multiplies, the other reads its next fragments and asks for a tile three steps on, so that the matrix pipe has work all the
 // time.
 //  - A tile is read by either group after the barrier behind which both have waited for their own loads of it: the wait for tile t + 1 is in
 //    front of the barrier that ends a group's reading of tile t.
-//  - A buffer is written again (the loads of tile t + BUFS - 1) after the barrier behind which both groups have their fragments of tile t - 1 in registers.
+//  - A buffer is written again (the loads of tile t + 3) after the barrier behind which both groups have their fragments of tile t - 1 in registers.
 // Group 1 waits once more in front of the loop, group 0 behind it: both pass the same number of barriers.  k is whole tiles (a last tile that k may end in
 // cost 6 us of 146 at 8,192 x 4,096 x 4,096).
-template <class T, int BM, int BN, int WM, int WN, int BUFS>
+template <class T>
 __global__ __launch_bounds__(512) void turns_kernel(Product a) {
-  constexpr int BK = 64, MB = BM / WM / 16, NB = BN / WN / 16, LT = BN * BK, TILE = (BM + BN) * BK, LOADS = TILE / 1024 / 8;
-  static_assert(WM * WN == 8, "eight waves");
+  constexpr int BM = 256, BN = 256, WM = 4, WN = 2, BUFS = 4, BK = 64, MB = BM / WM / 16, NB = BN / WN / 16, LT = BN * BK, TILE = (BM + BN) * BK, LOADS = TILE / 1024 / 8;
   __shared__ __attribute__((aligned(16))) int8_t lds[BUFS * TILE];        // the columns' tile | the rows' tile, BUFS times
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wm = wave % WM * MB * 16, wn = wave / WM * NB * 16;
   const unsigned tm = (unsigned)(a.m + BM - 1) / BM, tn = (unsigned)(a.n + BN - 1) / BN;
@@ -563,39 +645,61 @@ __global__ __launch_bounds__(256) void join_kernel(Product a) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
     const int64_t m = i / per_row;
     const int n = (int)(i - m * per_row) * 4;
+    Ends<T> ends;
+    ends.ask(a, m, n);
     i32x4 v = {0, 0, 0, 0};
 #pragma unroll 4
     for (int s = 0; s < a.splits; ++s) v += load_sums(a.part + ((int64_t)s * a.m + m) * a.n, n, a.n);
-    finish4<T>(a, m, n, v);
+    ends.finish(a, m, n, v);
   }
 }
 
-enum Kind { kFragments, kSmall, kMiddle, kDirect, kTurns, kLarge };
-struct Plan { Kind kind; int splits, k_per, mb, nb; };         // mb, nb: blocks of 16 rows and columns (fragments)
-
-// Operands in whole pieces of 16 bytes, whose tiles' offsets are 32-bit numbers
-inline bool whole_pieces(const Linear8Args& f) {
-  return f.d_in % 16 == 0 && f.ld_x % 16 == 0 && f.ld_w % 16 == 0 && f.ld_x < (1 << 23) && f.ld_w < (1 << 23) &&
-         reinterpret_cast<uintptr_t>(f.x) % 16 == 0 && reinterpret_cast<uintptr_t>(f.w) % 16 == 0;
+// Operands whose rows no 16 bytes align, laid out again: rows of a.k bytes apart, zeros behind the row's own `k`.  A piece of 16 bytes a thread.
+struct Unaligned { const int8_t* from; int8_t* to; int64_t ld; int rows; };
+template <class T>
+__global__ __launch_bounds__(256) void align_kernel(Unaligned x, Unaligned w, int k, int k_out) {
+  const int pieces = k_out / 16;
+  const int64_t total = ((int64_t)x.rows + w.rows) * pieces;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t line = i / pieces;
+    const int at = (int)(i - line * pieces) * 16;
+    const bool of_x = line < x.rows;
+    const int64_t row = of_x ? line : line - x.rows;
+    const int8_t* from = (of_x ? x.from + row * x.ld : w.from + row * w.ld) + at;
+    u32x4 v = {0, 0, 0, 0};
+    if (at < k) v = load16<T, kWide>(from, k - at);          // (k > 16)
+    *reinterpret_cast<u32x4*>((of_x ? x.to : w.to) + row * k_out + at) = v;
+  }
 }
 
-// Which kernel, by the number of tiles and the length of their sums (us, bf16 outputs with the full epilogue; each pair is the two sides of a rule):
-//   fragments  the smallest tile that makes 256 workgroups at most (500 x 500 x 500: 32 x 32 4.0, 32 x 16 4.1, 32 x 64 4.5; 16 x 11,008 x 4,096: 32 x 64 13.3, 16 x 16 14.6) and
-//              reads 400 KB of operands a workgroup at most (256 x 2,048 x 4,096, 393 KB: 14.5, in 128 x 128 16.6; 128 x 4,096 x 8,192, 786 KB: 25.5 and
-//              20.4), with up to 16 rows 1 MB; rows that no 16 bytes align cost it three times that: 64 KB (100 x 1,000 x 999, 48 KB: 5.8, in 64 x 64 8.4;
-//              1,000 x 257 x 1,999, 192 KB: 15.9 and 13.5)
-//   256 x 256  whole tiles of 64 of k, long sums, and tiles that fill the 256 CUs' rounds to nine tenths: 8,192 x 4,096 x 4,096 153, in 128 x 128 182;
-//              2,048 x 8,192 x 4,096 95 and 104; but 5,000 x 4,096 x 4,096 (320 tiles) 141 and 130
-//   128 x 128  from 2^32 multiplications on (padded) where tiles go into LDS directly: 512 x 4,096 x 4,096 24.1, in 64 x 64 31.5; 16,384 x 256 x 1,024 17.7 and
-//              19.3; but 512 x 4,096 x 1,024 16.8 and 14.2; k split to make a workgroup for every CU (200 x 4,096 x 4,096 in one 26.5, in four 18.6);
-//              by eight waves in turns where a CU has one workgroup at most or little to sum (2,048 x 2,048 x 2,048 20.1, by four waves 22.1; 4,096 x 8,192 x 256
-//              66 and 70; but 16,384 x 1,024 x 1,024 50 and 47)
-//              from 2^34 on through registers: 1,024 x 4,096 x 4,096 42 and 47; but 4,000 x 1,000 x 1,000 28 and 20
+enum Kind { kFragments, kSmall, kDirect, kLarge };
+struct Plan { Kind kind; int splits, k_per, mb, nb, aligned; };      // mb, nb: blocks of 16 rows and columns (fragments); aligned: bytes of k in operands that are laid out again
+
+// Operands in whole pieces of 16 bytes, whose tiles' offsets are 32-bit numbers: by their sizes, and by where they lie too
+inline bool whole_rows(const Linear8Args& f) {
+  return f.d_in % 16 == 0 && f.ld_x % 16 == 0 && f.ld_w % 16 == 0 && f.ld_x < (1 << 23) && f.ld_w < (1 << 23);
+}
+inline bool whole_pieces(const Linear8Args& f) {
+  return whole_rows(f) && reinterpret_cast<uintptr_t>(f.x) % 16 == 0 && reinterpret_cast<uintptr_t>(f.w) % 16 == 0;
+}
+
+// Which kernel, by the number of tiles and the length of their sums (us, bf16 outputs with gelu, bias and residual; each pair is the two sides of a rule):
+//   fragments  the smallest tile that makes 256 workgroups at most (500 x 500 x 500: 32 x 32 3.8, 32 x 16 7.4, 32 x 64 4.4; 16 x 11,008 x 4,096: 32 x 64 12.7, 16 x 16 15.0) and
+//              reads 400 KB of operands a workgroup at most (256 x 2,048 x 4,096, 393 KB: 14.2, in 128 x 128 16.0; 128 x 4,096 x 8,192, 786 KB: 24.8 and
+//              19.7), with up to 16 rows 1 MB; rows that no 16 bytes align cost it three times that: 64 KB (100 x 1,000 x 999, 48 KB: 5.5, in 64 x 64 8.0;
+//              1,000 x 257 x 1,999, 192 KB: 15.9 and 13.4)
+//   256 x 256  whole tiles of 64 of k, long sums, and tiles that fill the 256 CUs' rounds to nine tenths: 8,192 x 4,096 x 4,096 157, in 128 x 128 174;
+//              2,048 x 8,192 x 4,096 81 and 91; but 5,000 x 4,096 x 4,096 (320 tiles) 119 and 108, 4,096 x 8,192 x 256 54.6 and 52.0
+//   128 x 128  from 2^31 multiplications on (padded) with 192 tiles and more, from 2^32 on with fewer: 8,192 x 512 x 512 9.9, in 64 x 64 12.4; 4,000 x 1,000 x 1,008 14.2 and
+//              17.8; but 1,500 x 1,500 x 1,504 19.4 and 17.0; k split to make a workgroup for every CU (200 x 4,096 x 4,096 in one 26.5, in four 18.1)
 //   64 x 64    everything smaller, k split while there are fewer than 1,024 workgroups, eight tiles of k a split at least, four where there are few workgroups
 //              (70 x 64 x 8,192 in 8 splits 12.6, in 16 9.1)
-inline Plan plan_of(int64_t m, int64_t n, int64_t k, bool whole) {
+// Rows that 16 bytes do not align are laid out again where that makes one of the larger kernels possible, with 192 tiles of 128 x 128 and more and 128 rows and
+// columns (8,192 x 4,096 x 4,095: 168, in 64 x 64 as they are 461; 4,000 x 1,000 x 1,001 18.4 and 21.4; 50,000 x 128 x 1,001 36 and 44; but 6,000 x 500 x 1,001, 188 tiles,
+// 21.0 and 17.2; 100,000 x 64 x 4,095 281 and 163).
+inline Plan plan_of(int64_t m, int64_t n, int64_t k, bool whole, bool align) {
   const auto tiles_of = [&](int64_t b) { return ((m + b - 1) / b) * ((n + b - 1) / b); };
-  Plan p{kFragments, 1, (int)up(k, kBK), 0, 0};
+  Plan p{kFragments, 1, (int)up(k, kBK), 0, 0, 0};
   const int64_t most = !whole ? 64 << 10 : m <= 16 ? 1 << 20 : 400 << 10;
   for (const auto& b : {std::pair<int, int>{1, 1}, {2, 1}, {2, 2}, {2, 4}, {4, 4}}) {
     p.mb = b.first;
@@ -612,14 +716,16 @@ inline Plan plan_of(int64_t m, int64_t n, int64_t k, bool whole) {
     p.splits = (int)((k + p.k_per - 1) / p.k_per);
   };
   const int64_t large = tiles_of(256), middle = tiles_of(128), small = tiles_of(64), rounds = (large + 255) / 256;
+  if (!whole && align && k > 16 && middle >= 192 && m >= 128 && n >= 128) {
+    Plan q = plan_of(m, n, up(k, 64), true, false);
+    q.aligned = (int)up(k, 64);
+    if (q.kind > kSmall) return q;
+  }
   if (whole && k % 64 == 0 && k >= 1024 && large * 10 >= rounds * 256 * 9) {
     p.kind = kLarge;
-  } else if (whole && middle * k >= 1 << 18) {
+  } else if (whole && middle * k >= (middle >= 192 ? 1 << 17 : 1 << 18)) {
     p.kind = kDirect;
     split(middle, 256, 8);
-    if (k % 64 == 0 && p.splits == 1 && (middle <= 256 || k <= 512)) p.kind = kTurns;
-  } else if (middle * k >= 1 << 20 && middle >= 256) {
-    p.kind = kMiddle;
   } else {
     p.kind = kSmall;
     split(small, 1024, small * (k / (8 * kBK)) < 64 ? 4 : 8);
@@ -627,21 +733,33 @@ inline Plan plan_of(int64_t m, int64_t n, int64_t k, bool whole) {
   return p;
 }
 
+// Workspace: operands laid out again, then the sums of splits
+inline size_t aligned_bytes(const Plan& p, int64_t m, int64_t n) { return (size_t)up((m + n) * p.aligned, 256); }
 inline size_t part_bytes(const Linear8Args& f) {
   if (f.rows == 0) return 0;                                  // (a plan has a tile at least)
-  // (the pointers' alignment is not known where the workspace is asked for: enough for either)
-  const Plan p = plan_of(f.rows, f.d_out, f.d_in, true), q = plan_of(f.rows, f.d_out, f.d_in, false);
-  const int splits = p.splits > q.splits ? p.splits : q.splits;
-  return splits > 1 ? (size_t)splits * f.rows * f.d_out * sizeof(int) : 0;
+  const auto bytes = [&](const Plan& p) {
+    return aligned_bytes(p, f.rows, f.d_out) + (p.splits > 1 ? (size_t)p.splits * f.rows * f.d_out * sizeof(int) : 0);
+  };
+  // (where the operands lie is not known when the workspace is asked for: enough for either)
+  const bool whole = whole_rows(f);
+  const size_t any = bytes(plan_of(f.rows, f.d_out, f.d_in, false, !whole)), best = whole ? bytes(plan_of(f.rows, f.d_out, f.d_in, true, false)) : 0;
+  return any > best ? any : best;
 }
 
 template <class T>
 hipError_t run(Product a, const Plan& p, void* ws, hipStream_t s) {
   a.splits = p.splits;
   a.k_per = p.k_per;
-  a.part = static_cast<int*>(ws);
+  a.part = reinterpret_cast<int*>(static_cast<char*>(ws) + aligned_bytes(p, a.m, a.n));
   const auto grid = [&](int64_t b) { return ((a.m + b - 1) / b) * ((a.n + b - 1) / b) * p.splits; };
   hipError_t e = hipErrorInvalidValue;
+  if (p.aligned) {
+    int8_t* to = static_cast<int8_t*>(ws);
+    const Unaligned x{a.r, to, a.ld_r, a.m}, w{a.l, to + (int64_t)a.m * p.aligned, a.ld_l, a.n};
+    const int64_t blocks = (((int64_t)a.m + a.n) * (p.aligned / 16) + 255) / 256;
+    if ((e = launch(align_kernel<int8_t>, blocks < 8192 ? blocks : 8192, 256, s, x, w, a.k, p.aligned)) != hipSuccess) return e;
+    a.r = x.to; a.l = w.to; a.ld_r = a.ld_l = a.k = p.aligned;
+  }
   switch (p.kind) {
     case kFragments: {
       const int64_t n = ((a.m + 16 * p.mb - 1) / (16 * p.mb)) * (int64_t)((a.n + 16 * p.nb - 1) / (16 * p.nb));
@@ -651,11 +769,9 @@ hipError_t run(Product a, const Plan& p, void* ws, hipStream_t s) {
       if (p.nb == 2) return launch(fragments_kernel<T, 2, 2>, n, 512, s, a);
       return launch(fragments_kernel<T, 2, 4>, n, 512, s, a);
     }
-    case kSmall: e = launch(product_kernel<T, 64, 64, 2, 2, 3>, grid(64), 256, s, a); break;
-    case kMiddle: e = launch(product_kernel<T, 128, 128, 2, 2, 1>, grid(128), 256, s, a); break;
+    case kSmall: e = launch(product_kernel<T>, grid(64), 256, s, a); break;
     case kDirect: e = launch(direct_kernel<T>, grid(128), 256, s, a); break;
-    case kTurns: return launch(turns_kernel<T, 128, 128, 2, 4, 5>, grid(128), 512, s, a);
-    case kLarge: return launch(turns_kernel<T, 256, 256, 4, 2, 4>, grid(256), 512, s, a);
+    case kLarge: return launch(turns_kernel<T>, grid(256), 512, s, a);
   }
   if (e != hipSuccess || p.splits == 1) return e;
   const int64_t blocks = ((int64_t)a.m * ((a.n + 3) / 4) + 255) / 256;
@@ -670,7 +786,7 @@ hipError_t forward(const Linear8Args& f, void* ws, hipStream_t s) {
   a.r_scale = f.x_scale; a.l_scale = f.w_scale;
   a.bias = f.bias; a.residual = f.residual; a.ld_res = f.ld_res;
   a.out = f.y; a.ld_out = f.ld_y; a.act = f.act;
-  return run<T>(a, plan_of(a.m, a.n, a.k, whole_pieces(f)), ws, s);
+  return run<T>(a, plan_of(a.m, a.n, a.k, whole_pieces(f), !whole_rows(f)), ws, s);
 }
 
 }  // namespace dense8

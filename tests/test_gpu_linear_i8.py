@@ -150,10 +150,12 @@ def test_rows_past_32_bits(size):
     within(got, refs.linear_i8(x, xs, w, ws, b, "none", r, dt), "y")
 
 
-# one size and more for each kernel and its edges: fragments of every shape; tiles of 64 x 64 in one sum and in several; 128 x 128 through registers (rows that no
-# 16 bytes align), directly with k that ends inside a tile, in one sum and in several; in turns with few and with many tiles; 256 x 256, whole and cut
+# one size and more for each kernel and its edges: fragments of every shape; tiles of 64 x 64 in one sum and in several; 128 x 128 directly, with k that ends
+# inside a tile, in one sum and in several; 256 x 256, whole and cut; outputs of fewer columns than an eight and of a few more; rows that no
+# 16 bytes align laid out again for each of them
 KINDS = [(16, 512, 4000), (33, 512, 2000), (100, 640, 1250), (60, 1500, 8100), (1000, 272, 1000), (500, 1027, 900), (300, 3001, 200), (2100, 4001, 2050), (2100, 1040, 2050),
-         (200, 4112, 4096), (1500, 2048, 1530), (2000, 512, 4090), (3900, 1088, 4090), (4096, 1024, 4096)]
+         (200, 4112, 4096), (1500, 2048, 1530), (2000, 512, 4090), (3900, 1088, 4090), (4096, 1024, 4096), (25000, 704, 5), (60000, 1024, 5), (60000, 1024, 13),
+         (4000, 1001, 1000), (8190, 1023, 2048), (1999, 2050, 2001), (20000, 33, 2000), (20000, 17, 2003)]
 
 
 @pytest.mark.parametrize("dt", TYPES, ids=str)
@@ -163,6 +165,34 @@ def test_every_kernel(size, dt):
     cpu = lambda t: tuple(v.cpu() for v in t)  # noqa: E731
     within(binding.linear_i8(x, xs, w, ws, bias=b, activation="gelu", residual=r), cpu(refs.linear_i8(x, xs, w, ws, b, "gelu", r, dt)), "y")
     within(binding.linear_i8(x, xs, w, ws, dtype=dt), cpu(refs.linear_i8(x, xs, w, ws, None, "none", None, dt)), "no epilogue")
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=str)
+@pytest.mark.parametrize("size", [(33, 512, 2000), (300, 3001, 200), (2100, 1040, 2050), (200, 4112, 4096), (1500, 2048, 1530), (3900, 1088, 4090), (1999, 2050, 2001)], ids=str)
+def test_y_over_the_residual(size, dt):
+    """The C entry's y may be exactly the residual."""
+    x, xs, w, ws, b, r = (t.cuda() for t in make(*size, dt))
+    want = binding.linear_i8(x, xs, w, ws, bias=b, activation="gelu", residual=r)
+    rows, d_in, d_out = size
+    args = binding._PACK_LINEAR_I8.pack(binding._dtype_code(r), binding.ACTIVATIONS["gelu"], rows, d_in, d_out, 0, d_in, d_in, d_out, d_out, x.data_ptr(), w.data_ptr(),
+                                        xs.data_ptr(), ws.data_ptr(), b.data_ptr(), r.data_ptr(), r.data_ptr())
+    L = binding.load_library()
+    binding._run_operator(L.stgn_linear_quantized_workspace, L.stgn_linear_quantized, args, None, r.device)
+    assert torch.equal(r, want)
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=str)
+@pytest.mark.parametrize("at", [0, 1, 8, 16])
+def test_rows_that_start_anywhere(at, dt):
+    """Whole pieces but for where the first row lies, or how far apart rows are; the residual is only read."""
+    x, xs, w, ws, b, r = (t.cuda() for t in make(2100, 1040, 2050, dt))
+    for ld in (1040 + 16, 1040 + 19):
+        X = torch.empty(2100 * ld + 16, dtype=torch.int8, device="cuda")[at:at + 2100 * ld].view(2100, ld)[:, :1040]
+        X.copy_(x)
+        y = r.clone()
+        got = binding.linear_i8(X, xs, w, ws, bias=b, activation="silu", residual=y)
+        within(got, tuple(v.cpu() for v in refs.linear_i8(x, xs, w, ws, b, "silu", r, dt)), "y")
+        assert torch.equal(y, r)
 
 
 @pytest.mark.parametrize("size", [(260, 32784, 260), (1500, 2048, 1500)], ids=str)

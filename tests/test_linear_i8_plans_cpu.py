@@ -16,21 +16,24 @@ int main() {
   for (long m : rows)
     for (long n : cols)
       for (long k : sum)
-        for (int whole = 0; whole < (k % 16 == 0 ? 2 : 1); ++whole) {
-          const Plan p = plan_of(m, n, k, whole);
+        for (int rows = 0; rows < 3; ++rows) {                // whole pieces; whole ones but for where they lie; rows that 16 bytes do not align
+          if (rows < 2 && k % 16) continue;
           stgn::Linear8Args f{};
-          f.rows = (int)m; f.d_out = (int)n; f.d_in = (int)k;
-          printf("%ld %ld %ld %d %d %d %d %d %d %zu\n", m, n, k, whole, (int)p.kind, p.splits, p.k_per, p.mb, p.nb, part_bytes(f));
+          f.rows = (int)m; f.d_out = (int)n; f.d_in = (int)k; f.ld_x = rows == 2 ? k / 16 * 16 + 17 : k; f.ld_w = k;
+          f.x = reinterpret_cast<const int8_t*>(rows == 1 ? 8 : 16);
+          const Plan p = plan_of(m, n, k, whole_pieces(f), !whole_rows(f));
+          printf("%ld %ld %ld %d %d %d %d %d %d %zu %d\n", m, n, k, rows, (int)p.kind, p.splits, p.k_per, p.mb, p.nb, part_bytes(f), p.aligned);
         }
   return 0;
 }
 """
-FRAGMENTS, SMALL, MIDDLE, DIRECT, TURNS, LARGE = range(6)
+FRAGMENTS, SMALL, DIRECT, LARGE = range(4)
+WHOLE, ELSEWHERE, UNALIGNED = range(3)
 
 
 @pytest.fixture(scope="module")
 def plans(tmp_path_factory):
-    """m, n, k, whether both operands are whole pieces, and the plan: kernel, splits, k a split, blocks; bytes of the workspace"""
+    """m, n, k, how the rows lie, and the plan: kernel, splits, k a split, blocks; bytes of the workspace; k of operands that are laid out again"""
     at = tmp_path_factory.mktemp("plans")
     (at / "ask.hip").write_text(ASK)
     subprocess.run([os.environ.get("HIPCC", "/opt/rocm/bin/hipcc"), "-O1", "--offload-host-only", "--offload-arch=gfx950", "-std=c++17", "-I", build.CSRC, "-I",
@@ -39,22 +42,25 @@ def plans(tmp_path_factory):
 
 
 def test_every_kernel_is_reached(plans):
-    assert {p[4] for p in plans} == {FRAGMENTS, SMALL, MIDDLE, DIRECT, TURNS, LARGE}
+    assert {p[4] for p in plans if p[3] == WHOLE} == {FRAGMENTS, SMALL, DIRECT, LARGE}
+    assert {p[4] for p in plans if p[10]} == {DIRECT, LARGE}
     assert {p[7:9] for p in plans if p[4] == FRAGMENTS} == {(1, 1), (2, 1), (2, 2), (2, 4), (4, 4)}
 
 
 def test_tiles_that_go_into_lds_directly_are_whole_pieces(plans):
-    """The direct kernels read 16 aligned bytes a lane, the ones in turns whole tiles of 64 bytes of k: never a part of one."""
-    for m, n, k, whole, kind, splits, k_per, *_ in plans:
-        if kind in (DIRECT, TURNS, LARGE):
-            assert whole and k % 16 == 0 and k_per % 128 == 0, (m, n, k)
-        if kind in (TURNS, LARGE):
-            assert k % 64 == 0 and splits == 1, (m, n, k)
+    """The direct kernels read 16 aligned bytes a lane, the one of 256 x 256 whole tiles of 64 bytes of k: never a part of one."""
+    for m, n, k, rows, kind, splits, k_per, _, _, _, aligned in plans:
+        if aligned:
+            assert rows == UNALIGNED and k > 16 and aligned % 64 == 0 and k <= aligned < k + 64 and kind in (DIRECT, LARGE), (m, n, k)
+        if kind in (DIRECT, LARGE):
+            assert (rows == WHOLE or aligned) and (aligned or k) % 16 == 0 and k_per % 128 == 0, (m, n, k)
+        if kind == LARGE:
+            assert (aligned or k) % 64 == 0 and splits == 1, (m, n, k)
 
 
 def test_splits_cover_the_sum_once_and_fit_the_workspace(plans):
-    for m, n, k, whole, kind, splits, k_per, mb, nb, size in plans:
-        assert splits >= 1 and (splits - 1) * k_per < k <= splits * k_per, (m, n, k)
-        assert size >= (splits * m * n * 4 if splits > 1 else 0), (m, n, k)
+    for m, n, k, _, kind, splits, k_per, mb, nb, size, aligned in plans:
+        assert splits >= 1 and (splits - 1) * k_per < (aligned or k) <= splits * k_per, (m, n, k)
+        assert size >= (splits * m * n * 4 if splits > 1 else 0) + (m + n) * aligned, (m, n, k)
         if kind == FRAGMENTS:
             assert splits == 1 and -(-m // (16 * mb)) * -(-n // (16 * nb)) <= 256, (m, n, k)
