@@ -222,14 +222,15 @@ __global__ __launch_bounds__(512) void fragments_kernel(Product a) {
 
 // ---- tiles through registers
 
-// 64 x 64 outputs a workgroup of four waves, any alignment.  Three tiles of k are on their way in registers while one is multiplied: where tiles are small and
-// few, what a tile takes is the wait for memory.
-template <class T>
-__global__ __launch_bounds__(256, 4) void product_kernel(Product a) {
+// 64 x 64 outputs a workgroup, any alignment.  HALVES = 1: four waves, three tiles of 128 bytes of k on their way in registers while one is multiplied.  HALVES
+// = 2, for few workgroups, where what a tile takes is a wait: eight waves, tiles of 256 bytes, either half of the waves takes one half and at the end finishes
+// one half of the rows (1,531 x 777 x 1,027: 13.6 us, by four waves 15.5; 500 x 1,027 x 900 8.6 and 11.3; but 6,000 x 500 x 1,001 19.7 and 17.5).
+template <class T, int HALVES>
+__global__ __launch_bounds__(HALVES * 256, 4) void product_kernel(Product a) {
   using El = Elem<int8_t>;
-  constexpr int BM = 64, BN = 64, THREADS = 256, MB = 2, NB = 2, DEPTH = 3, S = lds_stride<int8_t>(kBK);
+  constexpr int BM = 64, BN = 64, BK = HALVES * kBK, THREADS = HALVES * 256, MB = 2, NB = 2, DEPTH = HALVES == 1 ? 3 : 1, S = lds_stride<int8_t>(BK);
   __shared__ __attribute__((aligned(16))) int8_t ls[BN * S], rs[BM * S];
-  const int wave = threadIdx.x >> 6, wm = wave % 2 * MB * 16, wn = wave / 2 * NB * 16;
+  const int wave = threadIdx.x >> 6, half = wave >> 2, wm = wave % 2 * MB * 16, wn = wave / 2 % 2 * NB * 16;
   const unsigned tm = (unsigned)(a.m + BM - 1) / BM, tn = (unsigned)(a.n + BN - 1) / BN;
   const int split = (int)(blockIdx.x / (tm * tn));
   int row, col;
@@ -237,8 +238,8 @@ __global__ __launch_bounds__(256, 4) void product_kernel(Product a) {
   const int m0 = row * BM, n0 = col * BN;
   const int kb = split * a.k_per, ke = min(a.k, kb + a.k_per);
 
-  using MoveL = ProductMove<int8_t, BN, kBK, THREADS, true>;
-  using MoveR = ProductMove<int8_t, BM, kBK, THREADS, true>;
+  using MoveL = ProductMove<int8_t, BN, BK, THREADS, true>;
+  using MoveR = ProductMove<int8_t, BM, BK, THREADS, true>;
   MoveL ml;
   MoveR mr;
   ml.start(a.l, a.ld_l, n0, a.n, kb, ke, a.k);
@@ -255,7 +256,8 @@ __global__ __launch_bounds__(256, 4) void product_kernel(Product a) {
   };
   auto multiply = [&] {
 #pragma unroll
-    for (int s = 0; s < kBK; s += El::KF) {
+    for (int i = 0; i < kBK; i += El::KF) {
+      const int s = half * kBK + i;
       i32x4 lf[NB], rf[MB];
 #pragma unroll
       for (int x = 0; x < NB; ++x) lf[x] = frag_rows(ls, S, wn + x * 16, s);
@@ -269,43 +271,45 @@ __global__ __launch_bounds__(256, 4) void product_kernel(Product a) {
   };
 #pragma unroll
   for (int d = 0; d < DEPTH; ++d)
-    if (kb + d * kBK < ke) fetch(d, kb + d * kBK);
-  for (int kt = kb; kt < ke; kt += DEPTH * kBK) {
+    if (kb + d * BK < ke) fetch(d, kb + d * BK);
+  for (int kt = kb; kt < ke; kt += DEPTH * BK) {
 #pragma unroll
     for (int d = 0; d < DEPTH; ++d) {
-      const int k = kt + d * kBK;
+      const int k = kt + d * BK;
       if (k >= ke) break;
       __syncthreads();
       ml.store(ls, rl[d]);
       mr.store(rs, rr[d]);
       __syncthreads();
-      if (k + DEPTH * kBK < ke) fetch(d, k + DEPTH * kBK);
+      if (k + DEPTH * BK < ke) fetch(d, k + DEPTH * BK);
       multiply();
     }
   }
   const int lane = threadIdx.x & 63, m = m0 + wm + (lane & 15), n = n0 + wn + 4 * (lane >> 4);
-  if (a.splits > 1) {
+  constexpr int ROWS = MB / HALVES;                           // blocks of sixteen rows that this wave finishes
+  Ends<T> ends[ROWS][NB];
+  auto line = [&](int y) { return m + (HALVES == 1 ? y : half) * 16; };
 #pragma unroll
-    for (int y = 0; y < MB; ++y)
+  for (int y = 0; y < ROWS; ++y)
 #pragma unroll
-      for (int x = 0; x < NB; ++x)
-        if (m + y * 16 < a.m && n + x * 16 < a.n) store_sums(a.part + (split * (int64_t)a.m + m + y * 16) * a.n, n + x * 16, a.n, acc[x][y]);
-    return;
+    for (int x = 0; x < NB; ++x)
+      if (a.splits == 1 && line(y) < a.m && n + x * 16 < a.n) ends[y][x].ask(a, line(y), n + x * 16);
+  if constexpr (HALVES == 2) {
+    __shared__ i32x4 part[8][NB][64];
+#pragma unroll
+    for (int x = 0; x < NB; ++x) part[wave][x][lane] = half ? acc[x][0] : acc[x][1];
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < NB; ++x) acc[x][0] = (half ? acc[x][1] : acc[x][0]) + part[wave ^ 4][x][lane];
   }
-  Ends<T> ends[2][NB];                                        // of sixteen rows and the next sixteen
-  auto ask = [&](int y) {
 #pragma unroll
-    for (int x = 0; x < NB; ++x)
-      if (m + y * 16 < a.m && n + x * 16 < a.n) ends[y & 1][x].ask(a, m + y * 16, n + x * 16);
-  };
-  ask(0);
+  for (int y = 0; y < ROWS; ++y) {
 #pragma unroll
-  for (int y = 0; y < MB; ++y) {
-    if (y + 1 < MB) ask(y + 1);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int x = 0; x < NB; ++x)
-      if (m + y * 16 < a.m && n + x * 16 < a.n) ends[y & 1][x].finish(a, m + y * 16, n + x * 16, acc[x][y]);
+    for (int x = 0; x < NB; ++x) {
+      if (line(y) >= a.m || n + x * 16 >= a.n) continue;
+      if (a.splits > 1) store_sums(a.part + (split * (int64_t)a.m + line(y)) * a.n, n + x * 16, a.n, acc[x][y]);
+      else ends[y][x].finish(a, line(y), n + x * 16, acc[x][y]);
+    }
   }
 }
 
@@ -672,7 +676,7 @@ __global__ __launch_bounds__(256) void align_kernel(Unaligned x, Unaligned w, in
   }
 }
 
-enum Kind { kFragments, kSmall, kDirect, kLarge };
+enum Kind { kFragments, kSmall, kSmall2, kDirect, kLarge };
 struct Plan { Kind kind; int splits, k_per, mb, nb, aligned; };      // mb, nb: blocks of 16 rows and columns (fragments); aligned: bytes of k in operands that are laid out again
 
 // Operands in whole pieces of 16 bytes, whose tiles' offsets are 32-bit numbers: by their sizes, and by where they lie too
@@ -687,13 +691,13 @@ inline bool whole_pieces(const Linear8Args& f) {
 //   fragments  the smallest tile that makes 256 workgroups at most (500 x 500 x 500: 32 x 32 3.8, 32 x 16 7.4, 32 x 64 4.4; 16 x 11,008 x 4,096: 32 x 64 12.7, 16 x 16 15.0) and
 //              reads 400 KB of operands a workgroup at most (256 x 2,048 x 4,096, 393 KB: 14.2, in 128 x 128 16.0; 128 x 4,096 x 8,192, 786 KB: 24.8 and
 //              19.7), with up to 16 rows 1 MB; rows that no 16 bytes align cost it three times that: 64 KB (100 x 1,000 x 999, 48 KB: 5.5, in 64 x 64 8.0;
-//              1,000 x 257 x 1,999, 192 KB: 15.9 and 13.4)
+//              1,000 x 257 x 1,999, 192 KB: 16.0 and 12.3)
 //   256 x 256  whole tiles of 64 of k, long sums, and tiles that fill the 256 CUs' rounds to nine tenths: 8,192 x 4,096 x 4,096 157, in 128 x 128 174;
 //              2,048 x 8,192 x 4,096 81 and 91; but 5,000 x 4,096 x 4,096 (320 tiles) 119 and 108, 4,096 x 8,192 x 256 54.6 and 52.0
 //   128 x 128  from 2^31 multiplications on (padded) with 192 tiles and more, from 2^32 on with fewer: 8,192 x 512 x 512 9.9, in 64 x 64 12.4; 4,000 x 1,000 x 1,008 14.2 and
 //              17.8; but 1,500 x 1,500 x 1,504 19.4 and 17.0; k split to make a workgroup for every CU (200 x 4,096 x 4,096 in one 26.5, in four 18.1)
-//   64 x 64    everything smaller, k split while there are fewer than 1,024 workgroups, eight tiles of k a split at least, four where there are few workgroups
-//              (70 x 64 x 8,192 in 8 splits 12.6, in 16 9.1)
+//   64 x 64    everything smaller; by eight waves with up to 512 tiles, k split to make up to 512 workgroups of 512 bytes of k at least (64 x 8,192 x 8,191 in four 27.1,
+//              in two 33.3, in eight 31.1; 1,000 x 257 x 1,999 in three 12.3, in one 15.4; 70 x 64 x 8,192 in 16 8.6, in eight 9.4)
 // Rows that 16 bytes do not align are laid out again where that makes one of the larger kernels possible, with 192 tiles of 128 x 128 and more and 128 rows and
 // columns (8,192 x 4,096 x 4,095: 168, in 64 x 64 as they are 461; 4,000 x 1,000 x 1,001 18.4 and 21.4; 50,000 x 128 x 1,001 36 and 44; but 6,000 x 500 x 1,001, 188 tiles,
 // 21.0 and 17.2; 100,000 x 64 x 4,095 281 and 163).
@@ -719,7 +723,7 @@ inline Plan plan_of(int64_t m, int64_t n, int64_t k, bool whole, bool align) {
   if (!whole && align && k > 16 && middle >= 192 && m >= 128 && n >= 128) {
     Plan q = plan_of(m, n, up(k, 64), true, false);
     q.aligned = (int)up(k, 64);
-    if (q.kind > kSmall) return q;
+    if (q.kind >= kDirect) return q;
   }
   if (whole && k % 64 == 0 && k >= 1024 && large * 10 >= rounds * 256 * 9) {
     p.kind = kLarge;
@@ -727,8 +731,8 @@ inline Plan plan_of(int64_t m, int64_t n, int64_t k, bool whole, bool align) {
     p.kind = kDirect;
     split(middle, 256, 8);
   } else {
-    p.kind = kSmall;
-    split(small, 1024, small * (k / (8 * kBK)) < 64 ? 4 : 8);
+    p.kind = small > 512 ? kSmall : kSmall2;
+    if (p.kind == kSmall2) split(small, 512, 4);
   }
   return p;
 }
@@ -769,7 +773,8 @@ hipError_t run(Product a, const Plan& p, void* ws, hipStream_t s) {
       if (p.nb == 2) return launch(fragments_kernel<T, 2, 2>, n, 512, s, a);
       return launch(fragments_kernel<T, 2, 4>, n, 512, s, a);
     }
-    case kSmall: e = launch(product_kernel<T>, grid(64), 256, s, a); break;
+    case kSmall: return launch(product_kernel<T, 1>, grid(64), 256, s, a);
+    case kSmall2: e = launch(product_kernel<T, 2>, grid(64), 512, s, a); break;
     case kDirect: e = launch(direct_kernel<T>, grid(128), 256, s, a); break;
     case kLarge: return launch(turns_kernel<T>, grid(256), 512, s, a);
   }

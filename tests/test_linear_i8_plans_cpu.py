@@ -27,7 +27,7 @@ int main() {
   return 0;
 }
 """
-FRAGMENTS, SMALL, DIRECT, LARGE = range(4)
+FRAGMENTS, SMALL, SMALL2, DIRECT, LARGE = range(5)
 WHOLE, ELSEWHERE, UNALIGNED = range(3)
 
 
@@ -42,7 +42,7 @@ def plans(tmp_path_factory):
 
 
 def test_every_kernel_is_reached(plans):
-    assert {p[4] for p in plans if p[3] == WHOLE} == {FRAGMENTS, SMALL, DIRECT, LARGE}
+    assert {p[4] for p in plans if p[3] == WHOLE} == {FRAGMENTS, SMALL, SMALL2, DIRECT, LARGE}
     assert {p[4] for p in plans if p[10]} == {DIRECT, LARGE}
     assert {p[7:9] for p in plans if p[4] == FRAGMENTS} == {(1, 1), (2, 1), (2, 2), (2, 4), (4, 4)}
 
@@ -62,5 +62,6 @@ def test_splits_cover_the_sum_once_and_fit_the_workspace(plans):
     for m, n, k, _, kind, splits, k_per, mb, nb, size, aligned in plans:
         assert splits >= 1 and (splits - 1) * k_per < (aligned or k) <= splits * k_per, (m, n, k)
         assert size >= (splits * m * n * 4 if splits > 1 else 0) + (m + n) * aligned, (m, n, k)
+        assert splits == 1 or kind in (SMALL2, DIRECT), (m, n, k)
         if kind == FRAGMENTS:
-            assert splits == 1 and -(-m // (16 * mb)) * -(-n // (16 * nb)) <= 256, (m, n, k)
+            assert -(-m // (16 * mb)) * -(-n // (16 * nb)) <= 256, (m, n, k)
