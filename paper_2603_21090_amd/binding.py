@@ -210,7 +210,7 @@ def _dtype_code(t):
 
 def _expect(name, t, like, shape):
     """The address of a tensor of this shape, of `like`'s type and device, whose last dimension lies side by side."""
-    if t.dtype != like.dtype or t.device != like.device:
+    if t.dtype != like.dtype or t.get_device() != like.get_device():
         raise ValueError(f"{name}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
     if t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
@@ -233,20 +233,23 @@ def _run_operator(ask, call, args, grad, device):
     """Workspace of the call (the caching allocator's, on the current stream), then the call.  ask: None where the call needs none; grad: None where
     there is no gradient to ask for."""
     import torch
-    if device.type != "cuda":
+    index = device.index                                      # (a tensor's: None on the host)
+    if index is None or device.type != "cuda":
         raise ValueError(f"tensors must be on the GPU, not on {device}")
-    if torch.cuda.current_device() != device.index:
+    if torch._C._cuda_getDevice() != index:
         with torch.cuda.device(device):
             return _run_operator(ask, call, args, grad, device)
-    n, rc = C.c_size_t(0), 0
+    rc, size, where = 0, 0, None
     if ask is not None:
+        n = C.c_size_t(0)
         rc = ask(args, C.byref(n)) if grad is None else ask(args, None, C.byref(n)) if grad else ask(args, C.byref(n), None)
-    if rc == 0:
-        size, ws = n.value, None
-        if size:
+        size = n.value
+        if size and rc == 0:
             ws = torch.empty(size, dtype=torch.uint8, device=device)
+            where = ws.data_ptr()
+    if rc == 0:
         # (the handle alone: building a Stream object around it takes as long as the launch)
-        rc = call(args, ws.data_ptr() if size else None, size, torch._C._cuda_getCurrentRawStream(device.index))
+        rc = call(args, where, size, torch._C._cuda_getCurrentRawStream(index))
     if rc:
         raise StgnError(rc, load_library().stgn_last_error(None).decode())
 
@@ -358,7 +361,7 @@ def attention_grad(dout, q, k, v, out, lse, q_lens=None, k_lens=None, causal=Fal
 def _rows(name, t, like=None):
     """Address of a matrix and elements between its rows, or an error; of `like`'s type, device and shape."""
     shape = t.shape
-    if like is not None and (t.dtype != like.dtype or t.device != like.device or shape != like.shape):
+    if like is not None and (t.dtype != like.dtype or t.get_device() != like.get_device() or shape != like.shape):
         raise ValueError(f"{name}: {t.dtype} {tuple(shape)} on {t.device}, expected {like.dtype} {tuple(like.shape)} on {like.device}")
     if len(shape) != 2 or shape[1] < 1:
         raise ValueError(f"{name} must be a matrix with one column at least")
@@ -451,12 +454,12 @@ def linear_i8(x, x_scale, w, w_scale, bias=None, activation="none", residual=Non
     if activation not in ACTIVATIONS:
         raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}")
     (xp, ld_x), (wp, ld_w) = _rows("x", x), _rows("w", w)
-    (rows, d_in), (d_out, k), device = x.shape, w.shape, x.device
-    if x.dtype != torch.int8 or w.dtype != torch.int8 or w.device != device or k != d_in:
-        raise ValueError(f"x and w must be int8 matrices of the same d_in on one device, not {x.dtype} {tuple(x.shape)} on {device} and {w.dtype} {tuple(w.shape)} on {w.device}")
+    (rows, d_in), (d_out, k), where = x.shape, w.shape, x.get_device()
+    if x.dtype != torch.int8 or w.dtype != torch.int8 or w.get_device() != where or k != d_in:
+        raise ValueError(f"x and w must be int8 matrices of the same d_in on one device, not {x.dtype} {tuple(x.shape)} on {x.device} and {w.dtype} {tuple(w.shape)} on {w.device}")
     for name, t, n in (("x_scale", x_scale, rows), ("w_scale", w_scale, d_out)):
-        if t.dtype != torch.float32 or t.device != device or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
-            raise ValueError(f"{name}: a dense float32 tensor [{n}] on {device} is expected")
+        if t.dtype != torch.float32 or t.get_device() != where or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
+            raise ValueError(f"{name}: a dense float32 tensor [{n}] on {x.device} is expected")
     if dtype is None:
         dtype = bias.dtype if bias is not None else residual.dtype if residual is not None else torch.bfloat16
     y = x.new_empty((rows, d_out), dtype=dtype)
@@ -475,7 +478,7 @@ def dropout(x, p, rng, site=0, residual=None):
     import torch
     L = load_library()
     (xp, ld_x), code, (rows, width) = _rows("x", x), _dtype_code(x), x.shape
-    if rng.dtype != torch.int64 or rng.device != x.device or rng.shape != (2,) or not rng.is_contiguous():
+    if rng.dtype != torch.int64 or rng.get_device() != x.get_device() or rng.shape != (2,) or not rng.is_contiguous():
         raise ValueError(f"rng: a dense int64 tensor [2] on {x.device} is expected")
     rp, ld_res = _rows("residual", residual, x) if residual is not None else (0, 0)
     y = _dense_like(x)
