@@ -665,6 +665,15 @@ __global__ __launch_bounds__(1024) void column_tops_kernel(ColumnsArgs a, uint32
 
 constexpr int kTileRows = 128, kTileCols = 64;
 
+// 16 bytes of a column, those of them that it has
+__device__ inline void store_line(int8_t* to, const int8_t* from, int left) {
+  if (left >= 16) {
+    *reinterpret_cast<u32x4_any*>(to) = *reinterpret_cast<const u32x4*>(from);
+  } else {
+    for (int j = 0; j < left; ++j) to[j] = from[j];
+  }
+}
+
 template <class T>
 __global__ __launch_bounds__(256) void columns_kernel(ColumnsArgs a, const uint32_t* tops, int chunks) {
   constexpr int E = kE<T>, STRIDE = kTileRows + 16, ACROSS = kTileCols / E, ITEMS = kTileRows / 4 * ACROSS / 256;
@@ -717,13 +726,72 @@ __global__ __launch_bounds__(256) void columns_kernel(ColumnsArgs a, const uint3
   for (int i = threadIdx.x; i < kTileCols * (kTileRows / 16); i += 256) {
     const int c = i / (kTileRows / 16), at = i % (kTileRows / 16) * 16;
     if (n0 + c >= a.width || m0 + at >= a.rows) continue;
-    int8_t* to = a.q + (int64_t)(n0 + c) * a.ld_q + m0 + at;
-    const int8_t* from = tile + c * STRIDE + at;
-    if (m0 + at + 16 <= a.rows) {
-      *reinterpret_cast<u32x4_any*>(to) = *reinterpret_cast<const u32x4*>(from);
-    } else {
-      for (int j = 0; j < a.rows - m0 - at; ++j) to[j] = from[j];
+    store_line(a.q + (int64_t)(n0 + c) * a.ld_q + m0 + at, tile + c * STRIDE + at, (int)(a.rows - m0 - at));
+  }
+}
+
+// Up to 1,024 rows: a workgroup has its 64 columns whole, in registers, and one launch without a workspace does both (bf16, 256 x 1,024: 5.0 us, two launches 6.8; 1,024 x
+// 8,192 10.8 and 12.3; 1,000 x 1,000 9.2 and 8.7, and the host's share is half)
+constexpr int kOneRows = 1024;
+
+template <class T>
+__global__ __launch_bounds__(1024) void whole_columns_kernel(ColumnsArgs a) {
+  constexpr int E = kE<T>, STRIDE = kOneRows + 16, ACROSS = kTileCols / E, ITEMS = kOneRows / 4 * ACROSS / 1024;
+  __shared__ uint32_t top[kTileCols];
+  __shared__ __attribute__((aligned(16))) int8_t tile[kTileCols * STRIDE];
+  const int n0 = (int)blockIdx.x * kTileCols, piece = (int)threadIdx.x % ACROSS, c = n0 + piece * E;
+  if (threadIdx.x < kTileCols) top[threadIdx.x] = 0;
+  auto row_of = [&](int i) { return (i * 1024 + (int)threadIdx.x) / ACROSS * 4; };
+  u32x4 raw[ITEMS][4];
+  uint32_t mine[E];
+#pragma unroll
+  for (int j = 0; j < E; ++j) mine[j] = 0;
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int m = row_of(i) + u;
+      raw[i][u] = m < a.rows && c < a.width ? load_own(static_cast<const T*>(a.x) + m * a.ld_x, c, a.width) : u32x4{0, 0, 0, 0};
     }
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      float v[E];
+      unpack<T>(raw[i][u], v);
+#pragma unroll
+      for (int j = 0; j < E; ++j) mine[j] = max(mine[j], magnitude(v[j]));
+    }
+#pragma unroll
+  for (int j = 0; j < E; ++j)
+#pragma unroll
+    for (int d = ACROSS; d < 64; d *= 2) mine[j] = max(mine[j], (uint32_t)__shfl_xor((int)mine[j], d));
+  __syncthreads();
+  if ((threadIdx.x & 63) < ACROSS) {
+#pragma unroll
+    for (int j = 0; j < E; ++j) atomicMax(&top[piece * E + j], mine[j]);
+  }
+  __syncthreads();
+  if (threadIdx.x < kTileCols && n0 + (int)threadIdx.x < a.width) a.scale[n0 + threadIdx.x] = scale_of(top[threadIdx.x]);
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i) {
+    if (row_of(i) >= a.rows) continue;
+    float v[4][E];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) unpack<T>(raw[i][u], v[u]);
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+      const double by = up_of(top[piece * E + j]);
+      *reinterpret_cast<uint32_t*>(tile + (piece * E + j) * STRIDE + row_of(i)) =
+          low_bytes(to_eight(v[0][j], by), to_eight(v[1][j], by), to_eight(v[2][j], by), to_eight(v[3][j], by));
+    }
+  }
+  __syncthreads();
+  const int along = (a.rows + 15) / 16;
+  for (int i = (int)threadIdx.x; i < kTileCols * along; i += 1024) {
+    const int line = i / along, at = i % along * 16;
+    if (n0 + line >= a.width) continue;
+    store_line(a.q + (int64_t)(n0 + line) * a.ld_q + at, tile + line * STRIDE + at, a.rows - at);
   }
 }
 
@@ -733,16 +801,17 @@ inline int column_chunks(int64_t rows, int64_t width) {       // of 128 rows and
   return (int)(want < most ? want : most);
 }
 template <class T>
-size_t columns_bytes(const ColumnsArgs& a) { return (size_t)column_chunks<T>(a.rows, a.width) * a.width * sizeof(uint32_t); }
+size_t columns_bytes(const ColumnsArgs& a) { return a.rows <= kOneRows ? 0 : (size_t)column_chunks<T>(a.rows, a.width) * a.width * sizeof(uint32_t); }
 
 template <class T>
 hipError_t columns(const ColumnsArgs& a, void* ws, hipStream_t s) {
+  if (a.rows <= kOneRows) return launch(whole_columns_kernel<T>, (a.width + kTileCols - 1) / kTileCols, 1024, s, a);   // (no rows: the scales)
   const int chunks = column_chunks<T>(a.rows, a.width);
-  const int rows_per = (a.rows + chunks - 1) / chunks > 0 ? (a.rows + chunks - 1) / chunks : 1;
+  const int rows_per = (a.rows + chunks - 1) / chunks;
   uint32_t* tops = static_cast<uint32_t*>(ws);
   hipError_t e = launch(column_tops_kernel<T>, (int64_t)chunks * ((a.width + 64 * kE<T> - 1) / (64 * kE<T>)), 1024, s, a, tops, rows_per);
   if (e != hipSuccess) return e;
-  const int64_t down = a.rows ? (a.rows + kTileRows - 1) / kTileRows : 1;           // (no rows: the scales)
+  const int64_t down = (a.rows + kTileRows - 1) / kTileRows;
   return launch(columns_kernel<T>, down * ((a.width + kTileCols - 1) / kTileCols), 256, s, a, (const uint32_t*)tops, chunks);
 }
 

@@ -112,7 +112,7 @@ def test_no_rows(lib, wide):
     assert lib.stgn_rms_norm_grad(C.byref(args), 1 << 30, n.value, None) == 0
     for columns in (0, 1):
         args = quantize_args(rows=0, columns=columns, width=wide, ld_x=wide, ld_q=wide)
-        assert lib.stgn_quantize_workspace(C.byref(args), C.byref(n)) == 0 and (n.value > 0) == (columns == 1)
+        assert lib.stgn_quantize_workspace(C.byref(args), C.byref(n)) == 0 and n.value == 0
     args = quantize_args(rows=0, width=wide, ld_x=wide, ld_q=wide)
     assert lib.stgn_quantize(C.byref(args), None, 0, None) == 0
     assert lib.stgn_dropout(C.byref(dropout_args(rows=0, width=wide, ld_x=wide, ld_y=wide, ld_residual=wide)), None) == 0
@@ -128,7 +128,7 @@ def test_null_arguments_and_workspaces(lib):
     args = norm_args()
     assert lib.stgn_rms_norm_workspace(C.byref(args), None, None) == 0
     assert lib.stgn_rms_norm_workspace(C.byref(args), C.byref(m), C.byref(n)) == 0 and n.value > 0 and m.value == 0
-    for call, args in ((lib.stgn_rms_norm_grad, args), (lib.stgn_quantize, quantize_args(columns=1))):
+    for call, args in ((lib.stgn_rms_norm_grad, args), (lib.stgn_quantize, quantize_args(columns=1, rows=2000, ld_q=2000))):
         if call is lib.stgn_quantize:
             assert lib.stgn_quantize_workspace(C.byref(args), C.byref(n)) == 0 and n.value > 0
         assert call(C.byref(args), None, n.value, None) == WORKSPACE

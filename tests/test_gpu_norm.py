@@ -121,7 +121,7 @@ def test_rows_in_8_bits(size, dt):
 
 
 @pytest.mark.parametrize("dt", TYPES, ids=str)
-@pytest.mark.parametrize("size", [(1, 1), (1, 300), (300, 1), (3, 7), (127, 65), (128, 64), (129, 63), (1000, 257), (4096, 96), (33, 5000), (2050, 770)], ids=str)
+@pytest.mark.parametrize("size", [(1, 1), (1, 300), (300, 1), (3, 7), (127, 65), (128, 64), (129, 63), (1000, 257), (1023, 65), (1024, 200), (1025, 64), (4096, 96), (33, 5000), (2050, 770)], ids=str)
 def test_columns_in_8_bits(size, dt):
     x, *_ = make(*size, dt)
     q, scale = binding.quantize(x.cuda(), columns=True)
