@@ -473,7 +473,55 @@ __device__ __forceinline__ void finish_eights(const Product& a, int m0, int n0, 
   }
 }
 
-// ... of any width, or a split's sums
+// ... of the eight that the output has in part: the 1 .. 7 columns from `part` on, which lanes of one group hold in one pair of blocks.  All lanes load, from
+// the output's last row where theirs is past it, so that nothing waits before everything is asked for (1,300 x 1,903 x 1,600: one after the other 24.6 us, so 22.8)
+template <class T, int NB, int MB>
+__device__ __forceinline__ void finish_part(const Product& a, int m0, int n0, i32x4 (&acc)[NB][MB], int part) {
+  const int lane = threadIdx.x & 63, m = m0 + (lane & 15), count = a.n - part;
+  i32x4 sums[2][MB];
+#pragma unroll
+  for (int x = 0; x < NB; x += 2) {
+    if ((part - n0) / 32 != x / 2) continue;                  // (uniform)
+#pragma unroll
+    for (int y = 0; y < MB; ++y) {
+      sums[0][y] = acc[x][y];
+      sums[1][y] = acc[x + 1][y];
+    }
+  }
+  float ls[7], rs[MB];
+  T bias[7], res[MB][7];
+#pragma unroll
+  for (int j = 0; j < 7; ++j) {
+    if (j >= count) continue;
+    ls[j] = a.l_scale[part + j];
+    if (a.bias) bias[j] = static_cast<const T*>(a.bias)[part + j];
+  }
+#pragma unroll
+  for (int y = 0; y < MB; ++y) {
+    const int64_t row = min(m + y * 16, a.m - 1);
+    rs[y] = a.r_scale[row];
+    if (!a.residual) continue;
+#pragma unroll
+    for (int j = 0; j < 7; ++j)
+      if (j < count) res[y][j] = static_cast<const T*>(a.residual)[row * a.ld_res + part + j];
+  }
+  const bool mine = (part - n0) % 32 / 8 == lane >> 4;
+#pragma unroll
+  for (int y = 0; y < MB; ++y) {
+    floatx4 v[2];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j / 4][j % 4] = j < 7 && j < count ? (float)sums[j / 4][y][j % 4] * rs[y] * ls[j < 7 ? j : 0] + (a.bias ? (float)bias[j < 7 ? j : 0] : 0.f) : 0.f;
+    activate<T>(a.act, v[0]);
+    activate<T>(a.act, v[1]);
+    if (!mine || m + y * 16 >= a.m) continue;
+    T* out = static_cast<T*>(a.out) + (m + y * 16) * a.ld_out + part;
+#pragma unroll
+    for (int j = 0; j < 7; ++j)
+      if (j < count) out[j] = (T)(v[j / 4][j % 4] + (a.residual ? (float)res[y][j] : 0.f));
+  }
+}
+
+// ... all of it (for outputs of eight columns and more), or a split's sums
 template <class T, int NB, int MB>
 __device__ __forceinline__ void finish_pairs(const Product& a, int split, int m0, int n0, i32x4 (&acc)[NB][MB]) {
   auto eights = [&](auto whole) {
@@ -485,28 +533,22 @@ __device__ __forceinline__ void finish_pairs(const Product& a, int split, int m0
       default: finish_eights<T, dense::ACT_NONE, WHOLE>(a, m0, n0, acc); break;
     }
   };
-  if (a.splits == 1 && m0 + MB * 16 <= a.m && n0 + NB * 16 <= a.n) return eights(std::true_type());
-  if (a.splits == 1 && a.n >= 8) {
-    eights(std::false_type());
-    if (n0 + NB * 16 <= a.n || a.n % 8 == 0) return;
-  }
-  const int lane = threadIdx.x & 63;
+  if (m0 >= a.m || n0 >= a.n) return;
+  if (a.splits > 1) {
+    const int lane = threadIdx.x & 63, m = m0 + (lane & 15), n = n0 + 8 * (lane >> 4);
 #pragma unroll
-  for (int y = 0; y < MB; ++y) {
-    const int64_t m = m0 + y * 16 + (lane & 15);
-    if (m >= a.m) continue;
+    for (int y = 0; y < MB; ++y)
 #pragma unroll
-    for (int x = 0; x < NB; ++x) {
-      const int n = n0 + x / 2 * 32 + 8 * (lane >> 4) + x % 2 * 4;
-      if (a.splits > 1) {
-        if (n < a.n) store_sums(a.part + (split * (int64_t)a.m + m) * a.n, n, a.n, acc[x][y]);
-      } else if (n < a.n && n >= a.n / 8 * 8) {               // (of an eight that the output has in part)
-        Ends<T> ends;
-        ends.ask(a, m, n);
-        ends.finish(a, m, n, acc[x][y]);
+      for (int x = 0; x < NB; ++x) {
+        const int c = n + x / 2 * 32 + x % 2 * 4;
+        if (m + y * 16 < a.m && c < a.n) store_sums(a.part + (split * (int64_t)a.m + m + y * 16) * a.n, c, a.n, acc[x][y]);
       }
-    }
+    return;
   }
+  if (m0 + MB * 16 <= a.m && n0 + NB * 16 <= a.n) return eights(std::true_type());
+  eights(std::false_type());
+  const int part = a.n / 8 * 8;
+  if (part < a.n && part < n0 + NB * 16) finish_part<T>(a, m0, n0, acc, part);
 }
 
 // 128 x 128 outputs a workgroup of four waves, two tiles of 128 bytes of k in LDS, one barrier a tile; two workgroups a CU, so that one's epilogue
@@ -692,10 +734,12 @@ inline bool whole_pieces(const Linear8Args& f) {
 //              reads 400 KB of operands a workgroup at most (256 x 2,048 x 4,096, 393 KB: 14.2, in 128 x 128 16.0; 128 x 4,096 x 8,192, 786 KB: 24.8 and
 //              19.7), with up to 16 rows 1 MB; rows that no 16 bytes align cost it three times that: 64 KB (100 x 1,000 x 999, 48 KB: 5.5, in 64 x 64 8.0;
 //              1,000 x 257 x 1,999, 192 KB: 16.0 and 12.3)
-//   256 x 256  whole tiles of 64 of k, long sums, and tiles that fill the 256 CUs' rounds to nine tenths: 8,192 x 4,096 x 4,096 157, in 128 x 128 174;
-//              2,048 x 8,192 x 4,096 81 and 91; but 5,000 x 4,096 x 4,096 (320 tiles) 119 and 108, 4,096 x 8,192 x 256 54.6 and 52.0
-//   128 x 128  from 2^31 multiplications on (padded) with 192 tiles and more, from 2^32 on with fewer: 8,192 x 512 x 512 9.9, in 64 x 64 12.4; 4,000 x 1,000 x 1,008 14.2 and
-//              17.8; but 1,500 x 1,500 x 1,504 19.4 and 17.0; k split to make a workgroup for every CU (200 x 4,096 x 4,096 in one 26.5, in four 18.1)
+//   256 x 256  whole tiles of 64 of k, long sums, more than 128 rows and columns, and tiles that fill the 256 CUs' rounds to nine tenths: 8,192 x 4,096 x 4,096 157, in 128 x 128
+//              174; 2,048 x 8,192 x 4,096 81 and 91; but 5,000 x 4,096 x 4,096 (320 tiles) 119 and 108, 4,096 x 8,192 x 256 54.6 and 52.0, 65,000 x 128 x 1,024 30.8 and 26.6
+//   128 x 128  from 64 rows and columns on: from 2^31 multiplications on (padded) where more than 512 tiles of 64 x 64 would be made, from 2^32 on with fewer: 8,192 x 512 x 512
+//              9.9, in 64 x 64 12.4; 1,536 x 1,536 x 1,536 14.2 and 17.8; but 512 x 4,096 x 1,024 11.3 and 10.4; 50,000 x 48 x 1,024 17.3 and 16.0; from 1.5 x 2^32 on for columns that are
+//              no eights (2,000 x 2,001 x 2,000 23.8 and 27.3; 1,300 x 1,903 x 1,600 22.8 and 19.3); k split to make a workgroup for every CU (200 x 4,096 x 4,096 in one 26.5, in
+//              four 18.1)
 //   64 x 64    everything smaller; by eight waves with up to 512 tiles, k split to make up to 512 workgroups of 512 bytes of k at least (64 x 8,192 x 8,191 in four 27.1,
 //              in two 33.3, in eight 31.1; 1,000 x 257 x 1,999 in three 12.3, in one 15.4; 70 x 64 x 8,192 in 16 8.6, in eight 9.4)
 // Rows that 16 bytes do not align are laid out again where that makes one of the larger kernels possible, with 192 tiles of 128 x 128 and more and 128 rows and
@@ -725,9 +769,10 @@ inline Plan plan_of(int64_t m, int64_t n, int64_t k, bool whole, bool align) {
     q.aligned = (int)up(k, 64);
     if (q.kind >= kDirect) return q;
   }
-  if (whole && k % 64 == 0 && k >= 1024 && large * 10 >= rounds * 256 * 9) {
+  const int64_t least = n % 8 ? 3 << 17 : small > 512 ? 1 << 17 : 1 << 18;
+  if (whole && m > 128 && n > 128 && k % 64 == 0 && k >= 1024 && large * 10 >= rounds * 256 * 9) {
     p.kind = kLarge;
-  } else if (whole && middle * k >= (middle >= 192 ? 1 << 17 : 1 << 18)) {
+  } else if (whole && m >= 64 && n >= 64 && middle * k >= least) {
     p.kind = kDirect;
     split(middle, 256, 8);
   } else {

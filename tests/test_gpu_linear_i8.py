@@ -151,11 +151,11 @@ def test_rows_past_32_bits(size):
 
 
 # one size and more for each kernel and its edges: fragments of every shape; tiles of 64 x 64 in one sum and in several; 128 x 128 directly, with k that ends
-# inside a tile, in one sum and in several; 256 x 256, whole and cut; outputs of fewer columns than an eight and of a few more; rows that no
+# inside a tile, in one sum and in several; 256 x 256, whole and cut; outputs of few columns and a part of an eight; rows that no
 # 16 bytes align laid out again for each of them
 KINDS = [(16, 512, 4000), (33, 512, 2000), (100, 640, 1250), (60, 1500, 8100), (1000, 272, 1000), (500, 1027, 900), (300, 3001, 200), (2100, 4001, 2050), (2100, 1040, 2050),
-         (200, 4112, 4096), (1500, 2048, 1530), (2000, 512, 4090), (3900, 1088, 4090), (4096, 1024, 4096), (25000, 704, 5), (60000, 1024, 5), (60000, 1024, 13),
-         (4000, 1001, 1000), (8190, 1023, 2048), (1999, 2050, 2001), (20000, 33, 2000), (20000, 17, 2003)]
+         (200, 4112, 4096), (1500, 2048, 1530), (2000, 512, 4090), (3900, 1088, 4090), (4096, 1024, 4096), (25000, 704, 5), (60000, 1024, 5), (60000, 1024, 13), (60000, 1024, 69), (40000, 1024, 135),
+         (4000, 1001, 1000), (8190, 1023, 2048), (1999, 2050, 2001), (20000, 33, 2000), (20000, 17, 2000), (20000, 17, 2003)]
 
 
 @pytest.mark.parametrize("dt", TYPES, ids=str)

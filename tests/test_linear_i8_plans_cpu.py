@@ -54,6 +54,8 @@ def test_tiles_that_go_into_lds_directly_are_whole_pieces(plans):
             assert rows == UNALIGNED and k > 16 and aligned % 64 == 0 and k <= aligned < k + 64 and kind in (DIRECT, LARGE), (m, n, k)
         if kind in (DIRECT, LARGE):
             assert (rows == WHOLE or aligned) and (aligned or k) % 16 == 0 and k_per % 128 == 0, (m, n, k)
+        if kind in (DIRECT, LARGE):
+            assert n >= 8, (m, n, k)                          # their epilogue goes by eights
         if kind == LARGE:
             assert (aligned or k) % 64 == 0 and splits == 1, (m, n, k)
 
