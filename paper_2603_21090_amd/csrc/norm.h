@@ -528,7 +528,7 @@ __global__ __launch_bounds__(1024) void long_grad_kernel(NormGradArgs a, float* 
     });
   }
 }
-// ... the sums of 256 columns over a chunk of rows
+// ... the sums of 256 columns over a chunk of rows.  h r first, whose magnitude is the root of the width at most: dy h may be past what 32 bits hold where dy h r is not
 template <class T>
 __global__ __launch_bounds__(256) void long_gain_kernel(NormGradArgs a, const float* r, float* part, int rows_per) {
   __shared__ floatx4 wsum[4][64];
@@ -539,7 +539,7 @@ __global__ __launch_bounds__(256) void long_gain_kernel(NormGradArgs a, const fl
   if (n < a.width) {
 #pragma unroll 4
     for (int64_t m = chunk * rows_per + wave; m < m1; m += 4)
-      acc += load4(static_cast<const T*>(a.dy) + m * a.ld_dy, n, a.width) * load4(static_cast<const T*>(a.h) + m * a.ld_h, n, a.width) * r[m];
+      acc += load4(static_cast<const T*>(a.dy) + m * a.ld_dy, n, a.width) * (load4(static_cast<const T*>(a.h) + m * a.ld_h, n, a.width) * r[m]);
   }
   wsum[wave][lane] = acc;
   __syncthreads();
