@@ -26,10 +26,10 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-// rows of odd widths start anywhere: global memory takes wide accesses at any element's address
+// rows of odd widths start anywhere, those of 8-bit numbers at any byte: global memory takes wide accesses at any address
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(1)));
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
-typedef uint32_t u32_any __attribute__((aligned(2), may_alias));
+typedef uint32_t u32_any __attribute__((aligned(1), may_alias));
 
 template <class T> struct Elem;
 
