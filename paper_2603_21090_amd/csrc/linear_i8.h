@@ -222,21 +222,22 @@ __global__ __launch_bounds__(512) void fragments_kernel(Product a) {
 
 // ---- tiles through registers
 
-// 64 x 64 outputs a workgroup, any alignment.  HALVES = 1: four waves, three tiles of 128 bytes of k on their way in registers while one is multiplied.  HALVES
+// 64 x 64 outputs a workgroup, any alignment.  HALVES = 1: four waves, all of k, three tiles of 128 bytes of k on their way in registers while one is multiplied.  HALVES
 // = 2, for few workgroups, where what a tile takes is a wait: eight waves, tiles of 256 bytes, either half of the waves takes one half and at the end finishes
 // one half of the rows (1,531 x 777 x 1,027: 13.6 us, by four waves 15.5; 500 x 1,027 x 900 8.6 and 11.3; but 6,000 x 500 x 1,001 19.7 and 17.5).
 template <class T, int HALVES>
 __global__ __launch_bounds__(HALVES * 256, 4) void product_kernel(Product a) {
   using El = Elem<int8_t>;
   constexpr int BM = 64, BN = 64, BK = HALVES * kBK, THREADS = HALVES * 256, MB = 2, NB = 2, DEPTH = HALVES == 1 ? 3 : 1, S = lds_stride<int8_t>(BK);
+  constexpr bool SPLITS = HALVES == 2;                        // (few tiles; more of them are enough without)
   __shared__ __attribute__((aligned(16))) int8_t ls[BN * S], rs[BM * S];
   const int wave = threadIdx.x >> 6, half = wave >> 2, wm = wave % 2 * MB * 16, wn = wave / 2 % 2 * NB * 16;
   const unsigned tm = (unsigned)(a.m + BM - 1) / BM, tn = (unsigned)(a.n + BN - 1) / BN;
-  const int split = (int)(blockIdx.x / (tm * tn));
+  const int split = SPLITS ? (int)(blockIdx.x / (tm * tn)) : 0;
   int row, col;
-  dense::tile_of(blockIdx.x % (tm * tn), tm, tn, row, col);
+  dense::tile_of(SPLITS ? blockIdx.x % (tm * tn) : blockIdx.x, tm, tn, row, col);
   const int m0 = row * BM, n0 = col * BN;
-  const int kb = split * a.k_per, ke = min(a.k, kb + a.k_per);
+  const int kb = SPLITS ? split * a.k_per : 0, ke = SPLITS ? min(a.k, kb + a.k_per) : a.k;
 
   using MoveL = ProductMove<int8_t, BN, BK, THREADS, true>;
   using MoveR = ProductMove<int8_t, BM, BK, THREADS, true>;
@@ -293,7 +294,7 @@ __global__ __launch_bounds__(HALVES * 256, 4) void product_kernel(Product a) {
   for (int y = 0; y < ROWS; ++y)
 #pragma unroll
     for (int x = 0; x < NB; ++x)
-      if (a.splits == 1 && line(y) < a.m && n + x * 16 < a.n) ends[y][x].ask(a, line(y), n + x * 16);
+      if ((!SPLITS || a.splits == 1) && line(y) < a.m && n + x * 16 < a.n) ends[y][x].ask(a, line(y), n + x * 16);
   if constexpr (HALVES == 2) {
     __shared__ i32x4 part[8][NB][64];
 #pragma unroll
@@ -307,7 +308,7 @@ __global__ __launch_bounds__(HALVES * 256, 4) void product_kernel(Product a) {
 #pragma unroll
     for (int x = 0; x < NB; ++x) {
       if (line(y) >= a.m || n + x * 16 >= a.n) continue;
-      if (a.splits > 1) store_sums(a.part + (split * (int64_t)a.m + line(y)) * a.n, n + x * 16, a.n, acc[x][y]);
+      if (SPLITS && a.splits > 1) store_sums(a.part + (split * (int64_t)a.m + line(y)) * a.n, n + x * 16, a.n, acc[x][y]);
       else ends[y][x].finish(a, line(y), n + x * 16, acc[x][y]);
     }
   }
@@ -521,8 +522,8 @@ __device__ __forceinline__ void finish_part(const Product& a, int m0, int n0, i3
   }
 }
 
-// ... all of it (for outputs of eight columns and more), or a split's sums
-template <class T, int NB, int MB>
+// ... all of it (for outputs of eight columns and more), or with SPLITS a split's sums
+template <class T, bool SPLITS, int NB, int MB>
 __device__ __forceinline__ void finish_pairs(const Product& a, int split, int m0, int n0, i32x4 (&acc)[NB][MB]) {
   auto eights = [&](auto whole) {
     constexpr bool WHOLE = decltype(whole)::value;
@@ -534,7 +535,7 @@ __device__ __forceinline__ void finish_pairs(const Product& a, int split, int m0
     }
   };
   if (m0 >= a.m || n0 >= a.n) return;
-  if (a.splits > 1) {
+  if (SPLITS && a.splits > 1) {
     const int lane = threadIdx.x & 63, m = m0 + (lane & 15), n = n0 + 8 * (lane >> 4);
 #pragma unroll
     for (int y = 0; y < MB; ++y)
@@ -605,7 +606,7 @@ __global__ __launch_bounds__(256, 2) void direct_kernel(Product a) {
         for (int y = 0; y < MB; ++y) acc[x][y] = Elem<int8_t>::mma(lf[x], rf[y], acc[x][y]);
     }
   }
-  finish_pairs<T, NB, MB>(a, split, m0 + wm, n0 + wn, acc);
+  finish_pairs<T, true>(a, split, m0 + wm, n0 + wn, acc);
 }
 
 // until `tiles` of this wave's latest tiles of LOADS loads are on their way at most
@@ -633,15 +634,14 @@ __global__ __launch_bounds__(512) void turns_kernel(Product a) {
   __shared__ __attribute__((aligned(16))) int8_t lds[BUFS * TILE];        // the columns' tile | the rows' tile, BUFS times
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wm = wave % WM * MB * 16, wn = wave / WM * NB * 16;
   const unsigned tm = (unsigned)(a.m + BM - 1) / BM, tn = (unsigned)(a.n + BN - 1) / BN;
-  const int split = (int)(blockIdx.x / (tm * tn));
   int row, col;
-  dense::tile_of(blockIdx.x % (tm * tn), tm, tn, row, col);
-  const int m0 = row * BM, n0 = col * BN, kb = split * a.k_per, tiles = (min(a.k, kb + a.k_per) - kb) / BK;
+  dense::tile_of(blockIdx.x, tm, tn, row, col);
+  const int m0 = row * BM, n0 = col * BN, tiles = a.k / BK;
   DirectMove<BK, true, BN, 8, false> ml;
   DirectMove<BK, false, BM, 8, false> mr;
   static_assert(decltype(ml)::LOADS + decltype(mr)::LOADS == LOADS, "loads of a tile and wave");
-  ml.start(a.l, a.ld_l, n0, a.n, kb, wave);
-  mr.start(a.r, a.ld_r, m0, a.m, kb, wave);
+  ml.start(a.l, a.ld_l, n0, a.n, 0, wave);
+  mr.start(a.r, a.ld_r, m0, a.m, 0, wave);
   const uint32_t to = lds_address(lds);
   auto issue = [&](int buf) {
     ml.issue(to + buf * TILE, wave, BK);
@@ -680,7 +680,7 @@ __global__ __launch_bounds__(512) void turns_kernel(Product a) {
     buf = buf == BUFS - 1 ? 0 : buf + 1;
   }
   if (wave < 4) meet_here();
-  finish_pairs<T, NB, MB>(a, split, m0 + wm, n0 + wn, acc);
+  finish_pairs<T, false>(a, 0, m0 + wm, n0 + wn, acc);
 }
 
 // Sums of the splits and the epilogue, four outputs a thread

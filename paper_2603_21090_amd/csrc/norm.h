@@ -797,7 +797,7 @@ __global__ __launch_bounds__(1024) void whole_columns_kernel(ColumnsArgs a) {
 
 template <class T>
 inline int column_chunks(int64_t rows, int64_t width) {       // of 128 rows and more, a workgroup for every CU
-  const int64_t cols = (width + 64 * kE<T> - 1) / (64 * kE<T>), want = (256 + cols - 1) / cols, most = rows <= 128 ? 1 : (rows + 127) / 128;
+  const int64_t cols = (width + 64 * kE<T> - 1) / (64 * kE<T>), want = (256 + cols - 1) / cols, most = (rows + 127) / 128;
   return (int)(want < most ? want : most);
 }
 template <class T>
