@@ -375,7 +375,7 @@ int stgn_attention_grad(const stgn_attention_args *args, void *device_workspace,
  * zeros in q.  The sum of squares and r are computed in fp64, r is rounded to fp32 (3.4e38 at most: with eps = 0 a row of zeros stays zeros, and has no finite
  * gradient): q depends on the inputs alone.
  * Gradient, from dy and h: dx = r gain dy - h r^3 mean(gain dy h) + dh, which is the gradient of x and of the residual; dgain = column sums of dy h r.  dh (what comes
- * down the residual stream) may be NULL; a gradient whose pointer is NULL is not computed.
+ * down the residual stream) may be NULL; a gradient whose pointer is NULL is not computed.  gain dy is an fp32 product (infinite past 3.4e38, whatever r is).
  * x, residual, h, y, dy, dh: [rows x width]; rows lie ld_* elements apart, the numbers of a row side by side; q: int8 [rows x width], scale: fp32 [rows];
  * gain, dgain: [width]; dx is dense.  rows may be 0 (dgain is then zeros), width lies in 1 .. 2^24, eps is finite and not negative.  Outputs overlap nothing, except
  * that h and y may each be exactly x or exactly the residual (not both the same); tensors of equal ld_* may be different columns of one matrix. */

@@ -9,6 +9,9 @@
 //   64 x 64    tiles through registers into LDS, any alignment, k split where tiles are few
 //   128 x 128  tiles from memory into LDS directly, for operands in whole pieces of 16 bytes, or laid out so first
 //   256 x 256  directly too, in turns: two groups of four waves, one multiplying while the other reads
+// Sizes in these comments are rows x columns x k.  Figures are us of kernels with bf16 outputs, bias, gelu and residual, launched one after the other from a program in C++, up to
+// four sets of operands and outputs in turn; where two are given for one size, both are of one run, and another run's or card's are up to a tenth off.  Through the binding,
+// where a result takes the place of the one before it, the same kernels take less (8,192 x 4,096 x 4,096 141 us, 155 here).
 #pragma once
 #include <utility>
 
@@ -126,8 +129,8 @@ __device__ inline i32x4 piece_at(const int8_t* row, int k, int total) {
   return __builtin_bit_cast(i32x4, *reinterpret_cast<const u32x4_any*>(row + min(k, total - 16)));
 }
 
-// 16 MB rows and 16 NB columns a workgroup; eight waves take 128 bytes of k each in turn, four of their turns are on their way at once (4 x 4,096 x 4,096: 5.9
-// us, 2.9 TB/s of weights with the launch, and 11 in tiles of 64 x 64 with 8 splits and their joining; 1,024 x 1,024 x 1,024: 8.3 and 12)
+// 16 MB rows and 16 NB columns a workgroup; eight waves take 128 bytes of k each in turn, four of their turns are on their way at once (4 x 4,096 x 4,096: 5.7
+// us, 2.9 TB/s of weights with the launch, and 9.6 in tiles of 64 x 64 with 8 splits and their joining; 1,024 x 1,024 x 1,024: 7.9 and 8.3)
 template <class T, int MB, int NB>
 __global__ __launch_bounds__(512) void fragments_kernel(Product a) {
   constexpr int WAVES = 8, DEPTH = MB + NB > 6 ? 2 : 4;
@@ -224,7 +227,7 @@ __global__ __launch_bounds__(512) void fragments_kernel(Product a) {
 
 // 64 x 64 outputs a workgroup, any alignment.  HALVES = 1: four waves, all of k, three tiles of 128 bytes of k on their way in registers while one is multiplied.  HALVES
 // = 2, for few workgroups, where what a tile takes is a wait: eight waves, tiles of 256 bytes, either half of the waves takes one half and at the end finishes
-// one half of the rows (1,531 x 777 x 1,027: 13.6 us, by four waves 15.5; 500 x 1,027 x 900 8.6 and 11.3; but 6,000 x 500 x 1,001 19.7 and 17.5).
+// one half of the rows (1,531 x 777 x 1,027: 13.2 us, by four waves 14.9; 500 x 1,027 x 900 8.7 and 11.3; but 6,000 x 500 x 1,001 20.6 and 17.2).
 template <class T, int HALVES>
 __global__ __launch_bounds__(HALVES * 256, 4) void product_kernel(Product a) {
   using El = Elem<int8_t>;
@@ -729,22 +732,22 @@ inline bool whole_pieces(const Linear8Args& f) {
   return whole_rows(f) && reinterpret_cast<uintptr_t>(f.x) % 16 == 0 && reinterpret_cast<uintptr_t>(f.w) % 16 == 0;
 }
 
-// Which kernel, by the number of tiles and the length of their sums (us, bf16 outputs with gelu, bias and residual; each pair is the two sides of a rule):
-//   fragments  the smallest tile that makes 256 workgroups at most (500 x 500 x 500: 32 x 32 3.8, 32 x 16 7.4, 32 x 64 4.4; 16 x 11,008 x 4,096: 32 x 64 12.7, 16 x 16 15.0) and
-//              reads 400 KB of operands a workgroup at most (256 x 2,048 x 4,096, 393 KB: 14.2, in 128 x 128 16.0; 128 x 4,096 x 8,192, 786 KB: 24.8 and
-//              19.7), with up to 16 rows 1 MB; rows that no 16 bytes align cost it three times that: 64 KB (100 x 1,000 x 999, 48 KB: 5.5, in 64 x 64 8.0;
-//              1,000 x 257 x 1,999, 192 KB: 16.0 and 12.3)
-//   256 x 256  whole tiles of 64 of k, long sums, more than 128 rows and columns, and tiles that fill the 256 CUs' rounds to nine tenths: 8,192 x 4,096 x 4,096 157, in 128 x 128
-//              174; 2,048 x 8,192 x 4,096 81 and 91; but 5,000 x 4,096 x 4,096 (320 tiles) 119 and 108, 4,096 x 8,192 x 256 54.6 and 52.0, 65,000 x 128 x 1,024 30.8 and 26.6
+// Which kernel, by the number of tiles and the length of their sums (each pair is the two sides of a rule, of one run):
+//   fragments  the smallest tile that makes 256 workgroups at most (500 x 500 x 500: 32 x 32 3.9, 32 x 16 4.9, 32 x 64 4.4; 16 x 11,008 x 4,096: 32 x 64 12.9, 16 x 16 15.2) and
+//              reads 400 KB of operands a workgroup at most (256 x 2,048 x 4,096, 393 KB: 14.4, in 128 x 128 15.9; 128 x 4,096 x 8,192, 786 KB: 24.7 and
+//              19.8), with up to 16 rows 1 MB; rows that no 16 bytes align cost it three times that: 64 KB (100 x 1,000 x 999, 48 KB: 5.6, in 64 x 64 8.2;
+//              1,000 x 257 x 1,999, 192 KB: 15.9 and 12.1)
+//   256 x 256  whole tiles of 64 of k, long sums, more than 128 rows and columns, and tiles that fill the 256 CUs' rounds to nine tenths: 8,192 x 4,096 x 4,096 155, in 128 x 128
+//              171; 2,048 x 8,192 x 4,096 80 and 90; but 5,000 x 4,096 x 4,096 (320 tiles) 120 and 108, 4,096 x 8,192 x 256 54.6 and 52.0, 65,000 x 128 x 1,024 30.7 and 26.3
 //   128 x 128  from 64 rows and columns on: from 2^31 multiplications on (padded) where more than 512 tiles of 64 x 64 would be made, from 2^32 on with fewer: 8,192 x 512 x 512
-//              9.9, in 64 x 64 12.4; 1,536 x 1,536 x 1,536 14.2 and 17.8; but 512 x 4,096 x 1,024 11.3 and 10.4; 50,000 x 48 x 1,024 17.3 and 16.0; from 1.5 x 2^32 on for columns that are
-//              no eights (2,000 x 2,001 x 2,000 23.8 and 27.3; 1,300 x 1,903 x 1,600 22.8 and 19.3); k split to make a workgroup for every CU (200 x 4,096 x 4,096 in one 26.5, in
+//              10.0, in 64 x 64 12.8; 1,536 x 1,536 x 1,536 14.2 and 17.7; but 512 x 4,096 x 1,024 11.4 and 10.8; 50,000 x 48 x 1,024 17.4 and 15.9; from 1.5 x 2^32 on for columns that are
+//              no eights (2,000 x 2,001 x 2,000 23.2 and 27.1; 1,300 x 1,903 x 1,600 22.8 and 19.1); k split to make a workgroup for every CU (200 x 4,096 x 4,096 in one 25.1, in
 //              four 18.1)
-//   64 x 64    everything smaller; by eight waves with up to 512 tiles, k split to make up to 512 workgroups of 512 bytes of k at least (64 x 8,192 x 8,191 in four 27.1,
-//              in two 33.3, in eight 31.1; 1,000 x 257 x 1,999 in three 12.3, in one 15.4; 70 x 64 x 8,192 in 16 8.6, in eight 9.4)
+//   64 x 64    everything smaller; by eight waves with up to 512 tiles, k split to make up to 512 workgroups of 512 bytes of k at least (64 x 8,192 x 8,191 in four 27.3,
+//              in two 33.4, in eight 31.2; 1,000 x 257 x 1,999 in three 12.1, in one 15.6)
 // Rows that 16 bytes do not align are laid out again where that makes one of the larger kernels possible, with 192 tiles of 128 x 128 and more and 128 rows and
-// columns (8,192 x 4,096 x 4,095: 168, in 64 x 64 as they are 461; 4,000 x 1,000 x 1,001 18.4 and 21.4; 50,000 x 128 x 1,001 36 and 44; but 6,000 x 500 x 1,001, 188 tiles,
-// 21.0 and 17.2; 100,000 x 64 x 4,095 281 and 163).
+// columns (8,192 x 4,096 x 4,095: 165, in 64 x 64 as they are 462; 4,000 x 1,000 x 1,001 18.5 and 21.0; 50,000 x 128 x 1,001 36 and 43; but 6,000 x 500 x 1,001, 188 tiles,
+// 20.6 and 17.2; 100,000 x 64 x 4,095 279 and 156).
 inline Plan plan_of(int64_t m, int64_t n, int64_t k, bool whole, bool align) {
   const auto tiles_of = [&](int64_t b) { return ((m + b - 1) / b) * ((n + b - 1) / b); };
   Plan p{kFragments, 1, (int)up(k, kBK), 0, 0, 0};

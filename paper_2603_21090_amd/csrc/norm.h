@@ -3,11 +3,14 @@
 //   h = x + residual,  r = 1 / sqrt(mean h^2 + eps),  y = h r g;       scale = max |y| / 127,  q = y 127 / max |y| to the nearest whole number
 //   dx = r (g dy - h r mean(r g dy h)) + dh,                            dg = column sums of dy h r
 //
-// Bytes bound all of it: a row is read once and stays in its lanes' registers between its sums and its outputs.  LANES lanes hold a row, up to 16
-// numbers each, as few lanes as hold it: 16 lanes (sixteen rows a workgroup, whose sums take four steps within a wave) to 1,024 (one row); longer rows are
+// Bytes bound all of it: a row is read once and stays in its lanes' registers between its sums and its outputs.  LANES lanes hold a row, 8 to 32
+// numbers each (by_width): 16 lanes (sixteen rows a workgroup, whose sums take four steps within a wave) to 1,024 (one row); longer rows are
 // read again.
 // The sum of squares is a sum of 64 bits: r, and with it a number in 8 bits whose value lies next to a border, then does not hang on the
 // order of the sum, and no magnitude of 32 bits overflows it.
+// Figures are of kernels launched one after the other from a program in C++, three sets of inputs and outputs in turn; where two are given for one size, both
+// are of one run, and another run's or card's are up to a tenth off.  Through the binding, where a result takes the place of the one before it, the same kernels take less (the norm of
+// 16,384 x 4,096 in bf16 44 us, 50 here).
 #pragma once
 #include <math.h>
 
@@ -153,7 +156,8 @@ constexpr int block_of(int lanes) { return lanes < 256 ? 256 : lanes; }
 enum Kind { kNorm, kNorm8, kRows8 };                          // y; 8 bits of y (and y); 8 bits of x
 
 // Rows whose pieces stay in registers.  All of a row is read before any of it is written: outputs may lie where the inputs do.  A workgroup walks down the rows: the
-// gain is read once, and the next row is on its way while one is summed and written (in bf16 16,384 x 4,096 57 -> 50 us, 30,000 x 2,000 57 -> 47).
+// gain is read once, and the next row is on its way while one is summed and written (bf16, a workgroup for every row or four and so: 30,000 x 1,027 56 us and 34,
+// 30,000 x 2,000 57 and 47, 16,384 x 4,096 in 8 bits 63 and 48, the norm alone 50 and 50).
 template <class T, int LANES, int NP, Kind KIND>
 __global__ __launch_bounds__(block_of(LANES), LANES == 512 ? 4 : 1) void rows_kernel(NormArgs a) {
   constexpr int E = kE<T>, PER = block_of(LANES) / LANES;
@@ -242,7 +246,8 @@ __global__ __launch_bounds__(block_of(LANES), LANES == 512 ? 4 : 1) void rows_ke
   }
 }
 
-// Rows longer than 1,024 lanes hold: read once a sum and once for the outputs.
+// Rows longer than 1,024 lanes hold: read once a sum and once for the outputs.  A workgroup a row: as many rows as there are CUs keep the card busy, fewer do not (bf16, 64 rows of 2^20
+// numbers 210 us, one 158).
 template <class T, Kind KIND>
 __global__ __launch_bounds__(1024) void long_rows_kernel(NormArgs a) {
   constexpr int E = kE<T>, LANES = 1024;
@@ -308,9 +313,11 @@ __global__ __launch_bounds__(1024) void long_rows_kernel(NormArgs a) {
 
 constexpr int64_t kMostBlocks = 1 << 20;                      // of a launch; more rows go round again
 
-// f(lanes, pieces) for the fewest lanes that hold a row, or longer() where none do.  16 numbers a lane keep four waves and more on a SIMD; twice that for
-// the widest rows only.  GRAD: 512 lanes at most there, whose registers hold what the gradient keeps of 32 numbers (1,024 lanes of 16, half the registers
-// each, spill: 4,096 x 16,384 in bf16 192 us, 118 so).
+// f(lanes, pieces) for the fewest lanes that hold a row with 16 numbers each, or longer() where none do.  A SIMD has four waves of such norms (three in fp32) and three of
+// their gradients (two in fp32).  32 numbers a lane for the widest rows, some of whose kernels spill (up to 24 registers), and for 16-bit rows of 1,025 to
+// 2,048: two waves a SIMD, but a row is one wave's and no sum goes through LDS (30,000 x 1,027 34 us, by 256 lanes of 8 numbers 40 with their best number of workgroups;
+// in 8 bits 41 and 50, its gradient 62 and 77; 30,000 x 2,000 47 and 49, 47 and 56, 79 and 84).  GRAD: 512 lanes at most there, whose registers hold what the gradient
+// keeps of 32 numbers (1,024 lanes of 16, half the registers each, spill: 4,096 x 16,384 in bf16 192 us, 118 so).
 template <class T, bool GRAD, class F, class L>
 hipError_t by_width(int width, F f, L longer) {
 #define STGN_HOLDS(lanes, numbers) \
@@ -351,8 +358,10 @@ hipError_t rows_of(const NormArgs& a, hipStream_t s) {
       [&](auto lanes, auto pieces) {
         constexpr int L = decltype(lanes)::value, N = decltype(pieces)::value;
         int64_t blocks = blocks_for(a.rows, L);
-        // four workgroups a CU, two of 512 lanes, one of 1,024 walk down the rows (16,384 x 4,096 in bf16: 50 us, a workgroup a row 52; in 8 bits 52 and 68).  With a
-        // residual, whose four streams keep memory busy anyhow, a workgroup a row (92 us, 101 walking).
+        // 1,024 workgroups walk down the rows, 512 of 512 lanes, 256 of 1,024: as many as the CUs hold at once of kernels with four waves a SIMD, of which some have more and some
+        // fewer (bf16, us with half as many, these, half as many again: 16,384 x 4,096 48, 50, 52, in 8 bits 64, 48, 49; 30,000 x 1,027 31, 34, 35, in 8 bits 40, 41, 43; 200,000 x 64 22, 18, 17).  With a
+        // residual, whose four streams keep memory busy anyhow, a workgroup a row (16,384 x 4,096 91 us, 100 walking, 30,000 x 2,000 85 and 95; but 30,000 x 1,027, whose rows
+        // no 16 bytes align, 70 and 57).
         const int64_t most = L <= 256 ? 1024 : L == 512 ? 512 : 256;
         if (!(KIND == kNorm && a.residual) && blocks > most) blocks = most;
         return launch(rows_kernel<T, L, N, KIND>, blocks, block_of(L), s, a);
@@ -371,7 +380,9 @@ __device__ inline Back back_of(double squares, double dots, int width, double ep
   return b;
 }
 
-// A workgroup walks down the rows and keeps the gain's gradient of its rows in registers: one partial sum a column and workgroup.
+// A workgroup walks down the rows and keeps the gain's gradient of its rows in registers: one partial sum a column and workgroup.  These sums are of 32 bits, as 64 would take
+// 16 to 32 registers more, and the parts are added up in 64: in fp32 dgain of 40,000 x 200 is 1.1e-7 off in the norm and 0.7e-7 where all of a column is added in 64 bits, of
+// 1,000,000 x 200 2.1e-7 and 0.6e-7; in 16 bits the result's own rounding hides it.
 template <class T, int LANES, int NP>
 __global__ __launch_bounds__(block_of(LANES)) void grad_kernel(NormGradArgs a, float* part) {
   constexpr int E = kE<T>, PER = block_of(LANES) / LANES;
@@ -583,7 +594,7 @@ GradPlan grad_plan(const NormGradArgs& a) {
         constexpr int L = decltype(lanes)::value;
         p.blocks = blocks_for(a.rows, L);
         // As many workgroups as the CUs hold at once, each of which has its partial sums (16 numbers a lane in fp32, 32, rows of 16 lanes and full ones of 256: two a CU;
-        // us, bf16: 51,480 x 777 with 512 workgroups 80, 768 72, 1,024 92; 78,125 x 512 72, 64, 65; 9,765 x 4,096 65, 68, 80)
+        // us, bf16: 51,480 x 777 with 512 workgroups 79, 768 71, 1,024 92; 78,125 x 512 73, 64, 66; 9,765 x 4,096 66, 68, 79)
         constexpr int NUMBERS = decltype(pieces)::value * kE<T>;
         const bool two = NUMBERS > 16 || (NUMBERS == 16 && (sizeof(T) == 4 || L == 16 || (L == 256 && a.width * 4 >= L * NUMBERS * 3)));
         const int64_t most = L > 256 ? 256 : two ? 512 : NUMBERS == 16 ? 768 : 1024;
